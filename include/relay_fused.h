@@ -41,7 +41,11 @@ typedef enum {
   RELAY_ERR_DEVICE = 7       /* the HIP runtime refused the launch */
 } relay_status;
 
-typedef enum { RELAY_F32 = 0, RELAY_F16 = 1, RELAY_I8 = 2, RELAY_I16 = 3 /* the 16/32 scheme only */ } relay_dtype;
+typedef enum {
+  RELAY_F32 = 0, RELAY_F16 = 1, RELAY_I8 = 2,
+  RELAY_I16 = 3,  /* the 16/32 scheme only */
+  RELAY_BF16 = 4  /* the operators of relay_attention.h only */
+} relay_dtype;
 /* RELAY_NHWC4_PADDED: input of a first-layer conv with c <= 4 channels, stored [n][h + 2*pad_h]
  * [wp][4] with the zero border, wp - w - 2*pad_w slack columns and channels c..3 all zero
  * (relay_pack_input_nhwc4 writes it from NCHW; relay_nhwc4_padded_shape gives hp, wp).  The

@@ -1,6 +1,6 @@
 """ctypes binding of librelayfused.so: argument marshalling only.
 
-Each function has the name of the C entry point it calls (include/relay_fused.h) and
+Each function has the name of the C entry point it calls (include/relay_fused.h, include/relay_attention.h) and
 takes torch tensors on the GPU purely as (pointer, shape) carriers; PyTorch supplies device
 memory and the stream, every step of the computation runs in the library's own kernels.
 There is no fallback: if the library is missing or a call fails, an exception is raised.
@@ -14,7 +14,7 @@ from typing import Sequence, Optional, Tuple
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librelayfused.so")
 
-RELAY_F32, RELAY_F16, RELAY_I8, RELAY_I16 = 0, 1, 2, 3
+RELAY_F32, RELAY_F16, RELAY_I8, RELAY_I16, RELAY_BF16 = 0, 1, 2, 3, 4
 RELAY_NCHW, RELAY_NHWC, RELAY_NHWC4_PADDED = 0, 1, 2
 HAS_BIAS, HAS_BN, HAS_RESIDUAL, RELU = 1, 2, 4, 8
 
@@ -111,6 +111,14 @@ SIGNATURES = {
     "relay_probe_mfma": [_I, _I, _I, _P, _P],
     "relay_probe_copy": [_P, _P, C.c_int64, _P],
     "relay_probe_grid_barrier": [_I, _I, C.c_uint32, _P, _P, _P],
+    "relay_rope_table": [_P, _P, _P],
+    "relay_rope": [_P, _P, _P, _P, _P, _P],
+    "relay_rope_append": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P],
+    "relay_paged_attention_workspace_bytes": [_P, C.POINTER(_SZ)],
+    "relay_paged_attention": [_P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P],
+    "relay_qdense_w4_packed_bytes": [_P, C.POINTER(_SZ)],
+    "relay_prepack_qdense_w4": [_P, _P, _P, _P, _P, _SZ, _P],
+    "relay_qdense_w4": [_P, _P, _P, _P, _P, _P, _P],
     "relay_launch_list_create": [_P, C.POINTER(_P)],
     "relay_launch_list_run": [_P, _P],
     "relay_launch_list_destroy": [_P],
@@ -594,6 +602,140 @@ def relay_conv2d_maxpool_kernel_name(d: ConvDesc) -> str:
     buf = C.create_string_buffer(128)
     _check(lib().relay_conv2d_maxpool_kernel_name(C.byref(d), buf, 128))
     return buf.value.decode()
+
+
+# --------------------------------------------------------- attention layers served from a paged cache
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
+
+
+class RopeTableDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "first", "rotary_dim", "scaling")] + \
+        [(n, C.c_double) for n in ("base", "factor", "slow", "fast", "original_len", "magnitude")]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "heads", "head_dim", "rotary_dim", "style", "inverse", "table_rows")] + \
+        [(n, C.c_int64) for n in ("x_token_stride", "x_head_stride", "y_token_stride", "y_head_stride")]
+
+
+class RopeAppendDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "q_heads", "kv_heads", "head_dim", "rotary_dim", "style", "table_rows",
+                                         "num_pages", "page_size")] + \
+        [(n, C.c_int64) for n in ("q_token_stride", "k_token_stride", "v_token_stride", "q_out_token_stride", "page_stride",
+                                  "slot_stride", "head_stride")]
+
+
+class PagedAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "tokens", "q_heads", "kv_heads", "head_dim", "num_pages", "page_size",
+                                         "pages_per_seq", "max_q_len", "max_kv_len", "causal", "window")] + [("scale", C.c_float)] + \
+        [(n, C.c_int64) for n in ("q_token_stride", "out_token_stride", "page_stride", "slot_stride", "head_stride")]
+
+
+class QDenseW4Desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "m", "n", "k", "group", "has_zeros")] + [("flags", C.c_uint32)] + \
+        [(n, C.c_int64) for n in ("x_stride", "y_stride")]
+
+
+def dtype_of(t) -> int:
+    """relay_dtype of a floating-point tensor."""
+    name = str(t.dtype)
+    codes = {"torch.float32": RELAY_F32, "torch.float16": RELAY_F16, "torch.bfloat16": RELAY_BF16}
+    if name not in codes:
+        raise RelayError(3, f"no relay_dtype for {name}")
+    return codes[name]
+
+
+def _contiguous_heads(t, name):
+    if t.stride(-1) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise RelayError(2, f"{name}: the heads of a token must be contiguous, strides {tuple(t.stride())}")
+    return t.stride(0)
+
+
+def rope_table_desc(rows, rotary_dim, base=10000.0, first=0, scaling=ROPE_PLAIN, factor=1.0, slow=1.0, fast=32.0,
+                    original_len=1.0, magnitude=1.0) -> RopeTableDesc:
+    return RopeTableDesc(rows, first, rotary_dim, scaling, base, factor, slow, fast, original_len, magnitude)
+
+
+def rope_desc(x, cos_sin, y, style=ROPE_HALF, inverse=False) -> RopeDesc:
+    """Descriptor of relay_rope from its tensors: x, y [tokens, heads, head_dim] (any strides of the first two axes), cos_sin
+    [rows, rotary_dim/2, 2].  Kept for calls with tensors of the same shapes and strides."""
+    if x.shape != y.shape or x.dtype != y.dtype or x.stride(2) != 1 or y.stride(2) != 1:
+        raise RelayError(2, "x and y must have one shape and type and contiguous heads")
+    return RopeDesc(dtype_of(x), x.shape[0], x.shape[1], x.shape[2], 2 * cos_sin.shape[1], style, 1 if inverse else 0,
+                    cos_sin.shape[0], x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+
+
+def rope_append_desc(q, k, v, cos_sin, q_out, cache, style=ROPE_HALF) -> RopeAppendDesc:
+    """Descriptor of relay_rope_append from its tensors.  q, q_out [tokens, q_heads, head_dim], k, v [tokens, kv_heads, head_dim];
+    cache: k_cache (v_cache has the same shape and strides), [pages, page_size, kv_heads, head_dim] in any order in memory."""
+    if k.shape != v.shape or q.shape != q_out.shape or cache.shape[2:] != k.shape[1:] or cache.stride(3) != 1:
+        raise RelayError(2, "shapes of q, k, v and the cache do not go together")
+    return RopeAppendDesc(dtype_of(q), q.shape[0], q.shape[1], k.shape[1], q.shape[2], 2 * cos_sin.shape[1], style, cos_sin.shape[0],
+                          cache.shape[0], cache.shape[1], _contiguous_heads(q, "q"), _contiguous_heads(k, "k"), _contiguous_heads(v, "v"),
+                          _contiguous_heads(q_out, "q_out"), cache.stride(0), cache.stride(1), cache.stride(2))
+
+
+def paged_attention_desc(q, cache, page_table, out, max_q_len: int, max_kv_len: int, scale: float, causal=True,
+                         window=0) -> PagedAttentionDesc:
+    """Descriptor of relay_paged_attention from its tensors: q, out [tokens, q_heads, head_dim], cache as rope_append_desc,
+    page_table [batch, pages_per_seq]."""
+    if q.shape != out.shape or cache.shape[3] != q.shape[2] or cache.stride(3) != 1 or page_table.stride(1) != 1 or \
+            (page_table.shape[0] > 1 and page_table.stride(0) != page_table.shape[1]):
+        raise RelayError(2, "shapes of q, out, the cache and the page table do not go together")
+    return PagedAttentionDesc(dtype_of(q), page_table.shape[0], q.shape[0], q.shape[1], cache.shape[2], q.shape[2], cache.shape[0],
+                              cache.shape[1], page_table.shape[1], max_q_len, max_kv_len, 1 if causal else 0, window, scale,
+                              _contiguous_heads(q, "q"), _contiguous_heads(out, "out"), cache.stride(0), cache.stride(1), cache.stride(2))
+
+
+def qdense_w4_desc(x, y, group: int, zeros=None, bias=None, residual=None, relu=False) -> QDenseW4Desc:
+    """Descriptor of relay_qdense_w4 from its tensors: x [m, k], y [m, n] with contiguous rows; residual with y's strides."""
+    if x.stride(1) != 1 or y.stride(1) != 1 or x.shape[0] != y.shape[0] or x.dtype != y.dtype:
+        raise RelayError(2, "x [m, k] and y [m, n] must have one type and contiguous rows")
+    if residual is not None and (residual.shape != y.shape or residual.stride() != y.stride()):
+        raise RelayError(2, "residual must have the shape and strides of y")
+    return QDenseW4Desc(dtype_of(x), x.shape[0], y.shape[1], x.shape[1], group, 0 if zeros is None else 1,
+                        flags_of(bias, None, residual, relu), x.stride(0), y.stride(0))
+
+
+def relay_rope_table(d: RopeTableDesc, cos_sin) -> None:
+    _check(lib().relay_rope_table(C.addressof(d), _ptr(cos_sin), _stream()))
+
+
+def relay_rope(d: RopeDesc, x, cos_sin, positions, y) -> None:
+    _check(lib().relay_rope(C.addressof(d), _ptr(x), _ptr(cos_sin), _ptr(positions), _ptr(y), _stream()))
+
+
+def relay_rope_append(d: RopeAppendDesc, q, k, v, cos_sin, positions, slots, q_out, k_cache, v_cache) -> None:
+    _check(lib().relay_rope_append(C.addressof(d), _ptr(q), _ptr(k), _ptr(v), _ptr(cos_sin), _ptr(positions), _ptr(slots), _ptr(q_out),
+                                   _ptr(k_cache), _ptr(v_cache), _stream()))
+
+
+def relay_paged_attention_workspace_bytes(d: PagedAttentionDesc) -> int:
+    b = _SZ()
+    _check(lib().relay_paged_attention_workspace_bytes(C.addressof(d), C.byref(b)))
+    return b.value
+
+
+def relay_paged_attention(d: PagedAttentionDesc, q, k_cache, v_cache, page_table, q_starts, kv_lens, out, workspace=None) -> None:
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().relay_paged_attention(C.addressof(d), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(q_starts),
+                                       _ptr(kv_lens), _ptr(out), _ptr(workspace) if ws_bytes else None, ws_bytes, _stream()))
+
+
+def relay_qdense_w4_packed_bytes(d: QDenseW4Desc) -> int:
+    b = _SZ()
+    _check(lib().relay_qdense_w4_packed_bytes(C.addressof(d), C.byref(b)))
+    return b.value
+
+
+def relay_prepack_qdense_w4(d: QDenseW4Desc, codes, scales, zeros, packed) -> None:
+    _check(lib().relay_prepack_qdense_w4(C.addressof(d), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(packed),
+                                         packed.numel() * packed.element_size(), _stream()))
+
+
+def relay_qdense_w4(d: QDenseW4Desc, x, packed, bias, residual, y) -> None:
+    _check(lib().relay_qdense_w4(C.addressof(d), _ptr(x), _ptr(packed), _ptr(bias), _ptr(residual), _ptr(y), _stream()))
 
 
 def relay_launch_list_create(hip_graph: int) -> int:

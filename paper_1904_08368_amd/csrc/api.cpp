@@ -11,13 +11,15 @@
 
 #include "../../include/relay_fused.h"
 #include "../../include/relay_fusion.h"
+#include "api_common.hpp"
 #include "fusion.hpp"
 #include "kernels.hpp"
 
 namespace {
-
 thread_local char g_err[256] = "";
+}
 
+namespace relay {
 relay_status fail(relay_status st, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -25,10 +27,15 @@ relay_status fail(relay_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
+}  // namespace relay
+
+namespace {
+
+using relay::fail;
 
 int esize_of(int dtype) { return dtype == RELAY_F32 ? 4 : (dtype == RELAY_F16 || dtype == RELAY_I16) ? 2 : dtype == RELAY_I8 ? 1 : 0; }
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+using relay::aligned;
 
 constexpr long kMaxElems = (1L << 31) - 1;  // kernels index activations with 32-bit element offsets
 
@@ -126,10 +133,7 @@ void finish_args(relay::ConvArgs& a) {
   a.n_major = (size_t)a.K * a.Kred > (size_t)a.N * a.H * a.W * a.C ? 1 : 0;
 }
 
-relay_status device_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return RELAY_OK;
-  return fail(RELAY_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-}
+using relay::device_status;
 
 // implicit-GEMM paths: which (dtype, layout, channel count) combinations have a kernel
 relay_status check_igemm_support(const relay_conv2d_desc* d) {

@@ -1,0 +1,283 @@
+"""Attention over a paged cache against 64 bits: one new token to many, ragged batches, grouped heads, every head size class, pages that end inside
+a tile, masks that leave a row nothing, values that must not be read."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f16": (torch.float16, 2.0 ** -11, 2.0 ** -24), "bf16": (torch.bfloat16, 2.0 ** -8, 2.0 ** -133)}
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1904_08368_amd import binding
+    return binding
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _case(dtype, lens, hq, hkv, dim, ps, seed=0, extra_pages=2, qstd=2.0, hnd=False):
+    """lens: (new, kv) of each sequence.  The slots that no key occupies hold NaN, and so does a page that no sequence has."""
+    g = np.random.default_rng(seed + dim + 7 * len(lens))
+    need = [(kv + ps - 1) // ps for _, kv in lens]
+    pages, per = sum(need) + extra_pages, max(max(need), 1)
+    tt = TYPES[dtype][0]
+    order = g.permutation(pages)
+    table = np.full((len(lens), per), -1, dtype=np.int32)
+    kc, vc = (torch.full((pages, ps, hkv, dim), float("nan"), dtype=tt) for _ in range(2))
+    at = 0
+    for b, (_, kv) in enumerate(lens):
+        table[b, :need[b]] = order[at:at + need[b]]
+        at += need[b]
+        for c in (kc, vc):
+            vals = torch.from_numpy(g.standard_normal((need[b] * ps, hkv, dim)).astype(np.float32)).to(tt)
+            vals[kv:] = float("nan")
+            c[torch.from_numpy(table[b, :need[b]]).long()] = vals.view(need[b], ps, hkv, dim)
+    starts = np.cumsum([0] + [n for n, _ in lens]).astype(np.int32)
+    q = torch.from_numpy((qstd * g.standard_normal((int(starts[-1]), hq, dim))).astype(np.float32)).to(tt)
+    if hnd:
+        kc, vc = (c.transpose(1, 2).contiguous().transpose(1, 2) for c in (kc, vc))
+    return dict(q=q, kc=kc, vc=vc, table=table, starts=starts, kv=np.array([kv for _, kv in lens], dtype=np.int32), dtype=dtype,
+                max_q=max(n for n, _ in lens), max_kv=max(kv for _, kv in lens), dim=dim)
+
+
+def _dev(t):
+    return t.to(DEV) if t.is_contiguous() else t.to(DEV, memory_format=torch.preserve_format)
+
+
+def _run(B, c, causal=True, window=0, workspace=True, scale=None, pad_rows=0):
+    scale = 1 / math.sqrt(c["dim"]) if scale is None else scale
+    q, kc, vc = _dev(c["q"]), _dev(c["kc"]), _dev(c["vc"])
+    out = torch.full((q.shape[0] + pad_rows, *q.shape[1:]), 9.0, dtype=q.dtype, device=DEV)
+    o = out[:q.shape[0]]
+    table, starts, kv = (torch.from_numpy(c[n]).to(DEV) for n in ("table", "starts", "kv"))
+    d = B.paged_attention_desc(q, kc, table, o, c["max_q"], c["max_kv"], scale, causal, window)
+    ws = torch.zeros(B.relay_paged_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV) if workspace else None
+    B.relay_paged_attention(d, q, kc, vc, table, starts, kv, o, ws)
+    torch.cuda.synchronize()
+    if pad_rows:
+        assert (out[q.shape[0]:] == 9).all()
+    return o, dict(d=d, q=q, kc=kc, vc=vc, table=table, starts=starts, kv=kv, ws=ws, scale=scale)
+
+
+def _verify(c, got, scale, causal=True, window=0):
+    want, mag, spread, keys = O.attention(_np(c["q"]), np.nan_to_num(_np(c["kc"])), np.nan_to_num(_np(c["vc"])), c["table"], c["starts"], c["kv"],
+                                          scale, causal, window)
+    _, u, tiny = TYPES[c["dtype"]]
+    tol = O.attention_tolerance(want, mag, spread, keys, np.nanmax(np.abs(_np(c["vc"])), initial=0.0), c["dim"], u, tiny)
+    got = _np(got)
+    assert not np.isnan(got).any()
+    assert (np.abs(got - want) <= tol).all(), (float((np.abs(got - want) / tol).max()), np.unravel_index((np.abs(got - want) / tol).argmax(), got.shape))
+    assert (got[keys == 0] == 0).all()
+
+
+def _both(B, c, causal=True, window=0):
+    for ws in (True, False):
+        got, s = _run(B, c, causal, window, ws, pad_rows=1)
+        _verify(c, got, s["scale"], causal, window)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [8, 64, 72, 80, 96, 128, 136, 192, 256])
+@pytest.mark.parametrize("lens,hq,hkv,ps", [([(1, 1)], 4, 1, 16), ([(1, 77), (1, 300), (1, 16)], 8, 2, 16), ([(3, 50), (1, 1), (20, 20)], 6, 2, 8)])
+def test_head_sizes(B, dtype, dim, lens, hq, hkv, ps):
+    _both(B, _case(dtype, lens, hq, hkv, dim, ps))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 4), (8, 1), (16, 1), (24, 1), (40, 2), (6, 2), (5, 5)])
+@pytest.mark.parametrize("lens", [[(1, 530)], [(2, 99), (1, 260)], [(70, 200), (17, 33)]])
+def test_head_groups(B, hq, hkv, lens):
+    _both(B, _case("f16", lens, hq, hkv, 64, 16))
+
+
+@pytest.mark.parametrize("ps", [1, 5, 16, 24, 64, 128, 300])
+@pytest.mark.parametrize("lens", [[(1, 257)], [(40, 290), (3, 64)]])
+def test_page_sizes(B, ps, lens):
+    _both(B, _case("bf16", lens, 8, 2, 128, ps))
+
+
+@pytest.mark.parametrize("new,kv", [(1, 1), (1, 31), (1, 32), (1, 33), (1, 1000), (2, 2), (15, 15), (16, 64), (17, 65), (33, 33), (63, 128), (64, 64), (65, 200), (129, 129), (200, 411)])
+def test_lengths_around_tiles(B, new, kv):
+    _both(B, _case("f16", [(new, kv)], 4, 2, 64, 16))
+
+
+@pytest.mark.parametrize("causal,window", [(True, 1), (True, 7), (True, 33), (True, 100), (False, 0), (False, 1), (False, 50), (True, 100000)])
+@pytest.mark.parametrize("lens", [[(1, 400), (1, 3)], [(90, 300), (40, 40)]])
+def test_masks(B, causal, window, lens):
+    _both(B, _case("f16", lens, 8, 4, 64, 16), causal, window)
+
+
+def test_sequences_without_tokens_or_keys_and_rows_that_see_nothing(B):
+    """More new tokens than keys: the first ones stand before the first key.  A sequence without keys, one without tokens, both."""
+    _both(B, _case("f16", [(0, 40), (5, 0), (0, 0), (20, 12), (1, 0), (3, 9)], 4, 2, 64, 16))
+    _both(B, _case("bf16", [(2, 0), (70, 40)], 4, 2, 128, 16))
+
+
+def test_many_ragged_sequences(B):
+    g = np.random.default_rng(8)
+    lens = [(int(g.integers(0, 4)), int(g.integers(4, 200))) for _ in range(37)]
+    _both(B, _case("bf16", lens, 8, 1, 128, 16))
+
+
+def test_long_sequence_is_shared_out(B):
+    c = _case("f16", [(1, 5003)], 8, 2, 128, 16)
+    _both(B, c)
+    got, s = _run(B, c)
+    # the same bits on every call with the same workspace, whoever arrives last
+    first = got.clone()
+    for _ in range(5):
+        got.fill_(7)
+        B.relay_paged_attention(s["d"], s["q"], s["kc"], s["vc"], s["table"], s["starts"], s["kv"], got, s["ws"])
+        torch.cuda.synchronize()
+        assert torch.equal(got, first)
+
+
+def test_workspace_serves_calls_of_other_sizes(B):
+    big, small = _case("f16", [(1, 4000), (1, 2500)], 8, 2, 128, 16), _case("f16", [(1, 900)], 4, 1, 64, 16)
+    got, s = _run(B, big)
+    ws = s["ws"]
+    for c in (small, big, small, big):
+        _, t = _run(B, c)
+        assert t["ws"].numel() <= ws.numel()
+        out = torch.full_like(t["q"], float("nan"))
+        B.relay_paged_attention(t["d"], t["q"], t["kc"], t["vc"], t["table"], t["starts"], t["kv"], out, ws)
+        torch.cuda.synchronize()
+        _verify(c, out, t["scale"])
+
+
+@pytest.mark.parametrize("lens", [[(1, 90)], [(40, 90)], [(130, 300)]])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_unseen_keys_do_not_reach_a_result(B, lens, dtype, value):
+    """The newest key and value hold an infinity or a NaN: the tokens before see a cache without it, the last one does not."""
+    c = _case(dtype, lens, 4, 2, 64, 16)
+    new, kv = lens[0]
+    page, slot = int(c["table"][0, (kv - 1) // 16]), (kv - 1) % 16
+    clean = {k: (v.clone() if torch.is_tensor(v) else v) for k, v in c.items()}
+    for name in ("kc", "vc"):
+        c[name][page, slot] = value
+        clean[name][page, slot] = 0
+    got, s = _run(B, c)
+    ref, _ = _run(B, clean)
+    assert torch.equal(got[:-1], ref[:-1]) or new == 1
+    if new > 1:
+        ok = {**clean, "q": clean["q"]}
+        _verify({**ok, "starts": ok["starts"]}, torch.cat([got[:-1], ref[-1:]]), s["scale"])
+    assert not torch.isfinite(got[-1].float()).all()
+
+
+@pytest.mark.parametrize("lens", [[(1, 60)], [(50, 60)]])
+def test_infinite_values_that_are_seen(B, lens):
+    """A value of +inf in one channel, seen by some of the tokens: +inf there for them, the rest as without it."""
+    c = _case("f16", lens, 2, 2, 64, 16, qstd=0.5)
+    new, kv = lens[0]
+    j = kv - (new + 1) // 2
+    page, slot = int(c["table"][0, j // 16]), j % 16
+    c["vc"][page, slot, 0, 5] = float("inf")
+    got, s = _run(B, c)
+    sees = torch.arange(new) >= j - (kv - new)
+    assert (got[sees.to(DEV), 0, 5] == float("inf")).all()
+    got[sees.to(DEV), 0, 5] = 0
+    c["vc"][page, slot, 0, 5] = 0
+    ref, _ = _run(B, c)
+    ref[sees.to(DEV), 0, 5] = 0
+    assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_pages_outside_the_cache_are_not_read(B, new):
+    c = _case("f16", [(new, 100)], 4, 2, 64, 16)
+    c["table"][0, 1], c["table"][0, 4] = -5, 10 ** 6
+    got, s = _run(B, c)
+    _verify(c, got, s["scale"])
+    # every page bad: no key is read, whatever comes out
+    c["table"][:] = 1 << 30
+    _run(B, c)
+
+
+@pytest.mark.parametrize("lens", [[(1, 200)], [(60, 200)]])
+def test_extreme_scores(B, lens):
+    """Scores of +-1e4 and beyond: one key has all the weight, nothing overflows; and all scores equal: the mean."""
+    c = _case("f16", lens, 4, 2, 64, 16, qstd=100.0)
+    got, s = _run(B, c, scale=4.0)
+    assert torch.isfinite(got.float()).all()
+    want = O.attention(_np(c["q"]), np.nan_to_num(_np(c["kc"])), np.nan_to_num(_np(c["vc"])), c["table"], c["starts"], c["kv"], 4.0)[0]
+    # a score of up to 1e5 is off by 2^-24 x 66 x 1e5 = 0.4: rows whose two best scores are 40 apart have one winner all the same
+    assert np.median(np.abs(_np(got) - want)) <= 2.0 ** -10
+    c["q"].zero_()
+    got, s = _run(B, c)
+    _verify(c, got, s["scale"])
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_strided_tensors_and_head_major_cache(B, new):
+    """q as a range of a projection's rows, out as a range of a wider tensor, the cache with heads outside of the slots."""
+    c = _case("bf16", [(new, 180), (new, 70)], 4, 2, 64, 16, hnd=True)
+    t = c["q"].shape[0]
+    wide_q = torch.randn((t, 8 * 64), dtype=torch.bfloat16, device=DEV)
+    wide_q[:, 64:64 + 256] = c["q"].to(DEV).flatten(1)
+    wide_o = torch.full((t, 8 * 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    q, out = wide_q[:, 64:320].unflatten(1, (4, 64)), wide_o[:, 128:384].unflatten(1, (4, 64))
+    kc, vc = (c[n].transpose(1, 2).contiguous().to(DEV).transpose(1, 2) for n in ("kc", "vc"))
+    table, starts, kv = (torch.from_numpy(c[n]).to(DEV) for n in ("table", "starts", "kv"))
+    d = B.paged_attention_desc(q, kc, table, out, c["max_q"], c["max_kv"], 0.125)
+    ws = torch.zeros(B.relay_paged_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    B.relay_paged_attention(d, q, kc, vc, table, starts, kv, out, ws)
+    torch.cuda.synchronize()
+    _verify(c, out, 0.125)
+    assert (wide_o[:, :128] == 3).all() and (wide_o[:, 384:] == 3).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_offsets_beyond_32_bits(B, new):
+    """Pages 2^31 elements apart: a long cache's offsets pass 32 bits.  Only the pages themselves are written and read."""
+    c = _case("f16", [(new, 45)], 4, 2, 64, 16, extra_pages=0)
+    stride = (1 << 31) + 1024
+    big = [torch.empty(2 * stride + 16 * 2 * 64, dtype=torch.float16, device=DEV).as_strided((3, 16, 2, 64), (stride, 128, 64, 1)) for _ in range(2)]
+    for b, n in zip(big, ("kc", "vc")):
+        b.copy_(c[n].to(DEV))
+    q, out = c["q"].to(DEV), torch.empty_like(c["q"], device=DEV)
+    table, starts, kv = (torch.from_numpy(c[n]).to(DEV) for n in ("table", "starts", "kv"))
+    d = B.paged_attention_desc(q, big[0], table, out, c["max_q"], c["max_kv"], 0.125)
+    ws = torch.zeros(B.relay_paged_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    B.relay_paged_attention(d, q, big[0], big[1], table, starts, kv, out, ws)
+    torch.cuda.synchronize()
+    _verify(c, out, 0.125)
+
+
+def test_bounds_smaller_than_the_data_are_safe(B):
+    """max_q_len and max_kv_len below what the device holds: the rows within them are computed, the others left alone."""
+    c = _case("f16", [(5, 80)], 4, 2, 64, 16)
+    c["max_q"] = 3
+    got, s = _run(B, c)
+    assert (got[3:] == 9).all() and torch.isfinite(got[:3].float()).all()
+
+
+def test_side_stream_and_graph(B):
+    c = _case("f16", [(1, 3000), (1, 1200)], 8, 2, 128, 16)
+    got, s = _run(B, c)
+    want = got.clone()
+    side = torch.cuda.Stream()
+    out = torch.zeros_like(got)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.relay_paged_attention(s["d"], s["q"], s["kc"], s["vc"], s["table"], s["starts"], s["kv"], out, s["ws"])
+    side.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.relay_paged_attention(s["d"], s["q"], s["kc"], s["vc"], s["table"], s["starts"], s["kv"], out, s["ws"])
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
