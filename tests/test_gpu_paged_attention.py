@@ -132,6 +132,7 @@ def test_long_sequence_is_shared_out(B):
     c = _case("f16", [(1, 5003)], 8, 2, 128, 16)
     _both(B, c)
     got, s = _run(B, c)
+    assert s["ws"].numel() > 0
     # the same bits on every call with the same workspace, whoever arrives last
     first = got.clone()
     for _ in range(5):
@@ -216,6 +217,14 @@ def test_extreme_scores(B, lens):
     c["q"].zero_()
     got, s = _run(B, c)
     _verify(c, got, s["scale"])
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0])
+def test_scales(B, new, scale):
+    c = _case("f16", [(new, 150)], 4, 2, 64, 16, qstd=0.5)
+    got, s = _run(B, c, scale=scale)
+    _verify(c, got, scale)
 
 
 @pytest.mark.parametrize("new", [1, 50])
