@@ -60,7 +60,7 @@ struct AttnArgs {
   int num_pages, page_size, pages_per_seq;
   int max_q_len, max_kv_len, causal, window;
   float scale_log2;              // scale * log2(e)
-  FastDiv fd_page, fd_group;
+  FastDiv fd_page, fd_group, fd_kv_heads;
   int64_t q_token, out_token, page_stride, slot_stride, head_stride;
   void* workspace;
 };

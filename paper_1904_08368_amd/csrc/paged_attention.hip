@@ -1,350 +1,499 @@
 // Attention of new tokens over a paged cache:  o = sum_j softmax_j(scale q.k_j) v_j  over the keys a token sees.
 //
 // attn_rows_kernel: few query rows to a key head (a decode step, a short chunk).  A row is a token and one of the query heads that share the key
-// head, 16 rows to a workgroup: bound by the bytes of the keys and values, which every workgroup reads once for its 16 rows.  The workgroup's four
-// waves take blocks of 32 keys in turn, each with a softmax of its own: keys go from memory straight into the A operands of S^T = K Q^T,
-// values through a piece of LDS that only their wave uses, so that no wave waits for another before the end.  Where there are few workgroups,
-// a sequence's keys are shared out in chunks; partial results meet in the workspace.
+// head, 16 rows to a tile: bound by the bytes of the keys and values, which are read once for a tile's rows.  A workgroup's waves take blocks
+// of 32 keys in turn, each with a softmax of its own: keys go from memory straight into the A operands of S^T = K Q^T, values through a
+// piece of LDS that only their wave uses, so that no wave waits for another before the end.
+//
+// Lengths differ from sequence to sequence and are known on the device only.  So the work is dealt out there: a tile's keys are units
+// of a round of the waves, the units of all tiles stand in one line, and each of as many workgroups as fit the chip at once takes an equal
+// run of them.  A tile that lies within one run is finished by it; of others each workgroup leaves sums, maximum and weight in the
+// workspace, and the one that arrives last joins them in the order of the line.
+#include <type_traits>
+
 #include "attn_common.hpp"
 
 namespace relay {
 namespace {
 
-constexpr int kRows = 16, kBlock = 32, kWaves = 4;
+constexpr int kRows = 16, kBlock = 32;
 // Arrival counters lie 64 bytes apart in front of the workspace, in a region of their own that is the same for every call.
 constexpr int kCounters = 1024;
 constexpr size_t kCounterBytes = (size_t)kCounters * 64;
 
 struct RowsPlan {
-  int row_tiles, chunks, chunk;   // tiles of 16 rows of a sequence; chunks of `chunk` keys
+  int row_tiles;   // tiles of 16 rows of a sequence, at most
+  int deal;        // 1: units of all tiles are dealt out over the grid; 0: a workgroup to a tile
 };
 
 // floats that a workgroup leaves behind: sums [16][DP], then maximum and sum of each row
 template <int DP> constexpr int part_floats() { return kRows * DP + 2 * kRows; }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(const AttnArgs a, const RowsPlan pl) {
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// What one sequence brings to the line of units: its tiles (over all key heads), and the units of each.
+struct Share {
+  int tiles, units, lo, hi;
+  __device__ Share(const AttnArgs& a, const Seq& s, int round) {
+    const int nq = min(s.nq, a.max_q_len);
+    tiles = nq > 0 ? (int)(((long)nq * a.group + kRows - 1) / kRows) * a.kv_heads : 0;
+    lo = nq > 0 ? s.first(a, 0) : 0;
+    hi = nq > 0 ? s.last(a, nq - 1) + 1 : 0;
+    units = max(1, (hi - lo + round - 1) / round);
+  }
+};
+
+// Units of sequence b (none past the last).
+__device__ __forceinline__ int seq_units(const AttnArgs& a, int b, int round) {
+  if (b >= a.batch) return 0;
+  const Share sh(a, Seq(a, b), round);
+  return sh.tiles * sh.units;
+}
+// Units of all sequences, 64 at a time.
+__device__ __forceinline__ int all_units(const AttnArgs& a, int round, int lane) {
+  int total = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int n = seq_units(a, b0 + lane, round);
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    total += uniform(n);
+  }
+  return total;
+}
+// The sequence that a unit of the line lies in, and the units ahead of that sequence.
+struct Place { int b, before; };
+__device__ __forceinline__ Place find_unit(const AttnArgs& a, int unit, int round, int lane) {
+  int before = 0;
+  for (int b0 = 0;; b0 += 64) {
+    const int n = seq_units(a, b0 + lane, round);
+    int upto = n;   // units of this lane's sequence and those ahead of it among the 64
+    for (int o = 1; o < 64; o <<= 1) {
+      const int t = __shfl_up(upto, o, 64);
+      upto += lane >= o ? t : 0;
+    }
+    const unsigned long long past = __ballot(unit < before + upto);
+    if (past || b0 + 64 >= a.batch) {
+      const int at = past ? (int)__builtin_ctzll(past) : 63;
+      return {b0 + at, before + __builtin_amdgcn_readlane(upto - n, at)};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+}
+
+// FULL: head_dim is DP.  W: waves of a workgroup.
+template <typename T, int DP, bool FULL, int W>
+__global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(const AttnArgs a, const RowsPlan pl) {
   typedef Mma<T> M;
   typedef typename M::vec vec;
-  constexpr int KS = DP / 32, DT = DP / 16, PITCH = DP + 8;
+  constexpr int KS = DP / 32, DT = DP / 16, PITCH = DP + 8, ROUND = W * kBlock;
   static_assert(kBlock * PITCH * 2 >= kRows * DP * 4, "a wave's sums take the place of its values");
-  __shared__ __attribute__((aligned(16))) T vs[kWaves][kBlock * PITCH];
-  __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
+  __shared__ __attribute__((aligned(16))) T vs[W][kBlock * PITCH];
+  __shared__ float sm[W][kRows], sl[W][kRows];
   __shared__ int s_last;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
-  const int chunk_no = (int)blockIdx.x / pl.row_tiles, tile = (int)blockIdx.x - chunk_no * pl.row_tiles;
-  const int hk = (int)blockIdx.y, b = (int)blockIdx.z;
-  const Seq s(a, b);
-  const int rows = min(s.nq, a.max_q_len) * a.group, r0 = tile * kRows;
-  if (r0 >= rows) return;
-  const int i_min = (int)fast_div((unsigned)r0, a.fd_group), i_max = (int)fast_div((unsigned)min(r0 + kRows - 1, rows - 1), a.fd_group);
-  const int lo = s.first(a, i_min), hi = s.last(a, i_max) + 1;
-  const int active = pl.chunks == 1 ? 1 : max(1, (hi - lo + pl.chunk - 1) / pl.chunk);
-  if (chunk_no >= active) return;
-  const int c_lo = lo + chunk_no * pl.chunk, c_hi = min(hi, c_lo + pl.chunk);
-  // keys from full_lo to below full_hi are seen by all rows of the tile
-  const int full_lo = s.first(a, i_max), full_hi = s.last(a, i_min) + 1;
-  // this lane's row
-  const int r = r0 + col, ri = (int)fast_div((unsigned)min(r, rows - 1), a.fd_group);
-  const int token = s.start + ri, head = hk * a.group + min(r, rows - 1) - ri * a.group;
-  const bool row_ok = r < rows && (unsigned)token < (unsigned)a.tokens;
-  const int my_first = s.first(a, ri), my_last = s.last(a, ri);
-  const int D = a.head_dim;
-
-  vec qf[KS];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, col = lane & 15;
+  const int D = FULL ? DP : a.head_dim;
   // (a negative scale: of -q, so that the largest score is the largest; a scale of zero: of zeros)
   const unsigned flip = a.scale_log2 < 0.f ? 0x80008000u : 0u, keep = a.scale_log2 == 0.f ? 0u : 0xffffffffu;
   const float c = keep ? fabsf(a.scale_log2) : 1.f;
-#pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    uintx4 t = {0, 0, 0, 0};
-    if (row_ok && k * 32 + g * 8 < D)
-      t = *reinterpret_cast<const uintx4*>(static_cast<const T*>(a.q) + (long)token * a.q_token + (long)head * D + k * 32 + g * 8);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = (t[e] & keep) ^ flip;
-    qf[k] = __builtin_bit_cast(vec, t);
-  }
-  const int32_t* pages = a.page_table + (long)b * a.pages_per_seq;
-  const T* kbase = static_cast<const T*>(a.k) + (long)hk * a.head_stride + g * 8;
-  const T* vbase = static_cast<const T*>(a.v) + (long)hk * a.head_stride + g * 8;
-
-  // The place of this lane's two keys (col and col + 16 of a block) in the cache, and which of the block's 32 keys can be read.
-  long off[2] = {0, 0};
-  unsigned can = 0;
-  auto locate = [&](int j0) {
-    unsigned long long m[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int j = j0 + t * 16 + col;
-      const bool in = j < c_hi;
-      const int jj = in ? j : c_lo;
-      const unsigned pg = fast_div((unsigned)jj, a.fd_page);
-      const int page = pages[pg];
-      const bool ok = in && (unsigned)page < (unsigned)a.num_pages;
-      off[t] = ok ? (long)page * a.page_stride + (long)(jj - (int)pg * a.page_size) * a.slot_stride : 0;
-      m[t] = __ballot(ok);
-    }
-    can = ((unsigned)m[0] & 0xffffu) | ((unsigned)m[1] << 16);
-  };
-  uintx4 kf[2][KS], vf[2][KS];
-  auto fetch = [&]() {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        kf[t][k] = (uintx4){0, 0, 0, 0};
-        if (DP == D || k * 32 + g * 8 < D) kf[t][k] = *reinterpret_cast<const uintx4*>(kbase + off[t] + k * 32);
-      }
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        vf[t][k] = (uintx4){0, 0, 0, 0};
-        if (DP == D || k * 32 + g * 8 < D) vf[t][k] = *reinterpret_cast<const uintx4*>(vbase + off[t] + k * 32);
-      }
-  };
-
-  floatx4 acc[DT];
-#pragma unroll
-  for (int d = 0; d < DT; ++d) acc[d] = (floatx4){0, 0, 0, 0};
-  float m = kNegInf, l = 0.f;
   T* const myv = vs[wave];
-  int j0 = c_lo + wave * kBlock;
-  if (j0 < c_hi) {
-    locate(j0);
-    fetch();
+
+  // This workgroup's run of units.
+  const int w_no = (int)blockIdx.x;
+  int unit = 0, end = 1, run = 1;
+  if (pl.deal) {
+    const int total = all_units(a, ROUND, lane);
+    run = max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    unit = w_no * run;
+    end = min(total, unit + run);
   }
-  for (; j0 < c_hi; j0 += kWaves * kBlock) {
-    floatx4 st[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      st[t] = (floatx4){0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) st[t] = M::mfma16(__builtin_bit_cast(vec, kf[t][k]), qf[k], st[t]);
+  Place place = {0, 0};
+  int seq_end = 0;   // the first unit behind the sequence at hand
+
+  for (int piece = 0; unit < end; ++piece) {
+    if (!pl.deal) {
+      place.b = (int)blockIdx.z;
+    } else if (unit >= seq_end) {
+      place = find_unit(a, unit, ROUND, lane);
     }
-    const unsigned readable = can;
-    const bool whole = readable == 0xffffffffu && j0 >= full_lo && j0 + kBlock <= full_hi;   // (uniform)
-    unsigned long long odd = 0;   // keys with an infinity or a NaN among their values (bits 0..15, 32..47: first and second 16)
-    if (!whole) {
+    const int b = place.b;
+    const Seq s(a, b);
+    const Share sh(a, s, ROUND);
+    int in_seq, tile_unit = 0;   // tile of the sequence; its first unit
+    if (pl.deal) {
+      seq_end = place.before + sh.tiles * sh.units;
+      in_seq = uniform((unit - place.before) / sh.units);
+      tile_unit = place.before + in_seq * sh.units;
+    } else {
+      in_seq = (int)blockIdx.x * a.kv_heads + (int)blockIdx.y;
+      if (in_seq >= sh.tiles) return;
+    }
+    const int rows = min(s.nq, a.max_q_len) * a.group;
+    const int tile = (int)fast_div((unsigned)in_seq, a.fd_kv_heads), hk = in_seq - tile * a.kv_heads, r0 = tile * kRows;
+    const int stop = pl.deal ? min(end, tile_unit + sh.units) : end;
+    const bool whole_tile = !pl.deal || (unit == tile_unit && stop == tile_unit + sh.units);
+    const int i_min = (int)fast_div((unsigned)r0, a.fd_group), i_max = (int)fast_div((unsigned)min(r0 + kRows - 1, rows - 1), a.fd_group);
+    // the keys of this piece, as far as the tile's rows see them
+    const int lo = max(s.first(a, i_min), sh.lo + (unit - tile_unit) * ROUND);
+    const int hi = pl.deal ? min(s.last(a, i_max) + 1, sh.lo + (stop - tile_unit) * ROUND) : s.last(a, i_max) + 1;
+    // keys from full_lo to below full_hi are seen by all rows of the tile
+    const int full_lo = s.first(a, i_max), full_hi = s.last(a, i_min) + 1;
+    // this lane's row
+    const int r = r0 + col, ri = (int)fast_div((unsigned)min(r, rows - 1), a.fd_group);
+    const int token = s.start + ri, head = hk * a.group + min(r, rows - 1) - ri * a.group;
+    const bool row_ok = r < rows && (unsigned)token < (unsigned)a.tokens;
+    const int my_first = s.first(a, ri), my_last = s.last(a, ri);
+
+    const int32_t* pages = a.page_table + (long)b * a.pages_per_seq;
+    const T* kbase = static_cast<const T*>(a.k) + (long)hk * a.head_stride + g * 8;
+    const T* vbase = static_cast<const T*>(a.v) + (long)hk * a.head_stride + g * 8;
+
+    // Page numbers of this lane's two keys (col and col + 16 of a block), asked for a block before their keys: a look-up on the way would
+    // put a second trip through the caches into every block.
+    int pageno[2];
+    auto look_up = [&](int j0) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const bool ok = readable >> (t * 16 + col) & 1;
-        bool bad = false;
+        const int j = j0 + t * 16 + col;
+        pageno[t] = pages[fast_div((unsigned)(j < hi ? j : lo), a.fd_page)];
+      }
+    };
+    // The keys' places in the cache, and which of the block's 32 keys can be read.
+    long off[2] = {0, 0};
+    unsigned can = 0;
+    auto locate = [&](int j0) {
+      unsigned long long m[2];
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+      for (int t = 0; t < 2; ++t) {
+        const int j = j0 + t * 16 + col;
+        const bool ok = j < hi && (unsigned)pageno[t] < (unsigned)a.num_pages;
+        const int slot = j - (int)fast_div((unsigned)j, a.fd_page) * a.page_size;
+        const long at = (long)pageno[t] * a.page_stride + (long)slot * a.slot_stride;
+        off[t] = ok ? at : 0;
+        m[t] = __ballot(ok);
+      }
+      can = ((unsigned)m[0] & 0xffffu) | ((unsigned)m[1] << 16);
+    };
+    uintx4 kf[2][KS], vf[2][KS];
+    auto fetch = [&]() {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          if constexpr (!FULL) kf[t][k] = (uintx4){0, 0, 0, 0};
+          if (FULL || k * 32 + g * 8 < D) kf[t][k] = *reinterpret_cast<const uintx4*>(kbase + off[t] + k * 32);
+        }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          if constexpr (!FULL) vf[t][k] = (uintx4){0, 0, 0, 0};
+          if (FULL || k * 32 + g * 8 < D) vf[t][k] = *reinterpret_cast<const uintx4*>(vbase + off[t] + k * 32);
+        }
+    };
+
+    int j0 = lo + wave * kBlock;
+    if (j0 < hi) {
+      look_up(j0);
+      locate(j0);
+      fetch();
+      look_up(j0 + ROUND);
+    }
+    vec qf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      uintx4 t = {0, 0, 0, 0};
+      if (row_ok && (FULL || k * 32 + g * 8 < D))
+        t = *reinterpret_cast<const uintx4*>(static_cast<const T*>(a.q) + (long)token * a.q_token + (long)head * D + k * 32 + g * 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = (t[e] & keep) ^ flip;
+      qf[k] = __builtin_bit_cast(vec, t);
+    }
+    floatx4 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = (floatx4){0, 0, 0, 0};
+    float m = kNegInf, l = 0.f;
+    // One block: scores, softmax, output; in between the next block's keys and values are asked for.  MORE: there is a next one.  (As a
+    // condition inside the loop it would have the compiler keep two sets of them.)
+    auto block = [&](auto more) {
+      constexpr bool MORE = decltype(more)::value;
+      floatx4 st[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        st[t] = (floatx4){0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) st[t] = M::mfma16(__builtin_bit_cast(vec, kf[t][k]), qf[k], st[t]);
+      }
+      const unsigned readable = can;
+      unsigned long long odd = 0;   // keys with an infinity or a NaN among their values (bits 0..15, 32..47: first and second 16)
+      if (readable != 0xffffffffu || j0 < full_lo || j0 + kBlock > full_hi) {   // some of the rows may not see all of its keys
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bool ok = readable >> (t * 16 + col) & 1;
+          bool bad = false;
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned v = vf[t][k][e];
+              vf[t][k][e] = ok ? v : 0u;
+              bad |= ok && not_finite<T>(v);
+            }
+          unsigned long long bl = __ballot(bad);
+          bl |= bl >> 32;
+          odd |= ((bl | bl >> 16) & 0xffffull) << (32 * t);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            vf[t][k][e] = ok ? vf[t][k][e] : 0u;
-            bad |= not_finite<T>(vf[t][k][e]);
+            const int u = t * 16 + g * 4 + e, j = j0 + u;
+            const bool seen = (readable >> u & 1) && j >= my_first && j <= my_last;
+            st[t][e] = seen ? st[t][e] : kNegInf;
           }
-        unsigned long long bl = __ballot(bad);
-        bl |= bl >> 32;
-        odd |= ((bl | bl >> 16) & 0xffffull) << (32 * t);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
+        for (int k = 0; k < KS; ++k) *reinterpret_cast<uintx4*>(myv + (t * 16 + col) * PITCH + k * 32 + g * 8) = vf[t][k];
+      if constexpr (MORE) {
+        locate(j0 + ROUND);
+        fetch();
+        look_up(j0 + 2 * ROUND);
+      }
+      float bm = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
+      bm = max_quarters(bm);
+      const float mn = fmaxf(m, bm), base = mn == kNegInf ? 0.f : mn * c;
+      const float alpha = pow2(fmaf(m, c, -base));
+      m = mn;
+      float sum = 0.f;
+      uintx4 pw;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int u = t * 16 + g * 4 + e, j = j0 + u;
-          const bool seen = (readable >> u & 1) && j >= my_first && j <= my_last;
-          st[t][e] = seen ? st[t][e] : kNegInf;
+          st[t][e] = pow2(fmaf(st[t][e], c, -base));
+          sum += st[t][e];
         }
-    }
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) *reinterpret_cast<uintx4*>(myv + (t * 16 + col) * PITCH + k * 32 + g * 8) = vf[t][k];
-    if (j0 + kWaves * kBlock < c_hi) {
-      locate(j0 + kWaves * kBlock);
-      fetch();
-    }
-    float bm = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
-    bm = max_quarters(bm);
-    const float mn = fmaxf(m, bm), base = mn == kNegInf ? 0.f : mn * c;
-    const float alpha = pow2(fmaf(m, c, -base));
-    m = mn;
-    float sum = 0.f;
-    uintx4 pw;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        st[t][e] = pow2(fmaf(st[t][e], c, -base));
-        sum += st[t][e];
+      for (int t = 0; t < 2; ++t) {
+        pw[2 * t] = pack2<T>(st[t][0], st[t][1]);
+        pw[2 * t + 1] = pack2<T>(st[t][2], st[t][3]);
       }
+      l = fmaf(l, alpha, sum);
+      const vec pf = __builtin_bit_cast(vec, pw);
+      const T* at = myv + (g * 4 + (col >> 2)) * PITCH + (col & 3) * 4;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      pw[2 * t] = pack2<T>(st[t][0], st[t][1]);
-      pw[2 * t + 1] = pack2<T>(st[t][2], st[t][3]);
-    }
-    l = fmaf(l, alpha, sum);
-    const vec pf = __builtin_bit_cast(vec, pw);
+      for (int d = 0; d < DT; ++d) {
+        acc[d] *= alpha;
+        const uintx2 v0 = lds_transposed(at + d * 16), v1 = lds_transposed(at + d * 16 + 16 * PITCH);
+        uintx4 v = {v0[0], v0[1], v1[0], v1[1]};
+        // A product of zero and an infinity would be a NaN, also for the rows that do not see the key: such values are left
+        // out of the matrix product and go to the rows that see them one by one.
+        if (odd)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      acc[d] *= alpha;
-      const T* at = myv + (g * 4 + (col >> 2)) * PITCH + d * 16 + (col & 3) * 4;
-      const uintx2 v0 = lds_transposed(at), v1 = lds_transposed(at + 16 * PITCH);
-      uintx4 v = {v0[0], v0[1], v1[0], v1[1]};
+          for (int e = 0; e < 4; ++e) v[e] = only_finite<T>(v[e]);
+        acc[d] = M::mfma16(__builtin_bit_cast(vec, v), pf, acc[d]);
+      }
       if (odd) {
+        for (int u = 0; u < kBlock; ++u) {
+          if (!(odd >> (u + (u & 16)) & 1)) continue;
+          const bool seen = (readable >> u & 1) && j0 + u >= my_first && j0 + u <= my_last;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = only_finite<T>(v[e]);
-      }
-      acc[d] = M::mfma16(__builtin_bit_cast(vec, v), pf, acc[d]);
-    }
-    if (odd) {
-      // A product of zero and an infinity would be a NaN, also for the rows that do not see the key: these values were left
-      // out of the matrix product and go to the rows that see them one by one.
-      for (int u = 0; u < kBlock; ++u) {
-        if (!(odd >> (u + (u & 16)) & 1)) continue;
-        const bool seen = (readable >> u & 1) && j0 + u >= my_first && j0 + u <= my_last;
-        for (int d = 0; d < DT; ++d)
+          for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = (float)myv[u * PITCH + d * 16 + g * 4 + e];
-            if (seen && !__builtin_isfinite(v)) {
-#pragma unroll
-              for (int dd = 0; dd < DT; ++dd)
-                if (dd == d) acc[dd][e] += v;
+            for (int e = 0; e < 4; ++e) {
+              const float v = (float)myv[u * PITCH + d * 16 + g * 4 + e];
+              acc[d][e] += seen && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
             }
-          }
+        }
+      }
+    };
+    for (; j0 + ROUND < hi; j0 += ROUND) block(std::true_type());
+    if (j0 < hi) block(std::false_type());
+    l = sum_quarters(l);
+
+    // The waves' results, on the scale of the largest maximum.  (From here on by a copy of the thread's number that the compiler has to take
+    // as new in every piece: it would compute the addresses below ahead of all pieces and keep them in 60 registers.)
+    int tid_c = tid;
+    asm volatile("" : "+v"(tid_c));
+    const int col_c = tid_c & 15, g_c = (tid_c & 63) >> 4;
+    if (g_c == 0) {
+      sm[wave][col_c] = m;
+      sl[wave][col_c] = l;
+    }
+    __syncthreads();
+    float mt = kNegInf;
+#pragma unroll
+    for (int w = 0; w < W; ++w) mt = fmaxf(mt, sm[w][col_c]);
+    const float own = m == kNegInf ? 0.f : pow2((m - mt) * c);
+    float* const part = reinterpret_cast<float*>(vs[wave]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4*>(part + col_c * DP + d * 16 + g_c * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
+    __syncthreads();
+    const int live = min(kRows, rows - r0);
+    float* const slots = pl.deal ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) : nullptr;
+    float* const mine = pl.deal ? slots + (size_t)(2 * w_no + (piece > 0 ? 1 : 0)) * part_floats<DP>() : nullptr;
+
+    // one float4 of the output; row `cc` of the tile
+    auto put = [&](int cc, int d, floatx4 o, float lt) {
+      const int rr = r0 + cc, ii = (int)fast_div((unsigned)rr, a.fd_group);
+      const int tk = s.start + ii;
+      if ((unsigned)tk >= (unsigned)a.tokens) return;
+      const bool none = s.last(a, ii) < s.first(a, ii);
+      const float inv = 1.f / lt;
+      uintx2 w = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
+      if (none) w = (uintx2){0, 0};
+      *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)tk * a.out_token + (long)(hk * a.group + rr - ii * a.group) * D + d) = w;
+    };
+    for (int it = tid_c; it < live * (DP / 4); it += W * 64) {
+      const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
+      if (!FULL && d >= D) continue;
+      floatx4 o = {0, 0, 0, 0};
+      float mm = kNegInf, lt = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        o += *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(vs[w]) + cc * DP + d);
+        mm = fmaxf(mm, sm[w][cc]);
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w) lt += sm[w][cc] == kNegInf ? sl[w][cc] : sl[w][cc] * pow2((sm[w][cc] - mm) * c);
+      if (whole_tile) {
+        put(cc, d, o, lt);
+        continue;
+      }
+      *reinterpret_cast<floatx4*>(mine + cc * DP + d) = o;
+      if (d == 0) {
+        mine[kRows * DP + cc] = mm;
+        mine[kRows * DP + kRows + cc] = lt;
       }
     }
-  }
-  l = sum_quarters(l);
-
-  // The waves' results, on the scale of the largest maximum.
-  if (g == 0) {
-    sm[wave][col] = m;
-    sl[wave][col] = l;
-  }
-  __syncthreads();
-  float mt = kNegInf;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) mt = fmaxf(mt, sm[w][col]);
-  const float own = m == kNegInf ? 0.f : pow2((m - mt) * c);
-  float* const part = reinterpret_cast<float*>(vs[wave]);
-#pragma unroll
-  for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4*>(part + col * DP + d * 16 + g * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
-  __syncthreads();
-  const bool shared_out = active > 1;
-  const int tile_no = (b * a.kv_heads + hk) * pl.row_tiles + tile;
-  float* const ws = shared_out ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) + (size_t)tile_no * pl.chunks * part_floats<DP>() : nullptr;
-  float* const mine = shared_out ? ws + (size_t)chunk_no * part_floats<DP>() : nullptr;
-  const int live = min(kRows, rows - r0);
-
-  // one float4 of the output; row `cc` of the tile
-  auto put = [&](int cc, int d, floatx4 o, float lt) {
-    const int rr = r0 + cc, ii = (int)fast_div((unsigned)rr, a.fd_group);
-    const int tk = s.start + ii;
-    if ((unsigned)tk >= (unsigned)a.tokens) return;
-    const bool none = s.last(a, ii) < s.first(a, ii);
-    const float inv = 1.f / lt;
-    uintx2 w = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
-    if (none) w = (uintx2){0, 0};
-    *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)tk * a.out_token + (long)(hk * a.group + rr - ii * a.group) * D + d) = w;
-  };
-  for (int it = tid; it < live * (DP / 4); it += kWaves * 64) {
-    const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
-    if (d >= D) continue;
-    floatx4 o = {0, 0, 0, 0};
-    float mm = kNegInf, lt = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      o += *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(vs[w]) + cc * DP + d);
-      mm = fmaxf(mm, sm[w][cc]);
-    }
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) lt += sm[w][cc] == kNegInf ? sl[w][cc] : sl[w][cc] * pow2((sm[w][cc] - mm) * c);
-    if (!shared_out) {
-      put(cc, d, o, lt);
+    __syncthreads();   // (the next piece takes the waves' LDS; or all of this one's sums are on their way)
+    unit = stop;
+    if (whole_tile) {
+      if (!pl.deal) return;
       continue;
     }
-    *reinterpret_cast<floatx4*>(mine + cc * DP + d) = o;
-    if (d == 0) {
-      mine[kRows * DP + cc] = mm;
-      mine[kRows * DP + kRows + cc] = lt;
-    }
-  }
-  if (!shared_out) return;
 
-  // The workgroup that counts itself last joins the chunks.  The XCDs' L2s are not coherent with each other: the partial results are
-  // released to device scope before the count and acquired after it, by one wave for the workgroup.
-  __syncthreads();
-  if (tid == 0) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-    unsigned* cnt = static_cast<unsigned*>(a.workspace) + tile_no * 16;
-    const unsigned old = atomicAdd(cnt, 1u);
-    s_last = old == (unsigned)(active - 1);
-    if (s_last) {
-      atomicExch(cnt, 0u);
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    // The workgroup that counts itself last joins the tile.  The XCDs' L2s are not coherent with each other: the partial results are
+    // released to device scope before the count and acquired after it, by one wave for the workgroup.
+    const int w_first = uniform(tile_unit / run), w_last = uniform((tile_unit + sh.units - 1) / run);
+    const int pieces = w_last - w_first + 1;
+    if (tid == 0) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+      unsigned* cnt = static_cast<unsigned*>(a.workspace) + (b * pl.row_tiles * a.kv_heads + in_seq) * 16;
+      const unsigned old = atomicAdd(cnt, 1u);
+      s_last = old == (unsigned)(pieces - 1);
+      if (s_last) {
+        atomicExch(cnt, 0u);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+      }
     }
-  }
-  __syncthreads();
-  if (!s_last) return;
-  for (int it = tid; it < live * (DP / 4); it += kWaves * 64) {
-    const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
-    if (d >= D) continue;
-    float mm = kNegInf;
-    for (int u = 0; u < active; ++u) mm = fmaxf(mm, ws[(size_t)u * part_floats<DP>() + kRows * DP + cc]);
-    floatx4 o = {0, 0, 0, 0};
-    float lt = 0.f;
-    for (int u = 0; u < active; ++u) {
-      const float* p = ws + (size_t)u * part_floats<DP>();
-      const float mu = p[kRows * DP + cc], w = mu == kNegInf ? 0.f : pow2((mu - mm) * c);
-      o += *reinterpret_cast<const floatx4*>(p + cc * DP + d) * w;
-      lt += mu == kNegInf ? p[kRows * DP + kRows + cc] : p[kRows * DP + kRows + cc] * w;
+    __syncthreads();
+    if (!s_last) continue;
+    // the first of them may have come to this tile behind another one, the others start with it
+    auto slot = [&](int u) { return slots + (size_t)(2 * (w_first + u) + (u == 0 && w_first * run < tile_unit ? 1 : 0)) * part_floats<DP>(); };
+    // One wave finds the rows' maxima and the weight of every piece, each lane for a row and a fourth of the pieces.
+    float* const weight = reinterpret_cast<float*>(vs[0]);   // [piece][16], behind them the sums of the rows
+    if (wave == 0) {
+      float mm = kNegInf, lt = 0.f;
+#pragma unroll 4
+      for (int u = g_c; u < pieces; u += 4) {
+        const float mu = slot(u)[kRows * DP + col_c];
+        weight[u * kRows + col_c] = mu;
+        mm = fmaxf(mm, mu);
+      }
+      mm = max_quarters(mm);
+#pragma unroll 4
+      for (int u = g_c; u < pieces; u += 4) {
+        const float mu = weight[u * kRows + col_c], w = mu == kNegInf ? 0.f : pow2((mu - mm) * c);
+        const float lu = slot(u)[kRows * DP + kRows + col_c];
+        weight[u * kRows + col_c] = w;
+        lt += mu == kNegInf ? lu : lu * w;
+      }
+      lt = sum_quarters(lt);
+      if (g_c == 0) weight[pieces * kRows + col_c] = lt;
     }
-    put(cc, d, o, lt);
+    __syncthreads();
+    for (int it = tid_c; it < live * (DP / 4); it += W * 64) {
+      const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
+      if (!FULL && d >= D) continue;
+      floatx4 o = {0, 0, 0, 0};
+      // (every load is a round trip to memory: other XCDs wrote them)
+      constexpr int JB = 8;
+      for (int u = 0; u < pieces; u += JB) {
+        floatx4 t[JB];
+#pragma unroll
+        for (int e = 0; e < JB; ++e) t[e] = *reinterpret_cast<const floatx4*>(slot(min(u + e, pieces - 1)) + cc * DP + d);
+#pragma unroll
+        for (int e = 0; e < JB; ++e) o += u + e < pieces ? t[e] * weight[(u + e) * kRows + cc] : (floatx4){0, 0, 0, 0};
+      }
+      put(cc, d, o, weight[pieces * kRows + cc]);
+    }
+    __syncthreads();
   }
 }
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
-// How many workgroups the chip is given before a sequence's keys stay with one: four to a CU.
-constexpr long kFill = 1024;
+#ifndef NWAVES
+#define NWAVES 8
+#endif
+// waves of a workgroup: eight where their registers leave a CU room for them
+int waves_of(int dp) { return dp <= 128 ? NWAVES : 4; }
+#ifndef WGS
+#define WGS 256
+#endif
+// workgroups that the units are dealt out to: one to a CU, of the short heads two
+int workers_of(int dp) { return dp <= 64 ? 2 * WGS : WGS; }
 
-RowsPlan rows_plan(const AttnArgs& a, bool share) {
-  RowsPlan p;
-  p.row_tiles = (int)(((long)a.max_q_len * a.group + kRows - 1) / kRows);
-  const long tiles = (long)a.batch * a.kv_heads * p.row_tiles;
-  const int round = kWaves * kBlock;
-  // the most keys between the first and the last that a tile's rows see
-  const int keys = a.window > 0 && a.causal ? (int)min((long)a.max_kv_len, (long)a.window + kRows) : a.max_kv_len;
-  long want = share && tiles <= kCounters ? (kFill + tiles - 1) / tiles : 1;
-  const long most = max(1, (keys + round - 1) / round);
-  want = min(want, most);
-  const long rounds = (most + want - 1) / want;
-  p.chunk = want > 1 ? (int)(rounds * round) : a.max_kv_len;
-  p.chunks = want > 1 ? (int)((keys + p.chunk - 1) / p.chunk) : 1;
+struct RowsGrid {
+  RowsPlan plan;
+  dim3 grid;
+};
+
+RowsGrid rows_plan(const AttnArgs& a, bool share) {
+  RowsGrid p;
+  const int dp = padded_dim(a.head_dim);
+  p.plan.row_tiles = (int)(((long)a.max_q_len * a.group + kRows - 1) / kRows);
+  const long tiles = (long)a.batch * a.kv_heads * p.plan.row_tiles;
+  const int round = waves_of(dp) * kBlock;
+  // the most units of a tile, from the keys between the first and the last that a sequence's rows see
+  const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
+  const long units = max(1L, (keys + round - 1) / round);
+  p.plan.deal = share && tiles <= kCounters && units > 1 && tiles * units < 1L << 30;
+  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)workers_of(dp)));
+  else p.grid = dim3((unsigned)p.plan.row_tiles, (unsigned)a.kv_heads, (unsigned)a.batch);
   return p;
+}
+
+template <typename T, int DP, int W>
+hipError_t launch_dim(const AttnArgs& a, const RowsGrid& p, hipStream_t st) {
+  if (a.head_dim == DP) hipLaunchKernelGGL((attn_rows_kernel<T, DP, true, W>), p.grid, dim3(W * 64), 0, st, a, p.plan);
+  else hipLaunchKernelGGL((attn_rows_kernel<T, DP, false, W>), p.grid, dim3(W * 64), 0, st, a, p.plan);
+  return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_rows(const AttnArgs& a, hipStream_t st) {
-  const RowsPlan p = rows_plan(a, a.workspace != nullptr);
-  const dim3 grid((unsigned)(p.row_tiles * p.chunks), (unsigned)a.kv_heads, (unsigned)a.batch), block(kWaves * 64);
+  const RowsGrid p = rows_plan(a, a.workspace != nullptr);
   switch (padded_dim(a.head_dim)) {
-    case 64: hipLaunchKernelGGL((attn_rows_kernel<T, 64>), grid, block, 0, st, a, p); break;
-    case 96: hipLaunchKernelGGL((attn_rows_kernel<T, 96>), grid, block, 0, st, a, p); break;
-    case 128: hipLaunchKernelGGL((attn_rows_kernel<T, 128>), grid, block, 0, st, a, p); break;
-    default: hipLaunchKernelGGL((attn_rows_kernel<T, 256>), grid, block, 0, st, a, p);
+    case 64: return launch_dim<T, 64, NWAVES>(a, p, st);
+    case 96: return launch_dim<T, 96, NWAVES>(a, p, st);
+    case 128: return launch_dim<T, 128, NWAVES>(a, p, st);
+    default: return launch_dim<T, 256, 4>(a, p, st);
   }
-  return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attn_workspace_bytes(const AttnArgs& a) {
   if (a.max_q_len == 0) return 0;
-  const RowsPlan p = rows_plan(a, true);
-  if (p.chunks <= 1) return 0;
-  const size_t part = (size_t)(kRows * padded_dim(a.head_dim) + 2 * kRows) * 4;
-  return kCounterBytes + (size_t)a.batch * a.kv_heads * p.row_tiles * p.chunks * part;
+  const RowsGrid p = rows_plan(a, true);
+  if (!p.plan.deal) return 0;
+  return kCounterBytes + (size_t)p.grid.x * 2 * (size_t)(kRows * padded_dim(a.head_dim) + 2 * kRows) * 4;
 }
 
 bool attn_fits(const AttnArgs& a) {
-  return a.kv_heads < 65536 && a.batch < 65536 && a.max_kv_len <= 1 << 30 && (double)a.max_q_len * a.group < 2147483000.0;
+  return a.kv_heads < 65536 && a.batch < 65536 && a.max_kv_len <= 1 << 30 && (double)a.max_q_len * a.group * a.kv_heads < 1073741824.0;
 }
 
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t st) {
