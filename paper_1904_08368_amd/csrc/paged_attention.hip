@@ -20,6 +20,11 @@ constexpr int kRows = 16, kBlock = 32;
 // Arrival counters lie 64 bytes apart in front of the workspace, in a region of their own that is the same for every call.
 constexpr int kCounters = 1024;
 constexpr size_t kCounterBytes = (size_t)kCounters * 64;
+// workgroups that units are dealt out to, and so the most pieces of a tile
+#ifndef MP
+#define MP 256
+#endif
+constexpr int kMostPieces = MP;
 
 struct RowsPlan {
   int row_tiles;   // tiles of 16 rows of a sequence, at most
@@ -49,35 +54,41 @@ __device__ __forceinline__ int seq_units(const AttnArgs& a, int b, int round) {
   const Share sh(a, Seq(a, b), round);
   return sh.tiles * sh.units;
 }
-// Units of all sequences, 64 at a time.
-__device__ __forceinline__ int all_units(const AttnArgs& a, int round, int lane) {
-  int total = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int n = seq_units(a, b0 + lane, round);
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-    total += uniform(n);
+// How many units the lanes up to this one have.
+__device__ __forceinline__ int units_upto(int n, int lane) {
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(n, o, 64);
+    n += lane >= o ? t : 0;
   }
-  return total;
+  return n;
 }
-// The sequence that a unit of the line lies in, and the units ahead of that sequence.
-struct Place { int b, before; };
-__device__ __forceinline__ Place find_unit(const AttnArgs& a, int unit, int round, int lane) {
-  int before = 0;
-  for (int b0 = 0;; b0 += 64) {
-    const int n = seq_units(a, b0 + lane, round);
-    int upto = n;   // units of this lane's sequence and those ahead of it among the 64
-    for (int o = 1; o < 64; o <<= 1) {
-      const int t = __shfl_up(upto, o, 64);
-      upto += lane >= o ? t : 0;
-    }
-    const unsigned long long past = __ballot(unit < before + upto);
-    if (past || b0 + 64 >= a.batch) {
-      const int at = past ? (int)__builtin_ctzll(past) : 63;
-      return {b0 + at, before + __builtin_amdgcn_readlane(upto - n, at)};
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
+// The line of units: the first 64 sequences' in the lanes, the others' read again where they are wanted.
+struct Line {
+  int n, upto, total;   // units of sequence `lane`, of it and those ahead of it, of all
+  __device__ Line(const AttnArgs& a, int round, int lane, bool wanted) : n(0), upto(0), total(0) {
+    if (!wanted) return;
+    n = seq_units(a, lane, round);
+    upto = units_upto(n, lane);
+    total = __builtin_amdgcn_readlane(upto, 63);
+    for (int b0 = 64; b0 < a.batch; b0 += 64) total += __builtin_amdgcn_readlane(units_upto(seq_units(a, b0 + lane, round), lane), 63);
   }
-}
+  // the sequence that a unit lies in, and the units ahead of that sequence
+  __device__ void find(const AttnArgs& a, int unit, int round, int lane, int& b, int& before) const {
+    int nn = n, up = upto, ahead = 0;
+    for (int b0 = 0;; b0 += 64) {
+      const unsigned long long past = __ballot(unit < ahead + up);
+      if (past || b0 + 64 >= a.batch) {
+        const int at = past ? (int)__builtin_ctzll(past) : 63;
+        b = b0 + at;
+        before = ahead + __builtin_amdgcn_readlane(up - nn, at);
+        return;
+      }
+      ahead += __builtin_amdgcn_readlane(up, 63);
+      nn = seq_units(a, b0 + 64 + lane, round);
+      up = units_upto(nn, lane);
+    }
+  }
+};
 
 // FULL: head_dim is DP.  W: waves of a workgroup.
 template <typename T, int DP, bool FULL, int W>
@@ -99,29 +110,25 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
   // This workgroup's run of units.
   const int w_no = (int)blockIdx.x;
   int unit = 0, end = 1, run = 1;
+  const Line line(a, ROUND, lane, pl.deal != 0);
   if (pl.deal) {
-    const int total = all_units(a, ROUND, lane);
-    run = max(1, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    run = uniform(max(1, (line.total + (int)gridDim.x - 1) / (int)gridDim.x));
     unit = w_no * run;
-    end = min(total, unit + run);
+    end = min(line.total, unit + run);
   }
-  Place place = {0, 0};
+  int b = 0, before = 0;
   int seq_end = 0;   // the first unit behind the sequence at hand
 
   for (int piece = 0; unit < end; ++piece) {
-    if (!pl.deal) {
-      place.b = (int)blockIdx.z;
-    } else if (unit >= seq_end) {
-      place = find_unit(a, unit, ROUND, lane);
-    }
-    const int b = place.b;
+    if (!pl.deal) b = (int)blockIdx.z;
+    else if (unit >= seq_end) line.find(a, unit, ROUND, lane, b, before);
     const Seq s(a, b);
     const Share sh(a, s, ROUND);
     int in_seq, tile_unit = 0;   // tile of the sequence; its first unit
     if (pl.deal) {
-      seq_end = place.before + sh.tiles * sh.units;
-      in_seq = uniform((unit - place.before) / sh.units);
-      tile_unit = place.before + in_seq * sh.units;
+      seq_end = before + sh.tiles * sh.units;
+      in_seq = uniform((unit - before) / sh.units);
+      tile_unit = before + in_seq * sh.units;
     } else {
       in_seq = (int)blockIdx.x * a.kv_heads + (int)blockIdx.y;
       if (in_seq >= sh.tiles) return;
@@ -391,42 +398,56 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     if (!s_last) continue;
     // the first of them may have come to this tile behind another one, the others start with it
     auto slot = [&](int u) { return slots + (size_t)(2 * (w_first + u) + (u == 0 && w_first * run < tile_unit ? 1 : 0)) * part_floats<DP>(); };
-    // One wave finds the rows' maxima and the weight of every piece, each lane for a row and a fourth of the pieces.
-    float* const weight = reinterpret_cast<float*>(vs[0]);   // [piece][16], behind them the sums of the rows
-    if (wave == 0) {
-      float mm = kNegInf, lt = 0.f;
+    // maxima [piece][16] and sums [piece][16]; each wave makes weights of some rows' maxima, then all threads add up the pieces
+    constexpr int THREADS = W * 64;
+    float* const weight = reinterpret_cast<float*>(vs[0]);
+    float* const lsum = weight + kMostPieces * kRows;
+    static_assert(sizeof(vs) >= (2 * kMostPieces + 1) * kRows * 4 && sizeof(vs) >= (kMostPieces + THREADS / 4 + 1) * kRows * 4, "LDS of the join");
+    float* const row_sum = lsum + kMostPieces * kRows;
 #pragma unroll 4
-      for (int u = g_c; u < pieces; u += 4) {
-        const float mu = slot(u)[kRows * DP + col_c];
-        weight[u * kRows + col_c] = mu;
-        mm = fmaxf(mm, mu);
-      }
-      mm = max_quarters(mm);
-#pragma unroll 4
-      for (int u = g_c; u < pieces; u += 4) {
-        const float mu = weight[u * kRows + col_c], w = mu == kNegInf ? 0.f : pow2((mu - mm) * c);
-        const float lu = slot(u)[kRows * DP + kRows + col_c];
-        weight[u * kRows + col_c] = w;
-        lt += mu == kNegInf ? lu : lu * w;
-      }
-      lt = sum_quarters(lt);
-      if (g_c == 0) weight[pieces * kRows + col_c] = lt;
+    for (int i = tid_c; i < pieces * kRows; i += THREADS) {
+      const float* p = slot(i / kRows) + kRows * DP + i % kRows;
+      weight[i] = p[0];
+      lsum[i] = p[kRows];
     }
     __syncthreads();
-    for (int it = tid_c; it < live * (DP / 4); it += W * 64) {
-      const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
-      if (!FULL && d >= D) continue;
-      floatx4 o = {0, 0, 0, 0};
-      // (every load is a round trip to memory: other XCDs wrote them)
-      constexpr int JB = 8;
-      for (int u = 0; u < pieces; u += JB) {
-        floatx4 t[JB];
-#pragma unroll
-        for (int e = 0; e < JB; ++e) t[e] = *reinterpret_cast<const floatx4*>(slot(min(u + e, pieces - 1)) + cc * DP + d);
-#pragma unroll
-        for (int e = 0; e < JB; ++e) o += u + e < pieces ? t[e] * weight[(u + e) * kRows + cc] : (floatx4){0, 0, 0, 0};
+    for (int cc = wave; cc < live; cc += W) {
+      float mm = kNegInf, lt = 0.f;
+      for (int u = lane; u < pieces; u += 64) mm = fmaxf(mm, weight[u * kRows + cc]);
+      for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o, 64));
+      for (int u = lane; u < pieces; u += 64) {
+        const float mu = weight[u * kRows + cc], w = mu == kNegInf ? 0.f : pow2((mu - mm) * c);
+        lt += mu == kNegInf ? lsum[u * kRows + cc] : lsum[u * kRows + cc] * w;
+        weight[u * kRows + cc] = w;
       }
-      put(cc, d, o, weight[pieces * kRows + cc]);
+      for (int o = 32; o > 0; o >>= 1) lt += __shfl_xor(lt, o, 64);
+      if (lane == 0) row_sum[cc] = lt;
+    }
+    __syncthreads();
+    // where the rows' float4s are fewer than the threads, several threads share one: thread group `sub` of `subs` takes every subs-th piece
+    constexpr int JB = 8;   // loads in flight: each is a round trip to memory, other XCDs wrote the pieces
+    const int items = live * (DP / 4), subs = max(1, THREADS / items);
+    floatx4* const shared_sums = reinterpret_cast<floatx4*>(lsum);
+    for (int it0 = 0; it0 < items; it0 += THREADS) {
+      const int sub = subs > 1 ? tid_c / items : 0, it = it0 + tid_c - sub * items;
+      const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
+      const bool mine_too = it < items && sub < subs && (FULL || d < D);
+      floatx4 o = {0, 0, 0, 0};
+      if (mine_too)
+        for (int u = sub; u < pieces; u += JB * subs) {
+          floatx4 t[JB];
+#pragma unroll
+          for (int e = 0; e < JB; ++e) t[e] = *reinterpret_cast<const floatx4*>(slot(min(u + e * subs, pieces - 1)) + cc * DP + d);
+#pragma unroll
+          for (int e = 0; e < JB; ++e) o += u + e * subs < pieces ? t[e] * weight[(u + e * subs) * kRows + cc] : (floatx4){0, 0, 0, 0};
+        }
+      if (subs > 1) {
+        shared_sums[tid_c] = o;
+        __syncthreads();
+        if (sub == 0)
+          for (int e = 1; e < subs; ++e) o += shared_sums[e * items + it];
+      }
+      if (mine_too && sub == 0) put(cc, d, o, row_sum[cc]);
     }
     __syncthreads();
   }
@@ -434,17 +455,14 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
+#ifndef DEALMIN
+#define DEALMIN 1
+#endif
 #ifndef NWAVES
 #define NWAVES 8
 #endif
 // waves of a workgroup: eight where their registers leave a CU room for them
 int waves_of(int dp) { return dp <= 128 ? NWAVES : 4; }
-#ifndef WGS
-#define WGS 256
-#endif
-// workgroups that the units are dealt out to: one to a CU, of the short heads two
-int workers_of(int dp) { return dp <= 64 ? 2 * WGS : WGS; }
-
 struct RowsGrid {
   RowsPlan plan;
   dim3 grid;
@@ -459,8 +477,8 @@ RowsGrid rows_plan(const AttnArgs& a, bool share) {
   // the most units of a tile, from the keys between the first and the last that a sequence's rows see
   const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
   const long units = max(1L, (keys + round - 1) / round);
-  p.plan.deal = share && tiles <= kCounters && units > 1 && tiles * units < 1L << 30;
-  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)workers_of(dp)));
+  p.plan.deal = share && tiles <= kCounters && units > DEALMIN && tiles * units < 1L << 30;
+  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)kMostPieces));
   else p.grid = dim3((unsigned)p.plan.row_tiles, (unsigned)a.kv_heads, (unsigned)a.batch);
   return p;
 }
