@@ -68,6 +68,8 @@ struct AttnArgs {
 size_t attn_workspace_bytes(const AttnArgs& a);
 bool attn_fits(const AttnArgs& a);
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t st);
+// the kernel for many rows (paged_attention_tiles.hip)
+hipError_t launch_attention_tiles(const AttnArgs& a, int dtype, hipStream_t st);
 
 // Packed 4-bit weights.  Units in tiles of 16, the reduction in chunks of 128; a tile's chunk is 64 x 16 bytes, the A operands of four
 // 16x16x32 matrix instructions: lane l holds unit l % 16, and its word s the eight codes of i = 32 s + 8 (l / 16) + 0..7, code 2j in

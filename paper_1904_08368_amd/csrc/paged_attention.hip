@@ -514,7 +514,11 @@ bool attn_fits(const AttnArgs& a) {
   return a.kv_heads < 65536 && a.batch < 65536 && a.max_kv_len <= 1 << 30 && (double)a.max_q_len * a.group * a.kv_heads < 1073741824.0;
 }
 
+#ifndef TILEROWS
+#define TILEROWS 32
+#endif
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t st) {
+  if ((long)a.max_q_len * a.group > TILEROWS) return launch_attention_tiles(a, dtype, st);
   return dtype == T_F16 ? launch_rows<_Float16>(a, st) : launch_rows<__bf16>(a, st);
 }
 
