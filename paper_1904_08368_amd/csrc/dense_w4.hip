@@ -55,52 +55,142 @@ __device__ __forceinline__ void finish(const W4Args& a, int m, int j, float v) {
   static_cast<T*>(a.y)[(long)m * a.y_stride + j] = (T)v;
 }
 
-template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void w4_rows_kernel(const W4Args a, const W4Layout l) {
+// Few rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; DEPTH chunks of
+// codes are on their way.  A lane's x belongs to row 16 rt + lane % 16: lanes of rows that are not there load nothing, so that one row costs
+// the memory pipe a 16th of what 16 cost it.
+template <typename T, int NT, int RT, int W, int DEPTH>
+__global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W4Layout l) {
   typedef W4Type<T> C;
   typedef typename C::vec vec;
-  __shared__ floatx4 part[WAVES][64];
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-  const int tile = (int)blockIdx.x, m0 = (int)blockIdx.y * 16;
+  __shared__ floatx4 part[W][NT * RT][64];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int tile0 = (int)blockIdx.x * NT, m0 = (int)blockIdx.y * 16 * RT;
   const int g = lane >> 4, col = lane & 15;
-  const int row = min(m0 + col, a.m - 1);   // (columns beyond m repeat the last row and are not stored)
-  const T* x = static_cast<const T*>(a.x) + (long)row * a.x_stride + 8 * g;
   const unsigned char* base = static_cast<const unsigned char*>(a.packed);
-  const uintx4* w = reinterpret_cast<const uintx4*>(base) + (size_t)tile * l.chunks * 64 + lane;
-  // this lane's sums belong to units 4 g .. 4 g + 3 of the tile and to row `col`
-  const T* scales = reinterpret_cast<const T*>(base + l.scales_at) + (size_t)tile * l.groups * 16 + 4 * g;
-  const unsigned char* zeros = base + l.zeros_at + (size_t)tile * l.groups * 16 + 4 * g;
-  const int steps = (a.k + 31) / 32, per_group = a.group / 32;
-  // a wave takes whole groups
-  const int first = l.groups * wave / WAVES, last = l.groups * (wave + 1) / WAVES;
-  const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
-  floatx4 sum = {0, 0, 0, 0};
-  for (int gr = first; gr < last; ++gr) {
-    floatx4 acc = {0, 0, 0, 0}, xs = {0, 0, 0, 0};
-    const int s1 = min((gr + 1) * per_group, steps);
-    for (int s = gr * per_group; s < s1; ++s) {
-      const unsigned code = w[(size_t)(s >> 2) * 64][s & 3];
-      vec xv = __builtin_bit_cast(vec, (uintx4){0, 0, 0, 0});
-      if (s * 32 + 8 * g < a.k) xv = *reinterpret_cast<const vec*>(x + s * 32);
-      acc = C::mfma(widen<T>(code), xv, acc);
-      xs = C::mfma(ones, xv, xs);
-    }
+  const int first = l.chunks * wave / W, last = l.chunks * (wave + 1) / W;
+  const uintx4* w[NT];
+  const T* scales[NT];
+  const unsigned char* zeros[NT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float z = 16.f + (a.zeros ? (float)zeros[gr * 16 + i] : 8.f);
-      sum[i] = fmaf((float)scales[gr * 16 + i], fmaf(-z, xs[i], acc[i]), sum[i]);
+  for (int t = 0; t < NT; ++t) {
+    const int tile = min(tile0 + t, l.tiles - 1);   // (a tile past the last is computed again and not stored)
+    w[t] = reinterpret_cast<const uintx4*>(base) + (size_t)tile * l.chunks * 64 + lane;
+    // this lane's sums belong to units 4 g .. 4 g + 3 of the tile
+    scales[t] = reinterpret_cast<const T*>(base + l.scales_at) + (size_t)tile * l.groups * 16 + 4 * g;
+    zeros[t] = base + l.zeros_at + (size_t)tile * l.groups * 16 + 4 * g;
+  }
+  const T* x[RT];
+  bool row_ok[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = m0 + r * 16 + col;
+    row_ok[r] = row < a.m;
+    x[r] = static_cast<const T*>(a.x) + (long)min(row, a.m - 1) * a.x_stride + 8 * g;
+  }
+  uintx4 codes[DEPTH][NT];
+  auto load_codes = [&](int chunk, int at) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) codes[at][t] = w[t][(size_t)chunk * 64];
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (first + d < last) load_codes(first + d, d);
+  uintx4 xv[4][RT];
+  auto load_x = [&](int chunk) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const int k = chunk * 128 + s * 32;
+        xv[s][r] = (uintx4){0, 0, 0, 0};
+        if (row_ok[r] && k + 8 * g < a.k) xv[s][r] = *reinterpret_cast<const uintx4*>(x[r] + k);
+      }
+  };
+  // scales and 16 + zero points of the group at hand
+  const int per_group = a.group / 32;
+  int gr = first * 4 / per_group, left = per_group - (first * 4 - gr * per_group);   // (steps left in it)
+  typedef T four __attribute__((ext_vector_type(4)));
+  four sc[NT];
+  unsigned zp[NT];
+  auto load_group = [&]() {
+    const int at = min(gr, l.groups - 1) * 16;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      sc[t] = *reinterpret_cast<const four*>(scales[t] + at);
+      zp[t] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros[t] + at) : 0x08080808u;
+    }
+  };
+  load_group();
+  const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
+  floatx4 sum[NT][RT], acc[NT][RT], xs[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    xs[r] = (floatx4){0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sum[t][r] = acc[t][r] = (floatx4){0, 0, 0, 0};
+  }
+  auto flush = [&]() {
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float z = -16.f - (float)((zp[t] >> (8 * i)) & 255u), f = (float)sc[t][i];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(f, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
+      }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      xs[r] = (floatx4){0, 0, 0, 0};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t][r] = (floatx4){0, 0, 0, 0};
+    }
+  };
+  for (int c0 = first; c0 < last; c0 += DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int chunk = c0 + d;
+      if (chunk < last) {
+        load_x(chunk);
+        uintx4 cur[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) cur[t] = codes[d][t];
+        if (chunk + DEPTH < last) load_codes(chunk + DEPTH, d);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+#pragma unroll
+          for (int r = 0; r < RT; ++r) xs[r] = C::mfma(ones, __builtin_bit_cast(vec, xv[s][r]), xs[r]);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const vec wv = widen<T>(cur[t][s]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, __builtin_bit_cast(vec, xv[s][r]), acc[t][r]);
+          }
+          if (--left == 0) {
+            flush();
+            ++gr;
+            left = per_group;
+            load_group();
+          }
+        }
+      }
     }
   }
-  part[wave][lane] = sum;
+  flush();   // (a group that goes on in the next wave's part, or that the row ends in)
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) part[wave][t * RT + r][lane] = sum[t][r];
   __syncthreads();
-  if (wave) return;
+  for (int i = (int)threadIdx.x; i < NT * RT * 64; i += W * 64) {
+    const int which = i >> 6, ln = i & 63;
+    floatx4 v = {0, 0, 0, 0};
 #pragma unroll
-  for (int u = 1; u < WAVES; ++u) sum += part[u][lane];
-  if (m0 + col >= a.m) return;
+    for (int u = 0; u < W; ++u) v += part[u][which][ln];
+    const int row = m0 + (which % RT) * 16 + (ln & 15), j0 = (tile0 + which / RT) * 16 + 4 * (ln >> 4);
+    if (row >= a.m) continue;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = tile * 16 + 4 * g + i;
-    if (j < a.n) finish<T>(a, m0 + col, j, sum[i]);
+    for (int e = 0; e < 4; ++e)
+      if (j0 + e < a.n) finish<T>(a, row, j0 + e, v[e]);
   }
 }
 
@@ -145,12 +235,24 @@ hipError_t launch_w4_pack(const W4Args& a, const uint8_t* codes, const void* sca
 
 bool w4_fits(const W4Args& a) { return a.m <= 16 * 65535; }
 
+namespace {
+#ifndef D1
+#define D1 4
+#endif
+template <typename T>
+hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
+  auto go = [&](auto kernel, int nt, int rt) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((l.tiles + nt - 1) / nt), (unsigned)((a.m + 16 * rt - 1) / (16 * rt))), dim3(512), 0, st, a, l);
+    return hipGetLastError();
+  };
+  if (a.m <= 16) return go(w4_rows_kernel<T, 1, 1, 8, D1>, 1, 1);
+  return go(w4_rows_kernel<T, 2, 2, 8, 2>, 2, 2);
+}
+}  // namespace
+
 hipError_t launch_w4(const W4Args& a, int dtype, hipStream_t st) {
   const W4Layout l = w4_layout(a.n, a.k, a.group, a.zeros != 0);
-  const dim3 grid((unsigned)l.tiles, (unsigned)((a.m + 15) / 16));
-  if (dtype == T_F16) hipLaunchKernelGGL((w4_rows_kernel<_Float16, 8>), grid, dim3(512), 0, st, a, l);
-  else hipLaunchKernelGGL((w4_rows_kernel<__bf16, 8>), grid, dim3(512), 0, st, a, l);
-  return hipGetLastError();
+  return dtype == T_F16 ? launch_type<_Float16>(a, l, st) : launch_type<__bf16>(a, l, st);
 }
 
 }  // namespace relay
