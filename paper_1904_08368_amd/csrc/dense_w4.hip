@@ -55,8 +55,85 @@ __device__ __forceinline__ void finish(const W4Args& a, int m, int j, float v) {
   static_cast<T*>(a.y)[(long)m * a.y_stride + j] = (T)v;
 }
 
+// Up to four rows: bound by the codes' bytes, so what else goes through the memory pipe is kept small.  The 16 columns of a matrix
+// instruction are four rows by the four 32-long steps of a chunk: column 4 r + s holds row r's part of step s, one 16-byte load a
+// lane for a whole chunk.  The instruction of step s gives its column its product and the others products that nobody looks at; each
+// lane takes its own step's result, scaled by that step's group, and the four columns of a row meet at the end.
+// W waves share the reduction out in chunks of 128; DEPTH chunks are on their way.  (Loads return in the order of their issue: a chunk's codes, x and
+// scales are asked for together, or waiting for x would be waiting for the codes of chunks ahead.)
+template <typename T, int W, int DEPTH>
+__global__ __launch_bounds__(W * 64) void w4_few_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
+  typedef W4Type<T> C;
+  typedef typename C::vec vec;
+  typedef T four __attribute__((ext_vector_type(4)));
+  __shared__ floatx4 part[W][16];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int tile = (int)blockIdx.x, g = lane >> 4, col = lane & 15, step = col & 3, row = col >> 2;
+  const unsigned char* base = static_cast<const unsigned char*>(a.packed);
+  const int first = l.chunks * wave / W, last = l.chunks * (wave + 1) / W;
+  const uintx4* w = reinterpret_cast<const uintx4*>(base) + (size_t)tile * l.chunks * 64 + lane;
+  const T* scales = reinterpret_cast<const T*>(base + l.scales_at) + (size_t)tile * l.groups * 16 + 4 * g;
+  const unsigned char* zeros = base + l.zeros_at + (size_t)tile * l.groups * 16 + 4 * g;
+  const bool row_ok = row < a.m;
+  const T* x = static_cast<const T*>(a.x) + (row_ok ? (long)row * a.x_stride : 0) + step * 32 + 8 * g;
+  uintx4 codes[DEPTH], xv[DEPTH];
+  four sc[DEPTH];
+  unsigned zp[DEPTH];
+  auto load = [&](int chunk, int d) {
+    codes[d] = w[(size_t)chunk * 64];
+    xv[d] = (uintx4){0, 0, 0, 0};
+    if (row_ok && chunk * 128 + step * 32 + 8 * g < a.k) xv[d] = *reinterpret_cast<const uintx4*>(x + chunk * 128);
+    const int at = min((int)fast_div((unsigned)(chunk * 4 + step), per_group), l.groups - 1) * 16;
+    sc[d] = *reinterpret_cast<const four*>(scales + at);
+    zp[d] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros + at) : 0x08080808u;
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (first + d < last) load(first + d, d);
+  const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
+  floatx4 sum = {0, 0, 0, 0};
+  for (int c0 = first; c0 < last; c0 += DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int chunk = c0 + d;
+      if (chunk < last) {
+        const vec xb = __builtin_bit_cast(vec, xv[d]);
+        const floatx4 none = {0, 0, 0, 0};
+        const floatx4 xs = C::mfma(ones, xb, none);
+        floatx4 p[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) p[s] = C::mfma(widen<T>(codes[d][s]), xb, none);
+        const four f = sc[d];
+        const unsigned z = zp[d];
+        if (chunk + DEPTH < last) load(chunk + DEPTH, d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float lo = step & 1 ? p[1][i] : p[0][i], hi = step & 1 ? p[3][i] : p[2][i];
+          const float v = step & 2 ? hi : lo;
+          sum[i] = fmaf((float)f[i], fmaf(-16.f - (float)((z >> (8 * i)) & 255u), xs[i], v), sum[i]);
+        }
+      }
+    }
+  }
+  // the four columns of a row
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sum[i] += __shfl_xor(sum[i], 1, 64);
+    sum[i] += __shfl_xor(sum[i], 2, 64);
+  }
+  if (step == 0) part[wave][row * 4 + g] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  // lane: unit lane % 16 of the tile, row lane / 16
+  const int r = lane >> 4, j = lane & 15;
+  float v = 0.f;
+#pragma unroll
+  for (int u = 0; u < W; ++u) v += part[u][r * 4 + (j >> 2)][j & 3];
+  if (r < a.m && tile * 16 + j < a.n) finish<T>(a, r, tile * 16 + j, v);
+}
+
 // Few rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; DEPTH chunks of
-// codes are on their way.  A lane's x belongs to row 16 rt + lane % 16: lanes of rows that are not there load nothing, so that one row costs
+// codes and of x are on their way.  A lane's x belongs to row 16 rt + lane % 16: lanes of rows that are not there load nothing, so that one row costs
 // the memory pipe a 16th of what 16 cost it.
 template <typename T, int NT, int RT, int W, int DEPTH>
 __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W4Layout l) {
@@ -87,25 +164,22 @@ __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W
     row_ok[r] = row < a.m;
     x[r] = static_cast<const T*>(a.x) + (long)min(row, a.m - 1) * a.x_stride + 8 * g;
   }
-  uintx4 codes[DEPTH][NT];
-  auto load_codes = [&](int chunk, int at) {
+  uintx4 codes[DEPTH][NT], xv[DEPTH][4][RT];
+  auto load = [&](int chunk, int d) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) codes[at][t] = w[t][(size_t)chunk * 64];
-  };
-#pragma unroll
-  for (int d = 0; d < DEPTH; ++d)
-    if (first + d < last) load_codes(first + d, d);
-  uintx4 xv[4][RT];
-  auto load_x = [&](int chunk) {
+    for (int t = 0; t < NT; ++t) codes[d][t] = w[t][(size_t)chunk * 64];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const int k = chunk * 128 + s * 32;
-        xv[s][r] = (uintx4){0, 0, 0, 0};
-        if (row_ok[r] && k + 8 * g < a.k) xv[s][r] = *reinterpret_cast<const uintx4*>(x[r] + k);
+        xv[d][s][r] = (uintx4){0, 0, 0, 0};
+        if (row_ok[r] && k + 8 * g < a.k) xv[d][s][r] = *reinterpret_cast<const uintx4*>(x[r] + k);
       }
   };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (first + d < last) load(first + d, d);
   // scales and 16 + zero points of the group at hand
   const int per_group = a.group / 32;
   int gr = first * 4 / per_group, left = per_group - (first * 4 - gr * per_group);   // (steps left in it)
@@ -150,20 +224,15 @@ __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W
     for (int d = 0; d < DEPTH; ++d) {
       const int chunk = c0 + d;
       if (chunk < last) {
-        load_x(chunk);
-        uintx4 cur[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) cur[t] = codes[d][t];
-        if (chunk + DEPTH < last) load_codes(chunk + DEPTH, d);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
 #pragma unroll
-          for (int r = 0; r < RT; ++r) xs[r] = C::mfma(ones, __builtin_bit_cast(vec, xv[s][r]), xs[r]);
+          for (int r = 0; r < RT; ++r) xs[r] = C::mfma(ones, __builtin_bit_cast(vec, xv[d][s][r]), xs[r]);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const vec wv = widen<T>(cur[t][s]);
+            const vec wv = widen<T>(codes[d][t][s]);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, __builtin_bit_cast(vec, xv[s][r]), acc[t][r]);
+            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, __builtin_bit_cast(vec, xv[d][s][r]), acc[t][r]);
           }
           if (--left == 0) {
             flush();
@@ -172,6 +241,7 @@ __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W
             load_group();
           }
         }
+        if (chunk + DEPTH < last) load(chunk + DEPTH, d);
       }
     }
   }
@@ -236,6 +306,9 @@ hipError_t launch_w4_pack(const W4Args& a, const uint8_t* codes, const void* sca
 bool w4_fits(const W4Args& a) { return a.m <= 16 * 65535; }
 
 namespace {
+#ifndef D2
+#define D2 3
+#endif
 #ifndef D1
 #define D1 4
 #endif
@@ -245,7 +318,11 @@ hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)((l.tiles + nt - 1) / nt), (unsigned)((a.m + 16 * rt - 1) / (16 * rt))), dim3(512), 0, st, a, l);
     return hipGetLastError();
   };
-  if (a.m <= 16) return go(w4_rows_kernel<T, 1, 1, 8, D1>, 1, 1);
+  if (a.m <= 4) {
+    hipLaunchKernelGGL((w4_few_kernel<T, 8, D1>), dim3((unsigned)l.tiles), dim3(512), 0, st, a, l, make_fastdiv((uint32_t)a.group / 32));
+    return hipGetLastError();
+  }
+  if (a.m <= 16) return go(w4_rows_kernel<T, 1, 1, 8, D2>, 1, 1);
   return go(w4_rows_kernel<T, 2, 2, 8, 2>, 2, 2);
 }
 }  // namespace
