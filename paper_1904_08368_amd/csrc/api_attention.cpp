@@ -260,7 +260,7 @@ relay_status relay_prepack_qdense_w4(const relay_qdense_w4_desc* d, const uint8_
   if (packed == codes || packed == scales || packed == zeros) return fail(RELAY_ERR_UNSUPPORTED, "output must not alias an input");
   const size_t need = relay::w4_layout(a.n, a.k, a.group, a.zeros != 0).bytes;
   if (packed_bytes < need) return fail(RELAY_ERR_WORKSPACE, "packed weights of %zu bytes, %zu needed", packed_bytes, need);
-  return device_status(relay::launch_w4_pack(a, codes, scales, zeros, packed, static_cast<hipStream_t>(hip_stream)), "4-bit packing launch");
+  return device_status(relay::launch_w4_pack(a, d->dtype, codes, scales, zeros, packed, static_cast<hipStream_t>(hip_stream)), "4-bit packing launch");
 }
 
 relay_status relay_qdense_w4(const relay_qdense_w4_desc* d, const void* x, const void* packed, const float* bias, const void* residual,

@@ -73,8 +73,8 @@ hipError_t launch_attention_tiles(const AttnArgs& a, int dtype, hipStream_t st);
 
 // Packed 4-bit weights.  Units in tiles of 16, the reduction in chunks of 128; a tile's chunk is 64 x 16 bytes, the A operands of four
 // 16x16x32 matrix instructions: lane l holds unit l % 16, and its word s the eight codes of i = 32 s + 8 (l / 16) + 0..7, code 2j in
-// bits 4j.. and code 2j + 1 in bits 16 + 4j...  Behind all codes the scales [tile][group][16] in the activations' type, behind them
-// the zero points [tile][group][16] as bytes.  What lies past n or k is zero.
+// bits 4j.. and code 2j + 1 in bits 16 + 4j.. of the word before it is turned left (dense_w4.hip).  Behind all codes the scales [tile][group][16] in the
+// activations' type, behind them 16 + the zero points [tile][group][16] as bytes.  What lies past n or k is zero.
 struct W4Layout {
   int tiles, chunks, groups;
   size_t scales_at, zeros_at, bytes;
@@ -98,7 +98,7 @@ struct W4Args {
   int m, n, k, group, zeros, relu;
   int64_t x_stride, y_stride;
 };
-hipError_t launch_w4_pack(const W4Args& a, const uint8_t* codes, const void* scales, const uint8_t* zeros, void* packed, hipStream_t st);
+hipError_t launch_w4_pack(const W4Args& a, int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros, void* packed, hipStream_t st);
 bool w4_fits(const W4Args& a);
 hipError_t launch_w4(const W4Args& a, int dtype, hipStream_t st);
 

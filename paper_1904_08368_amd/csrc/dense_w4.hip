@@ -9,6 +9,9 @@
 // streams its part straight into the A operands (the packed order), and they add up through LDS.
 #include "attention.hpp"
 
+#ifndef FW
+#define FW 8
+#endif
 namespace relay {
 namespace {
 
@@ -33,18 +36,19 @@ template <> struct W4Type<__bf16> {
   static __device__ __forceinline__ floatx4 mfma(vec a, vec b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 
-// eight codes of a word -> the eight numbers 16 + code
+// Eight codes of a word -> the eight numbers 16 + code.  The packed word is turned left by kAt bits, so that pair j comes to its place by a turn
+// right of 4 j.  Mask and base are kept in registers: of the literals they are, the compiler makes two instructions of each and-or, and
+// this is half of all that a byte of codes costs.
 template <typename T>
-__device__ __forceinline__ typename W4Type<T>::vec widen(unsigned w) {
-  typedef W4Type<T> C;
-  uintx4 r;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int sh = C::kAt - 4 * j;
-    r[j] = ((sh >= 0 ? w << (sh > 0 ? sh : 0) : w >> (sh < 0 ? -sh : 0)) & C::kMask) | C::kBase;
+struct Widen {
+  unsigned mask, base;
+  __device__ Widen() : mask(W4Type<T>::kMask), base(W4Type<T>::kBase) { asm("" : "+v"(mask), "+v"(base)); }
+  __device__ __forceinline__ typename W4Type<T>::vec operator()(unsigned w) const {
+    const uintx4 r = {(w & mask) | base, (__builtin_rotateright32(w, 4) & mask) | base, (__builtin_rotateright32(w, 8) & mask) | base,
+                      (__builtin_rotateright32(w, 12) & mask) | base};
+    return __builtin_bit_cast(typename W4Type<T>::vec, r);
   }
-  return __builtin_bit_cast(typename C::vec, r);
-}
+};
 
 // the tail of one output
 template <typename T>
@@ -55,91 +59,101 @@ __device__ __forceinline__ void finish(const W4Args& a, int m, int j, float v) {
   static_cast<T*>(a.y)[(long)m * a.y_stride + j] = (T)v;
 }
 
-// Up to four rows: bound by the codes' bytes, so what else goes through the memory pipe is kept small.  The 16 columns of a matrix
-// instruction are four rows by the four 32-long steps of a chunk: column 4 r + s holds row r's part of step s, one 16-byte load a
-// lane for a whole chunk.  The instruction of step s gives its column its product and the others products that nobody looks at; each
-// lane takes its own step's result, scaled by that step's group, and the four columns of a row meet at the end.
-// W waves share the reduction out in chunks of 128; DEPTH chunks are on their way.  (Loads return in the order of their issue: a chunk's codes, x and
-// scales are asked for together, or waiting for x would be waiting for the codes of chunks ahead.)
-template <typename T, int W, int DEPTH>
+// Up to MR rows (1 or 4): bound by the codes' bytes, and close behind by the memory pipe, which takes a 16-byte load of a wave in 16 clocks whatever its
+// lanes ask for.  So beside the codes' loads there are few others: what a wave needs of x, scales and zero points for SC chunks of its
+// part of the reduction comes in whole 16-byte pieces and goes through LDS that only this wave uses (one row by 32768 x 8192: 31 us with a load of
+// x and of scales to every chunk, 40 with four of x).
+// W waves share the reduction out.  FL: steps of 32 between two applications of the scales, 4 where groups are whole chunks, 2 or 1 where they are not.
+template <typename T, int MR, int W, int FL>
 __global__ __launch_bounds__(W * 64) void w4_few_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
   typedef W4Type<T> C;
   typedef typename C::vec vec;
   typedef T four __attribute__((ext_vector_type(4)));
-  __shared__ floatx4 part[W][16];
+  constexpr int SC = MR == 1 ? 8 : 4, XP = SC * 16 * MR, XL = XP / 64, GP = SC * 8;   // 16-byte pieces of x; loads of them; pieces of scales at most
+  __shared__ __attribute__((aligned(16))) uintx4 lds[W][XP + GP + GP / 2];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int tile = (int)blockIdx.x, g = lane >> 4, col = lane & 15, step = col & 3, row = col >> 2;
+  const int tile = (int)blockIdx.x, g = lane >> 4, col = lane & 15;
   const unsigned char* base = static_cast<const unsigned char*>(a.packed);
   const int first = l.chunks * wave / W, last = l.chunks * (wave + 1) / W;
   const uintx4* w = reinterpret_cast<const uintx4*>(base) + (size_t)tile * l.chunks * 64 + lane;
-  const T* scales = reinterpret_cast<const T*>(base + l.scales_at) + (size_t)tile * l.groups * 16 + 4 * g;
-  const unsigned char* zeros = base + l.zeros_at + (size_t)tile * l.groups * 16 + 4 * g;
-  const bool row_ok = row < a.m;
-  const T* x = static_cast<const T*>(a.x) + (row_ok ? (long)row * a.x_stride : 0) + step * 32 + 8 * g;
-  uintx4 codes[DEPTH], xv[DEPTH];
-  four sc[DEPTH];
-  unsigned zp[DEPTH];
-  auto load = [&](int chunk, int d) {
-    codes[d] = w[(size_t)chunk * 64];
-    xv[d] = (uintx4){0, 0, 0, 0};
-    if (row_ok && chunk * 128 + step * 32 + 8 * g < a.k) xv[d] = *reinterpret_cast<const uintx4*>(x + chunk * 128);
-    const int at = min((int)fast_div((unsigned)(chunk * 4 + step), per_group), l.groups - 1) * 16;
-    sc[d] = *reinterpret_cast<const four*>(scales + at);
-    zp[d] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros + at) : 0x08080808u;
+  const uintx4* scales = reinterpret_cast<const uintx4*>(base + l.scales_at) + (size_t)tile * l.groups * 2;
+  const uintx4* zeros = reinterpret_cast<const uintx4*>(base + l.zeros_at) + (size_t)tile * l.groups;
+  uintx4 codes[SC], xv[XL], sv, zv;
+  auto group_of = [&](int chunk) { return (int)fast_div((unsigned)(chunk * 4), per_group); };
+  auto load_codes = [&](int chunk, int i) { if (chunk < last) codes[i] = w[(size_t)chunk * 64]; };
+  auto load_rest = [&](int chunk) {
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      const int piece = i * 64 + lane, row = piece / (SC * 16), at = chunk * 128 + (piece - row * SC * 16) * 8;
+      xv[i] = (uintx4){0, 0, 0, 0};
+      if (row < a.m && at < a.k) xv[i] = *reinterpret_cast<const uintx4*>(static_cast<const T*>(a.x) + (long)row * a.x_stride + at);
+    }
+    const int g0 = group_of(chunk), have = l.groups - g0;
+    if (lane < GP && lane < 2 * have) sv = scales[g0 * 2 + lane];
+    if (a.zeros && lane < GP / 2 && lane < have) zv = zeros[g0 + lane];
   };
 #pragma unroll
-  for (int d = 0; d < DEPTH; ++d)
-    if (first + d < last) load(first + d, d);
+  for (int i = 0; i < SC; ++i) load_codes(first + i, i);
+  if (first < last) load_rest(first);
+  uintx4* const mx = lds[wave];
+  const four* const msc = reinterpret_cast<const four*>(mx + XP);             // [group][16 units]
+  const unsigned* const mzp = reinterpret_cast<const unsigned*>(mx + XP + GP);
   const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
+  const Widen<T> widen;
+  const int xrow = (MR == 1 ? 0 : min(col, a.m - 1)) * SC * 16 + g;   // (columns of rows that are not there repeat the last one)
   floatx4 sum = {0, 0, 0, 0};
-  for (int c0 = first; c0 < last; c0 += DEPTH) {
+  for (int c0 = first; c0 < last; c0 += SC) {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const int chunk = c0 + d;
-      if (chunk < last) {
-        const vec xb = __builtin_bit_cast(vec, xv[d]);
-        const floatx4 none = {0, 0, 0, 0};
-        const floatx4 xs = C::mfma(ones, xb, none);
-        floatx4 p[4];
+    for (int i = 0; i < XL; ++i) mx[i * 64 + lane] = xv[i];
+    if (lane < GP) mx[XP + lane] = sv;
+    if (lane < GP / 2) mx[XP + GP + lane] = zv;
+    const int g0 = group_of(c0);
+    if (c0 + SC < last) load_rest(c0 + SC);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) p[s] = C::mfma(widen<T>(codes[d][s]), xb, none);
-        const four f = sc[d];
-        const unsigned z = zp[d];
-        if (chunk + DEPTH < last) load(chunk + DEPTH, d);
+    for (int i = 0; i < SC; ++i) {
+      if (c0 + i >= last) break;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float lo = step & 1 ? p[1][i] : p[0][i], hi = step & 1 ? p[3][i] : p[2][i];
-          const float v = step & 2 ? hi : lo;
-          sum[i] = fmaf((float)f[i], fmaf(-16.f - (float)((z >> (8 * i)) & 255u), xs[i], v), sum[i]);
+      for (int f = 0; f < 4 / FL; ++f) {
+        floatx4 acc = {0, 0, 0, 0}, xs = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = f * FL; s < (f + 1) * FL; ++s) {
+          const vec xb = __builtin_bit_cast(vec, mx[xrow + i * 16 + s * 4]);
+          xs = C::mfma(ones, xb, xs);
+          acc = C::mfma(widen(codes[i][s]), xb, acc);
         }
+        const int gr = min((int)fast_div((unsigned)((c0 + i) * 4 + f * FL), per_group), l.groups - 1) - g0;
+        const four sc = msc[gr * 4 + g];
+        const unsigned zp = a.zeros ? mzp[gr * 4 + g] : 0x18181818u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf((float)sc[e], fmaf(-(float)((zp >> (8 * e)) & 255u), xs[e], acc[e]), sum[e]);
       }
+      load_codes(c0 + SC + i, i);
     }
   }
-  // the four columns of a row
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    sum[i] += __shfl_xor(sum[i], 1, 64);
-    sum[i] += __shfl_xor(sum[i], 2, 64);
-  }
-  if (step == 0) part[wave][row * 4 + g] = sum;
+  floatx4* const part = reinterpret_cast<floatx4*>(mx);
+  if (col < MR) part[col * 4 + g] = sum;
   __syncthreads();
-  if (threadIdx.x >= 64) return;
   // lane: unit lane % 16 of the tile, row lane / 16
-  const int r = lane >> 4, j = lane & 15;
+  const int t = (int)threadIdx.x, r = t >> 4, j = t & 15;
+  if (r >= MR || r >= a.m || tile * 16 + j >= a.n) return;
   float v = 0.f;
 #pragma unroll
-  for (int u = 0; u < W; ++u) v += part[u][r * 4 + (j >> 2)][j & 3];
-  if (r < a.m && tile * 16 + j < a.n) finish<T>(a, r, tile * 16 + j, v);
+  for (int u = 0; u < W; ++u) v += reinterpret_cast<const float*>(lds[u])[r * 16 + j];
+  finish<T>(a, r, tile * 16 + j, v);
 }
 
-// Few rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; DEPTH chunks of
-// codes and of x are on their way.  A lane's x belongs to row 16 rt + lane % 16: lanes of rows that are not there load nothing, so that one row costs
-// the memory pipe a 16th of what 16 cost it.
-template <typename T, int NT, int RT, int W, int DEPTH>
-__global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W4Layout l) {
+// More rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; DEPTH chunks of
+// codes and of x are on their way.  x comes in whole rows of a chunk, 256 bytes to 16 lanes, and is turned into B operands in a piece of LDS
+// that only its wave uses: asked for as the operands want it, 64 bytes to a row, sixteen rows of a large power of two apart, it came
+// out of few channels of the caches (8192 units by 8192, 16 rows: 20 us, with twice the units to a wave 15).
+// FL: steps of 32 between two applications of the scales, 4 where groups are whole chunks, 2 or 1 where they are not.
+template <typename T, int NT, int RT, int W, int DEPTH, int FL>
+__global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
   typedef W4Type<T> C;
   typedef typename C::vec vec;
-  __shared__ floatx4 part[W][NT * RT][64];
+  constexpr int XL = 4 * RT;   // loads of x of a chunk, four rows each
+  constexpr int XPIECES = RT * 256, SUMS = NT * RT * 64;
+  __shared__ __attribute__((aligned(16))) uintx4 lds[W][XPIECES > SUMS ? XPIECES : SUMS];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int tile0 = (int)blockIdx.x * NT, m0 = (int)blockIdx.y * 16 * RT;
   const int g = lane >> 4, col = lane & 15;
@@ -156,106 +170,92 @@ __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W
     scales[t] = reinterpret_cast<const T*>(base + l.scales_at) + (size_t)tile * l.groups * 16 + 4 * g;
     zeros[t] = base + l.zeros_at + (size_t)tile * l.groups * 16 + 4 * g;
   }
-  const T* x[RT];
-  bool row_ok[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = m0 + r * 16 + col;
-    row_ok[r] = row < a.m;
-    x[r] = static_cast<const T*>(a.x) + (long)min(row, a.m - 1) * a.x_stride + 8 * g;
-  }
-  uintx4 codes[DEPTH][NT], xv[DEPTH][4][RT];
+  // load i: row 4 i + lane / 16, 16-byte piece lane % 16 of the chunk
+  const T* const x = static_cast<const T*>(a.x) + (long)m0 * a.x_stride + col * 8;
+  const int rows = a.m - m0;
+  typedef T four __attribute__((ext_vector_type(4)));
+  uintx4 codes[DEPTH][NT], xv[DEPTH][XL];
+  four sc[DEPTH][4 / FL][NT];
+  unsigned zp[DEPTH][4 / FL][NT];
   auto load = [&](int chunk, int d) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) codes[d][t] = w[t][(size_t)chunk * 64];
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
+    for (int f = 0; f < 4 / FL; ++f) {
+      const int at = min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1) * 16;
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const int k = chunk * 128 + s * 32;
-        xv[d][s][r] = (uintx4){0, 0, 0, 0};
-        if (row_ok[r] && k + 8 * g < a.k) xv[d][s][r] = *reinterpret_cast<const uintx4*>(x[r] + k);
+      for (int t = 0; t < NT; ++t) {
+        sc[d][f][t] = *reinterpret_cast<const four*>(scales[t] + at);
+        zp[d][f][t] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros[t] + at) : 0x18181818u;
       }
+    }
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      xv[d][i] = (uintx4){0, 0, 0, 0};
+      if (4 * i + g < rows && chunk * 128 + col * 8 < a.k) xv[d][i] = *reinterpret_cast<const uintx4*>(x + (long)(4 * i + g) * a.x_stride + chunk * 128);
+    }
   };
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d)
     if (first + d < last) load(first + d, d);
-  // scales and 16 + zero points of the group at hand
-  const int per_group = a.group / 32;
-  int gr = first * 4 / per_group, left = per_group - (first * 4 - gr * per_group);   // (steps left in it)
-  typedef T four __attribute__((ext_vector_type(4)));
-  four sc[NT];
-  unsigned zp[NT];
-  auto load_group = [&]() {
-    const int at = min(gr, l.groups - 1) * 16;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      sc[t] = *reinterpret_cast<const four*>(scales[t] + at);
-      zp[t] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros[t] + at) : 0x08080808u;
-    }
-  };
-  load_group();
+  uintx4* const mine = lds[wave];
   const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
-  floatx4 sum[NT][RT], acc[NT][RT], xs[RT];
+  const Widen<T> widen;
+  floatx4 sum[NT][RT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    xs[r] = (floatx4){0, 0, 0, 0};
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sum[t][r] = acc[t][r] = (floatx4){0, 0, 0, 0};
-  }
-  auto flush = [&]() {
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float z = -16.f - (float)((zp[t] >> (8 * i)) & 255u), f = (float)sc[t][i];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(f, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
-      }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      xs[r] = (floatx4){0, 0, 0, 0};
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t][r] = (floatx4){0, 0, 0, 0};
-    }
-  };
+    for (int r = 0; r < RT; ++r) sum[t][r] = (floatx4){0, 0, 0, 0};
   for (int c0 = first; c0 < last; c0 += DEPTH) {
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
       const int chunk = c0 + d;
-      if (chunk < last) {
+      if (chunk >= last) break;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+      for (int i = 0; i < XL; ++i) mine[(4 * i + g) * 16 + (col ^ ((4 * i + g) & 15))] = xv[d][i];
 #pragma unroll
-          for (int r = 0; r < RT; ++r) xs[r] = C::mfma(ones, __builtin_bit_cast(vec, xv[d][s][r]), xs[r]);
+      for (int f = 0; f < 4 / FL; ++f) {
+        floatx4 acc[NT][RT], xs[RT];
+        const floatx4 none = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = f * FL; s < (f + 1) * FL; ++s) {
+          const bool fresh = s == f * FL;
+          vec xb[RT];
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            xb[r] = __builtin_bit_cast(vec, mine[(r * 16 + col) * 16 + ((4 * s + g) ^ col)]);
+            xs[r] = C::mfma(ones, xb[r], fresh ? none : xs[r]);
+          }
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const vec wv = widen<T>(codes[d][t][s]);
+            const vec wv = widen(codes[d][t][s]);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, __builtin_bit_cast(vec, xv[d][s][r]), acc[t][r]);
-          }
-          if (--left == 0) {
-            flush();
-            ++gr;
-            left = per_group;
-            load_group();
+            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
           }
         }
-        if (chunk + DEPTH < last) load(chunk + DEPTH, d);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float z = -(float)((zp[d][f][t] >> (8 * i)) & 255u), k = (float)sc[d][f][t][i];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(k, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
+          }
       }
+      if (chunk + DEPTH < last) load(chunk + DEPTH, d);
     }
   }
-  flush();   // (a group that goes on in the next wave's part, or that the row ends in)
+  floatx4* const part = reinterpret_cast<floatx4*>(mine);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int r = 0; r < RT; ++r) part[wave][t * RT + r][lane] = sum[t][r];
+    for (int r = 0; r < RT; ++r) part[(t * RT + r) * 64 + lane] = sum[t][r];
   __syncthreads();
   for (int i = (int)threadIdx.x; i < NT * RT * 64; i += W * 64) {
     const int which = i >> 6, ln = i & 63;
     floatx4 v = {0, 0, 0, 0};
 #pragma unroll
-    for (int u = 0; u < W; ++u) v += part[u][which][ln];
+    for (int u = 0; u < W; ++u) v += reinterpret_cast<const floatx4*>(lds[u])[i];
     const int row = m0 + (which % RT) * 16 + (ln & 15), j0 = (tile0 + which / RT) * 16 + 4 * (ln >> 4);
     if (row >= a.m) continue;
 #pragma unroll
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(W * 64) void w4_rows_kernel(const W4Args a, const W
 }
 
 // a thread packs one word: eight codes, or one scale, or one zero point
-__global__ __launch_bounds__(256) void w4_pack_kernel(int n, int k, int zeros, W4Layout l, const uint8_t* codes, const uint16_t* scales,
+__global__ __launch_bounds__(256) void w4_pack_kernel(int n, int k, int zeros, int turn, W4Layout l, const uint8_t* codes, const uint16_t* scales,
                                                       const uint8_t* zps, unsigned char* out) {
   const size_t words = (size_t)l.tiles * l.chunks * 256, params = (size_t)l.tiles * l.groups * 16;
   for (size_t t = (size_t)blockIdx.x * 256 + threadIdx.x; t < words + params; t += (size_t)gridDim.x * 256) {
@@ -282,23 +282,23 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(int n, int k, int zeros, W
           w |= (b & 15u) << (4 * e) | (b >> 4) << (16 + 4 * e);
         }
       }
-      reinterpret_cast<unsigned*>(out)[t] = w;
+      reinterpret_cast<unsigned*>(out)[t] = __builtin_rotateleft32(w, turn);
     } else {
       const size_t u = t - words;
       const int j = (int)(u / ((size_t)l.groups * 16)) * 16 + (int)(u & 15), gr = (int)(u / 16 % l.groups);
       reinterpret_cast<uint16_t*>(out + l.scales_at)[u] = j < n ? scales[(size_t)j * l.groups + gr] : (uint16_t)0;
-      if (zeros) (out + l.zeros_at)[u] = j < n ? zps[(size_t)j * l.groups + gr] : (uint8_t)0;
+      if (zeros) (out + l.zeros_at)[u] = j < n ? (uint8_t)(16 + (zps[(size_t)j * l.groups + gr] & 15)) : (uint8_t)0;
     }
   }
 }
 
 }  // namespace
 
-hipError_t launch_w4_pack(const W4Args& a, const uint8_t* codes, const void* scales, const uint8_t* zeros, void* packed, hipStream_t st) {
+hipError_t launch_w4_pack(const W4Args& a, int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros, void* packed, hipStream_t st) {
   const W4Layout l = w4_layout(a.n, a.k, a.group, a.zeros != 0);
   const size_t items = (size_t)l.tiles * l.chunks * 256 + (size_t)l.tiles * l.groups * 16;
   const unsigned grid = (unsigned)((items + 255) / 256 < 65536 ? (items + 255) / 256 : 65536);
-  hipLaunchKernelGGL(w4_pack_kernel, dim3(grid), dim3(256), 0, st, a.n, a.k, a.zeros, l, codes, static_cast<const uint16_t*>(scales), zeros,
+  hipLaunchKernelGGL(w4_pack_kernel, dim3(grid), dim3(256), 0, st, a.n, a.k, a.zeros, dtype == T_F16 ? W4Type<_Float16>::kAt : W4Type<__bf16>::kAt, l, codes, static_cast<const uint16_t*>(scales), zeros,
                      static_cast<unsigned char*>(packed));
   return hipGetLastError();
 }
@@ -306,24 +306,34 @@ hipError_t launch_w4_pack(const W4Args& a, const uint8_t* codes, const void* sca
 bool w4_fits(const W4Args& a) { return a.m <= 16 * 65535; }
 
 namespace {
-#ifndef D2
-#define D2 3
-#endif
-#ifndef D1
-#define D1 4
-#endif
+template <typename T, int MR, int W>
+hipError_t launch_few(const W4Args& a, const W4Layout& l, hipStream_t st) {
+  const int per_group = a.group / 32;
+  const FastDiv fd = make_fastdiv((uint32_t)per_group);
+  const dim3 grid((unsigned)l.tiles), block(W * 64);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_few_kernel<T, MR, W, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_few_kernel<T, MR, W, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((w4_few_kernel<T, MR, W, 1>), grid, block, 0, st, a, l, fd);
+  return hipGetLastError();
+}
+
+template <typename T, int NT, int RT, int W, int DEPTH>
+hipError_t launch_rows(const W4Args& a, const W4Layout& l, hipStream_t st) {
+  const int per_group = a.group / 32;
+  const FastDiv fd = make_fastdiv((uint32_t)per_group);
+  const dim3 grid((unsigned)((l.tiles + NT - 1) / NT), (unsigned)((a.m + 16 * RT - 1) / (16 * RT))), block(W * 64);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, DEPTH, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, DEPTH, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, 1, 1>), grid, block, 0, st, a, l, fd);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
-  auto go = [&](auto kernel, int nt, int rt) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((l.tiles + nt - 1) / nt), (unsigned)((a.m + 16 * rt - 1) / (16 * rt))), dim3(512), 0, st, a, l);
-    return hipGetLastError();
-  };
-  if (a.m <= 4) {
-    hipLaunchKernelGGL((w4_few_kernel<T, 8, D1>), dim3((unsigned)l.tiles), dim3(512), 0, st, a, l, make_fastdiv((uint32_t)a.group / 32));
-    return hipGetLastError();
-  }
-  if (a.m <= 16) return go(w4_rows_kernel<T, 1, 1, 8, D2>, 1, 1);
-  return go(w4_rows_kernel<T, 2, 2, 8, 2>, 2, 2);
+  if (a.m == 1) return launch_few<T, 1, FW>(a, l, st);
+  if (a.m <= 4) return launch_few<T, 4, FW>(a, l, st);
+  if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
+  return launch_rows<T, 2, 2, 8, 1>(a, l, st);
 }
 }  // namespace
 
