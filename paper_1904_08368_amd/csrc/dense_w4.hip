@@ -8,6 +8,7 @@
 // Few rows of x: bound by the codes' bytes.  The waves of a workgroup share 16 units' rows out among them along the reduction, each
 // streams its part straight into the A operands (the packed order), and they add up through LDS.
 #include "attention.hpp"
+#include "lds_dma.hpp"
 
 #ifndef FW
 #define FW 8
@@ -264,6 +265,150 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
   }
 }
 
+// Many rows: a matrix product.  A workgroup makes 128 units of 128 rows, each of its four waves 64 of 64.  Everything goes through LDS, straight from
+// memory, two buffers each: x in halves of a chunk (64 of the reduction), one barrier to each, so that two workgroups fit a CU; codes, scales and zero
+// points, which two waves share, in whole chunks.  A word of codes is widened once for four matrix instructions.  The sums of a group and
+// those of all groups are both kept in registers, 64 each.  blockIdx.x runs over the units: workgroups that share rows of x follow each other.
+// FL as above.
+template <typename T, int FL>
+__global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
+  typedef W4Type<T> C;
+  typedef typename C::vec vec;
+  typedef T four __attribute__((ext_vector_type(4)));
+  constexpr int ROWS = 128, TILES = 8, XP = ROWS * 8, CP = TILES * 64, SP = TILES * 8, ZP = TILES * 4;   // 16-byte pieces of a buffer
+  __shared__ __attribute__((aligned(16))) uintx4 xl[2][XP], wl[2][CP + SP + ZP];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wu = wave & 1, wr = wave >> 1;
+  const int g = lane >> 4, col = lane & 15;
+  const int tile0 = (int)blockIdx.x * TILES, m0 = (int)blockIdx.y * ROWS;
+  const char* base = static_cast<const char*>(a.packed);
+  // What a wave copies: 32 rows of a half of x; of a chunk the codes of two tiles (a tile past the last is computed again and not stored), wave 0
+  // the scales and wave 1 the zero points.  Piece p (16 bytes) of a half row stands at p ^ row / 2 % 8: 16 rows' reads of one piece fall on
+  // different banks.
+  const T* xs[4];
+  int xk[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = (wave * 4 + i) * 64 + lane, row = at >> 3;
+    xk[i] = ((at & 7) ^ ((row >> 1) & 7)) * 8;
+    xs[i] = static_cast<const T*>(a.x) + (long)min(m0 + row, a.m - 1) * a.x_stride + xk[i];
+  }
+  const char* ws[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) ws[i] = base + ((size_t)min(tile0 + wave * 2 + i, l.tiles - 1) * l.chunks * 64 + lane) * 16;
+  const int ptile = wave == 0 ? lane >> 3 : lane >> 2, piece = wave == 0 ? lane & 7 : lane & 3;   // of scales: two to a group; of zero points: one
+  const bool pwanted = wave == 0 || (wave == 1 && a.zeros && lane < ZP);
+  const char* const ps = wave == 0 ? base + l.scales_at + ((size_t)min(tile0 + ptile, l.tiles - 1) * l.groups * 2 + piece) * 16
+                                   : base + l.zeros_at + ((size_t)min(tile0 + (ptile & 7), l.tiles - 1) * l.groups + piece) * 16;
+  const unsigned x_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&xl[0][0];
+  const unsigned w_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&wl[0][0];
+  auto copy_x = [&](int half) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (half * 64 + xk[i] < a.k) lds_dma16_at(x_at + (unsigned)((half & 1) * XP * 16 + (wave * 4 + i) * 1024), xs[i] + (long)half * 64);
+  };
+  auto copy_w = [&](int chunk) {
+    const unsigned to = w_at + (unsigned)((chunk & 1) * (int)sizeof(wl[0]));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) lds_dma16_at(to + (unsigned)(wave * 2 + i) * 1024u, ws[i] + (size_t)chunk * 1024);
+    if (wave < 2) {
+      const int g0 = (int)fast_div((unsigned)(chunk * 4), per_group);
+      if (pwanted && (wave == 0 ? g0 + (piece >> 1) : g0 + piece) < l.groups)
+        lds_dma16_at(to + (CP + (wave == 0 ? 0 : SP)) * 16, ps + (size_t)g0 * (wave == 0 ? 32 : 16));
+    }
+  };
+  const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
+  const Widen<T> widen;
+  const int halves = (a.k + 63) / 64;
+  floatx4 sum[4][4], acc[4][4], xsum[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) sum[t][r] = (floatx4){0, 0, 0, 0};
+  copy_w(0);
+  copy_x(0);
+  // the next half has arrived, all waves' copies, and no wave reads the buffers any more that are filled next
+  auto arrive = [&](int half) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (half + 1 < halves) {
+      copy_x(half + 1);
+    } else if (halves * 64 > a.k) {   // pieces that lie behind k are not copied: zeros
+      for (int i = (int)threadIdx.x; i < XP; i += 256)
+        if (half * 64 + ((i & 7) ^ ((i >> 4) & 7)) * 8 >= a.k) xl[half & 1][i] = (uintx4){0, 0, 0, 0};
+      __syncthreads();
+    }
+  };
+  const floatx4 none = {0, 0, 0, 0};
+  auto step = [&](int chunk, int s, bool fresh) {
+    const uintx4* const xrow = &xl[s >> 1][(wr * 64 + col) * 8];
+    const unsigned* const cl = reinterpret_cast<const unsigned*>(&wl[chunk & 1][wu * 256 + lane]) + s;
+    vec xb[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      xb[r] = __builtin_bit_cast(vec, xrow[r * 128 + ((4 * (s & 1) + g) ^ (col >> 1))]);
+      xsum[r] = C::mfma(ones, xb[r], fresh ? none : xsum[r]);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const vec wv = widen(cl[t * 256]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
+    }
+  };
+  auto apply = [&](int chunk, int s) {   // the scales and zero points of step s to the sums of its group so far
+    const four* const msc = reinterpret_cast<const four*>(&wl[chunk & 1][CP + wu * 32]) + g;               // [tile][group][4 g ..]
+    const unsigned* const mzp = reinterpret_cast<const unsigned*>(&wl[chunk & 1][CP + SP + wu * 16]) + g;
+    const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const four sc = msc[(t * 4 + gr) * 4];
+      const unsigned zp = a.zeros ? mzp[(t * 4 + gr) * 4] : 0x18181818u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = -(float)((zp >> (8 * e)) & 255u), k = (float)sc[e];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k, fmaf(z, xsum[r][e], acc[t][r][e]), sum[t][r][e]);
+      }
+    }
+  };
+  for (int chunk = 0; chunk < l.chunks; ++chunk) {
+    arrive(2 * chunk);
+    if (chunk + 1 < l.chunks) copy_w(chunk + 1);
+    step(chunk, 0, true);
+    if (FL == 1) {
+      apply(chunk, 0);
+      __builtin_amdgcn_sched_barrier(0);   // (the next step's operands, read any earlier, would not fit the registers)
+    }
+    step(chunk, 1, FL == 1);
+    if (FL <= 2) apply(chunk, 1);
+    if (2 * chunk + 1 < halves) {
+      arrive(2 * chunk + 1);
+      step(chunk, 2, FL <= 2);
+      if (FL == 1) {
+        apply(chunk, 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      step(chunk, 3, FL == 1);
+      if (FL <= 2) apply(chunk, 3);
+    }
+    if (FL == 4) apply(chunk, 0);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = m0 + wr * 64 + r * 16 + col;
+    if (row >= a.m) continue;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int j0 = (tile0 + wu * 4 + t) * 16 + 4 * g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j0 + e < a.n) finish<T>(a, row, j0 + e, sum[t][r][e]);
+    }
+  }
+}
+
 // a thread packs one word: eight codes, or one scale, or one zero point
 __global__ __launch_bounds__(256) void w4_pack_kernel(int n, int k, int zeros, int turn, W4Layout l, const uint8_t* codes, const uint16_t* scales,
                                                       const uint8_t* zps, unsigned char* out) {
@@ -329,11 +474,23 @@ hipError_t launch_rows(const W4Args& a, const W4Layout& l, hipStream_t st) {
 }
 
 template <typename T>
+hipError_t launch_tiles(const W4Args& a, const W4Layout& l, hipStream_t st) {
+  const int per_group = a.group / 32;
+  const FastDiv fd = make_fastdiv((uint32_t)per_group);
+  const dim3 grid((unsigned)((l.tiles + 7) / 8), (unsigned)((a.m + 127) / 128)), block(256);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((w4_tiles_kernel<T, 1>), grid, block, 0, st, a, l, fd);
+  return hipGetLastError();
+}
+
+template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
   if (a.m == 1) return launch_few<T, 1, FW>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, FW>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
-  return launch_rows<T, 2, 2, 8, 1>(a, l, st);
+  if (a.m <= 32) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
+  return launch_tiles<T>(a, l, st);
 }
 }  // namespace
 

@@ -5,19 +5,12 @@
 // exponentials and the LDS reads: a wave does 32 products of 32 x 32 x 16 on a tile (head_dim 128), 2048 exponentials in 32 instructions of quarter rate,
 // and reads all 32 KB of it.  Two workgroups share a CU, so that one's softmax runs beside the other's products.
 #include "attn_common.hpp"
+#include "lds_dma.hpp"
 
 namespace relay {
 namespace {
 
 constexpr int kTileRows = 128, kTileWaves = 4, kOddTiles = 16;
-
-// 16 bytes a lane from memory straight into LDS: lane i's arrive at lds_base + 16 i.  (M0: see lds_dma16.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_dma16_at(unsigned lds_base, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(p) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
