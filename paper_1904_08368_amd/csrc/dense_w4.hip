@@ -10,6 +10,9 @@
 #include "attention.hpp"
 #include "lds_dma.hpp"
 
+#ifndef TM
+#define TM 32
+#endif
 #ifndef FW
 #define FW 8
 #endif
@@ -266,8 +269,8 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
 }
 
 // Many rows: a matrix product.  A workgroup makes 128 units of 128 rows, each of its four waves 64 of 64.  Everything goes through LDS, straight from
-// memory, two buffers each: x in halves of a chunk (64 of the reduction), one barrier to each, so that two workgroups fit a CU; codes, scales and zero
-// points, which two waves share, in whole chunks.  A word of codes is widened once for four matrix instructions.  The sums of a group and
+// memory and two halves of a chunk ahead (64 of the reduction each, one barrier to each): x in a ring of three halves, so that two workgroups fit a CU; codes,
+// scales and zero points, which two waves share, in two buffers of a chunk.  A word of codes is widened once for four matrix instructions.  The sums of a group and
 // those of all groups are both kept in registers, 64 each.  blockIdx.x runs over the units: workgroups that share rows of x follow each other.
 // FL as above.
 template <typename T, int FL>
@@ -276,7 +279,8 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
   typedef typename C::vec vec;
   typedef T four __attribute__((ext_vector_type(4)));
   constexpr int ROWS = 128, TILES = 8, XP = ROWS * 8, CP = TILES * 64, SP = TILES * 8, ZP = TILES * 4;   // 16-byte pieces of a buffer
-  __shared__ __attribute__((aligned(16))) uintx4 xl[2][XP], wl[2][CP + SP + ZP];
+  constexpr int RING = 3;   // halves of x on their way or in use
+  __shared__ __attribute__((aligned(16))) uintx4 xl[RING][XP], wl[2][CP + SP + ZP];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wu = wave & 1, wr = wave >> 1;
   const int g = lane >> 4, col = lane & 15;
@@ -302,10 +306,10 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
                                    : base + l.zeros_at + ((size_t)min(tile0 + (ptile & 7), l.tiles - 1) * l.groups + piece) * 16;
   const unsigned x_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&xl[0][0];
   const unsigned w_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&wl[0][0];
-  auto copy_x = [&](int half) {
+  auto copy_x = [&](int half, int slot) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (half * 64 + xk[i] < a.k) lds_dma16_at(x_at + (unsigned)((half & 1) * XP * 16 + (wave * 4 + i) * 1024), xs[i] + (long)half * 64);
+      if (half * 64 + xk[i] < a.k) lds_dma16_at(x_at + (unsigned)(slot * XP * 16 + (wave * 4 + i) * 1024), xs[i] + (long)half * 64);
   };
   auto copy_w = [&](int chunk) {
     const unsigned to = w_at + (unsigned)((chunk & 1) * (int)sizeof(wl[0]));
@@ -325,24 +329,51 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int t = 0; t < 4; ++t) sum[t][r] = (floatx4){0, 0, 0, 0};
+  if (!a.zeros && lane < ZP) wl[wave & 1][CP + SP + lane] = (uintx4){0x18181818u, 0x18181818u, 0x18181818u, 0x18181818u};   // (16 + 8, to stay)
+  copy_x(0, 0);
   copy_w(0);
-  copy_x(0);
-  // the next half has arrived, all waves' copies, and no wave reads the buffers any more that are filled next
-  auto arrive = [&](int half) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  if (halves > 1) copy_x(1, 1);
+  // Half `half` has arrived, all waves' copies of it, and no wave reads the buffers any more that are filled next.  A wave's copies return in order: behind
+  // those of this half it has asked for the next half of x (four) and, since an even half, for a chunk's codes (two and, wave 0, the scales).
+  int slot = 0;   // of the half at hand in the ring
+  auto arrive = [&](int half, bool odd) {
+    if (half + 2 >= halves) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else if (!odd) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
+    else if (wave) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(7) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (half + 1 < halves) {
-      copy_x(half + 1);
-    } else if (halves * 64 > a.k) {   // pieces that lie behind k are not copied: zeros
+    if (half + 2 < halves) copy_x(half + 2, slot == 0 ? 2 : slot - 1);
+    if (half + 1 == halves && halves * 64 > a.k) {   // pieces that lie behind k are not copied: zeros
       for (int i = (int)threadIdx.x; i < XP; i += 256)
-        if (half * 64 + ((i & 7) ^ ((i >> 4) & 7)) * 8 >= a.k) xl[half & 1][i] = (uintx4){0, 0, 0, 0};
+        if (half * 64 + ((i & 7) ^ ((i >> 4) & 7)) * 8 >= a.k) xl[slot][i] = (uintx4){0, 0, 0, 0};
       __syncthreads();
     }
   };
   const floatx4 none = {0, 0, 0, 0};
+  auto scales_of = [&](int chunk, int s, int t, float (&k)[4], float (&z)[4]) {
+    const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
+    const four sc = (reinterpret_cast<const four*>(&wl[chunk & 1][CP + wu * 32]) + g)[(t * 4 + gr) * 4];   // [tile][group][4 g ..]
+    const unsigned zp = (reinterpret_cast<const unsigned*>(&wl[chunk & 1][CP + SP + wu * 16]) + g)[(t * 4 + gr) * 4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      k[e] = (float)sc[e];
+      z[e] = -(float)((zp >> (8 * e)) & 255u);
+    }
+  };
+  auto apply = [&](int chunk, int s) {   // the scales and zero points of step s to the sums of its group so far
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float k[4], z[4];
+      scales_of(chunk, s, t, k, z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], fmaf(z[e], xsum[r][e], acc[t][r][e]), sum[t][r][e]);
+    }
+  };
   auto step = [&](int chunk, int s, bool fresh) {
-    const uintx4* const xrow = &xl[s >> 1][(wr * 64 + col) * 8];
+    const uintx4* const xrow = &xl[slot][(wr * 64 + col) * 8];
     const unsigned* const cl = reinterpret_cast<const unsigned*>(&wl[chunk & 1][wu * 256 + lane]) + s;
     vec xb[4];
 #pragma unroll
@@ -353,45 +384,36 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const vec wv = widen(cl[t * 256]);
+      if constexpr (FL == 1) {   // (a tile's sums are used up at once and take a fourth of the registers, which reads ahead of them would fill)
+        __builtin_amdgcn_sched_barrier(0);
+        floatx4 p[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
-    }
-  };
-  auto apply = [&](int chunk, int s) {   // the scales and zero points of step s to the sums of its group so far
-    const four* const msc = reinterpret_cast<const four*>(&wl[chunk & 1][CP + wu * 32]) + g;               // [tile][group][4 g ..]
-    const unsigned* const mzp = reinterpret_cast<const unsigned*>(&wl[chunk & 1][CP + SP + wu * 16]) + g;
-    const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
+        for (int r = 0; r < 4; ++r) p[r] = C::mfma(wv, xb[r], none);
+        float k[4], z[4];
+        scales_of(chunk, s, t, k, z);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const four sc = msc[(t * 4 + gr) * 4];
-      const unsigned zp = a.zeros ? mzp[(t * 4 + gr) * 4] : 0x18181818u;
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float z = -(float)((zp >> (8 * e)) & 255u), k = (float)sc[e];
+          for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], fmaf(z[e], xsum[r][e], p[r][e]), sum[t][r][e]);
+      } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k, fmaf(z, xsum[r][e], acc[t][r][e]), sum[t][r][e]);
+        for (int r = 0; r < 4; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
       }
     }
   };
   for (int chunk = 0; chunk < l.chunks; ++chunk) {
-    arrive(2 * chunk);
+    arrive(2 * chunk, false);
     if (chunk + 1 < l.chunks) copy_w(chunk + 1);
     step(chunk, 0, true);
-    if (FL == 1) {
-      apply(chunk, 0);
-      __builtin_amdgcn_sched_barrier(0);   // (the next step's operands, read any earlier, would not fit the registers)
-    }
     step(chunk, 1, FL == 1);
-    if (FL <= 2) apply(chunk, 1);
+    if (FL == 2) apply(chunk, 1);
+    slot = slot == 2 ? 0 : slot + 1;
     if (2 * chunk + 1 < halves) {
-      arrive(2 * chunk + 1);
+      arrive(2 * chunk + 1, true);
       step(chunk, 2, FL <= 2);
-      if (FL == 1) {
-        apply(chunk, 2);
-        __builtin_amdgcn_sched_barrier(0);
-      }
       step(chunk, 3, FL == 1);
-      if (FL <= 2) apply(chunk, 3);
+      if (FL == 2) apply(chunk, 3);
+      slot = slot == 2 ? 0 : slot + 1;
     }
     if (FL == 4) apply(chunk, 0);
   }
@@ -489,7 +511,7 @@ hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
   if (a.m == 1) return launch_few<T, 1, FW>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, FW>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
-  if (a.m <= 32) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
+  if (a.m <= TM) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
   return launch_tiles<T>(a, l, st);
 }
 }  // namespace
