@@ -10,9 +10,6 @@
 #include "attention.hpp"
 #include "lds_dma.hpp"
 
-#ifndef TM
-#define TM 32
-#endif
 #ifndef FW
 #define FW 8
 #endif
@@ -506,13 +503,22 @@ hipError_t launch_tiles(const W4Args& a, const W4Layout& l, hipStream_t st) {
   return hipGetLastError();
 }
 
+// More than 16 rows: 32 at a time on the kernel whose waves share the reduction out, or as tiles of 128 x 128, each of which walks the whole reduction:
+// 1.85 us a chunk where a CU has one of them, 2.6 where it has two.  The other kernel takes 2.5 us and 0.73 ns a workgroup and chunk.  Measured, rows / tiles,
+// us, groups of 128: 8192 units by 8192, 64 rows 26 / 116, 128 rows 49 / 118, 256 rows 94 / 119; 4096 x 4096, 300 rows 33 / 63; 28000 x 4096, 64 rows
+// 48 / 63; 1500 x 2000 in groups of 64, 200 rows 11 / 39.
+bool rows_pay(const W4Args& a, const W4Layout& l) {
+  const long tiles = ((l.tiles + 7L) / 8) * ((a.m + 127) / 128), rows = ((l.tiles + 1L) / 2) * ((a.m + 31) / 32);
+  const double t_tiles = l.chunks * (tiles <= 256 ? 1.85 : 2.6 * (double)((tiles + 511) / 512)), t_rows = 2.5 + 0.73e-3 * (double)rows * l.chunks;
+  return t_rows < t_tiles;
+}
+
 template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
   if (a.m == 1) return launch_few<T, 1, FW>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, FW>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
-  if (a.m <= TM) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
-  return launch_tiles<T>(a, l, st);
+  return rows_pay(a, l) ? launch_rows<T, 2, 2, 8, 1>(a, l, st) : launch_tiles<T>(a, l, st);
 }
 }  // namespace
 
