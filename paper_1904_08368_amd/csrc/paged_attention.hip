@@ -20,15 +20,14 @@ constexpr int kRows = 16, kBlock = 32;
 // Arrival counters lie 64 bytes apart in front of the workspace, in a region of their own that is the same for every call.
 constexpr int kCounters = 1024;
 constexpr size_t kCounterBytes = (size_t)kCounters * 64;
-// workgroups that units are dealt out to, and so the most pieces of a tile
-#ifndef MP
-#define MP 256
-#endif
-constexpr int kMostPieces = MP;
+// workgroups that units are dealt out to, one to a CU, and so the most pieces of a tile; fewer of four waves where eight are the rule
+constexpr int kMostPieces = 256;
+constexpr int most_pieces(int dp, int waves) { return dp <= 128 && waves == 4 ? kMostPieces / 2 : kMostPieces; }
 
 struct RowsPlan {
   int row_tiles;   // tiles of 16 rows of a sequence, at most
   int deal;        // 1: units of all tiles are dealt out over the grid; 0: a workgroup to a tile
+  int unit;        // keys of a unit
 };
 
 // floats that a workgroup leaves behind: sums [16][DP], then maximum and sum of each row
@@ -39,19 +38,19 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // What one sequence brings to the line of units: its tiles (over all key heads), and the units of each.
 struct Share {
   int tiles, units, lo, hi;
-  __device__ Share(const AttnArgs& a, const Seq& s, int round) {
+  __device__ Share(const AttnArgs& a, const Seq& s, int unit) {
     const int nq = min(s.nq, a.max_q_len);
     tiles = nq > 0 ? (int)(((long)nq * a.group + kRows - 1) / kRows) * a.kv_heads : 0;
     lo = nq > 0 ? s.first(a, 0) : 0;
     hi = nq > 0 ? s.last(a, nq - 1) + 1 : 0;
-    units = max(1, (hi - lo + round - 1) / round);
+    units = max(1, (hi - lo + unit - 1) / unit);
   }
 };
 
 // Units of sequence b (none past the last).
-__device__ __forceinline__ int seq_units(const AttnArgs& a, int b, int round) {
+__device__ __forceinline__ int seq_units(const AttnArgs& a, int b, int unit) {
   if (b >= a.batch) return 0;
-  const Share sh(a, Seq(a, b), round);
+  const Share sh(a, Seq(a, b), unit);
   return sh.tiles * sh.units;
 }
 // How many units the lanes up to this one have.
@@ -65,15 +64,15 @@ __device__ __forceinline__ int units_upto(int n, int lane) {
 // The line of units: the first 64 sequences' in the lanes, the others' read again where they are wanted.
 struct Line {
   int n, upto, total;   // units of sequence `lane`, of it and those ahead of it, of all
-  __device__ Line(const AttnArgs& a, int round, int lane, bool wanted) : n(0), upto(0), total(0) {
+  __device__ Line(const AttnArgs& a, int size, int lane, bool wanted) : n(0), upto(0), total(0) {
     if (!wanted) return;
-    n = seq_units(a, lane, round);
+    n = seq_units(a, lane, size);
     upto = units_upto(n, lane);
     total = __builtin_amdgcn_readlane(upto, 63);
-    for (int b0 = 64; b0 < a.batch; b0 += 64) total += __builtin_amdgcn_readlane(units_upto(seq_units(a, b0 + lane, round), lane), 63);
+    for (int b0 = 64; b0 < a.batch; b0 += 64) total += __builtin_amdgcn_readlane(units_upto(seq_units(a, b0 + lane, size), lane), 63);
   }
   // the sequence that a unit lies in, and the units ahead of that sequence
-  __device__ void find(const AttnArgs& a, int unit, int round, int lane, int& b, int& before) const {
+  __device__ void find(const AttnArgs& a, int unit, int size, int lane, int& b, int& before) const {
     int nn = n, up = upto, ahead = 0;
     for (int b0 = 0;; b0 += 64) {
       const unsigned long long past = __ballot(unit < ahead + up);
@@ -84,7 +83,7 @@ struct Line {
         return;
       }
       ahead += __builtin_amdgcn_readlane(up, 63);
-      nn = seq_units(a, b0 + 64 + lane, round);
+      nn = seq_units(a, b0 + 64 + lane, size);
       up = units_upto(nn, lane);
     }
   }
@@ -110,7 +109,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
   // This workgroup's run of units.
   const int w_no = (int)blockIdx.x;
   int unit = 0, end = 1, run = 1;
-  const Line line(a, ROUND, lane, pl.deal != 0);
+  const Line line(a, pl.unit, lane, pl.deal != 0);
   if (pl.deal) {
     run = uniform(max(1, (line.total + (int)gridDim.x - 1) / (int)gridDim.x));
     unit = w_no * run;
@@ -121,9 +120,9 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
 
   for (int piece = 0; unit < end; ++piece) {
     if (!pl.deal) b = (int)blockIdx.z;
-    else if (unit >= seq_end) line.find(a, unit, ROUND, lane, b, before);
+    else if (unit >= seq_end) line.find(a, unit, pl.unit, lane, b, before);
     const Seq s(a, b);
-    const Share sh(a, s, ROUND);
+    const Share sh(a, s, pl.unit);
     int in_seq, tile_unit = 0;   // tile of the sequence; its first unit
     if (pl.deal) {
       seq_end = before + sh.tiles * sh.units;
@@ -139,8 +138,8 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     const bool whole_tile = !pl.deal || (unit == tile_unit && stop == tile_unit + sh.units);
     const int i_min = (int)fast_div((unsigned)r0, a.fd_group), i_max = (int)fast_div((unsigned)min(r0 + kRows - 1, rows - 1), a.fd_group);
     // the keys of this piece, as far as the tile's rows see them
-    const int lo = max(s.first(a, i_min), sh.lo + (unit - tile_unit) * ROUND);
-    const int hi = pl.deal ? min(s.last(a, i_max) + 1, sh.lo + (stop - tile_unit) * ROUND) : s.last(a, i_max) + 1;
+    const int lo = max(s.first(a, i_min), sh.lo + (unit - tile_unit) * pl.unit);
+    const int hi = pl.deal ? min(s.last(a, i_max) + 1, sh.lo + (stop - tile_unit) * pl.unit) : s.last(a, i_max) + 1;
     // keys from full_lo to below full_hi are seen by all rows of the tile
     const int full_lo = s.first(a, i_max), full_hi = s.last(a, i_min) + 1;
     // this lane's row
@@ -231,7 +230,8 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       }
       const unsigned readable = can;
       unsigned long long odd = 0;   // keys with an infinity or a NaN among their values (bits 0..15, 32..47: first and second 16)
-      if (readable != 0xffffffffu || j0 < full_lo || j0 + kBlock > full_hi) {   // some of the rows may not see all of its keys
+      const bool shared = j0 < full_lo || min(j0 + kBlock, hi) > full_hi;   // some of the rows may not see all of its keys
+      if (shared || readable != 0xffffffffu) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const bool ok = readable >> (t * 16 + col) & 1;
@@ -242,11 +242,13 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
             for (int e = 0; e < 4; ++e) {
               const unsigned v = vf[t][k][e];
               vf[t][k][e] = ok ? v : 0u;
-              bad |= ok && not_finite<T>(v);
+              if (shared) bad |= ok && not_finite<T>(v);
             }
-          unsigned long long bl = __ballot(bad);
-          bl |= bl >> 32;
-          odd |= ((bl | bl >> 16) & 0xffffull) << (32 * t);
+          if (shared) {
+            unsigned long long bl = __ballot(bad);
+            bl |= bl >> 32;
+            odd |= ((bl | bl >> 16) & 0xffffull) << (32 * t);
+          }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -401,9 +403,10 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     // maxima [piece][16] and sums [piece][16]; each wave makes weights of some rows' maxima, then all threads add up the pieces
     constexpr int THREADS = W * 64;
     float* const weight = reinterpret_cast<float*>(vs[0]);
-    float* const lsum = weight + kMostPieces * kRows;
-    static_assert(sizeof(vs) >= (2 * kMostPieces + 1) * kRows * 4 && sizeof(vs) >= (kMostPieces + THREADS / 4 + 1) * kRows * 4, "LDS of the join");
-    float* const row_sum = lsum + kMostPieces * kRows;
+    constexpr int PIECES = most_pieces(DP, W);
+    float* const lsum = weight + PIECES * kRows;
+    static_assert(sizeof(vs) >= (2 * PIECES + 1) * kRows * 4 && PIECES * kRows * 4 >= THREADS * 16, "LDS of the join");
+    float* const row_sum = lsum + PIECES * kRows;
 #pragma unroll 4
     for (int i = tid_c; i < pieces * kRows; i += THREADS) {
       const float* p = slot(i / kRows) + kRows * DP + i % kRows;
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     }
     __syncthreads();
     // where the rows' float4s are fewer than the threads, several threads share one: thread group `sub` of `subs` takes every subs-th piece
-    constexpr int JB = 8;   // loads in flight: each is a round trip to memory, other XCDs wrote the pieces
+    constexpr int JB = 16;   // loads in flight: each is a round trip to memory, other XCDs wrote the pieces
     const int items = live * (DP / 4), subs = max(1, THREADS / items);
     floatx4* const shared_sums = reinterpret_cast<floatx4*>(lsum);
     for (int it0 = 0; it0 < items; it0 += THREADS) {
@@ -455,17 +458,10 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
 
 int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 
-#ifndef DEALMIN
-#define DEALMIN 1
-#endif
-#ifndef NWAVES
-#define NWAVES 8
-#endif
-// waves of a workgroup: eight where their registers leave a CU room for them
-int waves_of(int dp) { return dp <= 128 ? NWAVES : 4; }
 struct RowsGrid {
   RowsPlan plan;
   dim3 grid;
+  int waves;
 };
 
 RowsGrid rows_plan(const AttnArgs& a, bool share) {
@@ -473,31 +469,42 @@ RowsGrid rows_plan(const AttnArgs& a, bool share) {
   const int dp = padded_dim(a.head_dim);
   p.plan.row_tiles = (int)(((long)a.max_q_len * a.group + kRows - 1) / kRows);
   const long tiles = (long)a.batch * a.kv_heads * p.plan.row_tiles;
-  const int round = waves_of(dp) * kBlock;
-  // the most units of a tile, from the keys between the first and the last that a sequence's rows see
+  // the most keys between the first and the last that a sequence's rows see
   const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
-  const long units = max(1L, (keys + round - 1) / round);
-  p.plan.deal = share && tiles <= kCounters && units > DEALMIN && tiles * units < 1L << 30;
-  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)kMostPieces));
+  // Eight waves where their registers leave a CU room for them, four where rounds of theirs do not even give half of the CUs one: less to launch
+  // and to join (us, four / eight waves: one sequence of 700 keys, 8 key heads 12.0 / 14.9, 1500 keys 12.7 / 15.4; 8 sequences of 3000 keys 36.7 / 32.7).
+  p.waves = dp > 128 || tiles * ((keys + 4 * kBlock - 1) / (4 * kBlock)) <= most_pieces(dp, 4) ? 4 : 8;
+  const int round = p.waves * kBlock;
+  // A unit is a round of the waves; where there are more of those than workgroups, a quarter of one, so that their shares come out more even
+  // (one sequence of 100001 keys, 4 key heads: 1564 rounds are seven to a workgroup, 6251 quarters 25).
+  p.plan.unit = tiles * ((keys + round - 1) / round) > kMostPieces ? round / 4 : round;
+  const long units = max(1L, (keys + p.plan.unit - 1) / p.plan.unit);
+  p.plan.deal = share && tiles <= kCounters && units > 1 && tiles * units < 1L << 30;
+  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)most_pieces(dp, p.waves)));
   else p.grid = dim3((unsigned)p.plan.row_tiles, (unsigned)a.kv_heads, (unsigned)a.batch);
   return p;
 }
 
 template <typename T, int DP, int W>
-hipError_t launch_dim(const AttnArgs& a, const RowsGrid& p, hipStream_t st) {
+hipError_t launch_waves(const AttnArgs& a, const RowsGrid& p, hipStream_t st) {
   if (a.head_dim == DP) hipLaunchKernelGGL((attn_rows_kernel<T, DP, true, W>), p.grid, dim3(W * 64), 0, st, a, p.plan);
   else hipLaunchKernelGGL((attn_rows_kernel<T, DP, false, W>), p.grid, dim3(W * 64), 0, st, a, p.plan);
   return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch_dim(const AttnArgs& a, const RowsGrid& p, hipStream_t st) {
+  return p.waves == 4 ? launch_waves<T, DP, 4>(a, p, st) : launch_waves<T, DP, 8>(a, p, st);
 }
 
 template <typename T>
 hipError_t launch_rows(const AttnArgs& a, hipStream_t st) {
   const RowsGrid p = rows_plan(a, a.workspace != nullptr);
   switch (padded_dim(a.head_dim)) {
-    case 64: return launch_dim<T, 64, NWAVES>(a, p, st);
-    case 96: return launch_dim<T, 96, NWAVES>(a, p, st);
-    case 128: return launch_dim<T, 128, NWAVES>(a, p, st);
-    default: return launch_dim<T, 256, 4>(a, p, st);
+    case 64: return launch_dim<T, 64>(a, p, st);
+    case 96: return launch_dim<T, 96>(a, p, st);
+    case 128: return launch_dim<T, 128>(a, p, st);
+    default: return launch_waves<T, 256, 4>(a, p, st);
   }
 }
 
