@@ -5,10 +5,11 @@
 // of 32 keys in turn, each with a softmax of its own: keys go from memory straight into the A operands of S^T = K Q^T, values through a
 // piece of LDS that only their wave uses, so that no wave waits for another before the end.
 //
-// Lengths differ from sequence to sequence and are known on the device only.  So the work is dealt out there: a tile's keys are units
-// of a round of the waves, the units of all tiles stand in one line, and each of as many workgroups as fit the chip at once takes an equal
-// run of them.  A tile that lies within one run is finished by it; of others each workgroup leaves sums, maximum and weight in the
-// workspace, and the one that arrives last joins them in the order of the line.
+// Lengths differ from sequence to sequence and are known on the device only.  So the work is dealt out there: a tile's keys are units, the units
+// of all tiles stand in one line, and each of as many workgroups as fit the chip at once takes an equal run of them.  Where there are fewer tiles than
+// workgroups, a unit is made as long as lets every workgroup have one; else units are short and a run goes over several tiles.  A tile
+// that lies within one run is finished by it; of others each workgroup leaves sums, maximum and weight in the workspace, and the one that arrives last
+// joins them in the order of the line.
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -30,31 +31,28 @@ struct RowsPlan {
   int unit;        // keys of a unit
 };
 
-// floats that a workgroup leaves behind: sums [16][DP], then maximum and sum of each row
+// floats that a workgroup leaves behind: sums [16][DP], then the pair of maximum and sum of each row
 template <int DP> constexpr int part_floats() { return kRows * DP + 2 * kRows; }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// What one sequence brings to the line of units: its tiles (over all key heads), and the units of each.
+// What one sequence brings to the line of units: its tiles (over all key heads), and the keys that its rows see, which are the units of each.
 struct Share {
-  int tiles, units, lo, hi;
-  __device__ Share(const AttnArgs& a, const Seq& s, int unit) {
+  int tiles, lo, hi;
+  __device__ Share(const AttnArgs& a, int b) : tiles(0), lo(0), hi(0) {
+    if (b >= a.batch) return;
+    const Seq s(a, b);
     const int nq = min(s.nq, a.max_q_len);
-    tiles = nq > 0 ? (int)(((long)nq * a.group + kRows - 1) / kRows) * a.kv_heads : 0;
-    lo = nq > 0 ? s.first(a, 0) : 0;
-    hi = nq > 0 ? s.last(a, nq - 1) + 1 : 0;
-    units = max(1, (hi - lo + unit - 1) / unit);
+    if (nq <= 0) return;
+    tiles = (int)(((long)nq * a.group + kRows - 1) / kRows) * a.kv_heads;
+    lo = s.first(a, 0);
+    hi = s.last(a, nq - 1) + 1;
   }
+  __device__ int units(int size) const { return max(1, (hi - lo + size - 1) / size); }
 };
 
-// Units of sequence b (none past the last).
-__device__ __forceinline__ int seq_units(const AttnArgs& a, int b, int unit) {
-  if (b >= a.batch) return 0;
-  const Share sh(a, Seq(a, b), unit);
-  return sh.tiles * sh.units;
-}
-// How many units the lanes up to this one have.
-__device__ __forceinline__ int units_upto(int n, int lane) {
+// How much the lanes up to this one have.
+__device__ __forceinline__ int upto_lane(int n, int lane) {
   for (int o = 1; o < 64; o <<= 1) {
     const int t = __shfl_up(n, o, 64);
     n += lane >= o ? t : 0;
@@ -63,16 +61,35 @@ __device__ __forceinline__ int units_upto(int n, int lane) {
 }
 // The line of units: the first 64 sequences' in the lanes, the others' read again where they are wanted.
 struct Line {
+  int size;             // keys of a unit
   int n, upto, total;   // units of sequence `lane`, of it and those ahead of it, of all
-  __device__ Line(const AttnArgs& a, int size, int lane, bool wanted) : n(0), upto(0), total(0) {
-    if (!wanted) return;
-    n = seq_units(a, lane, size);
-    upto = units_upto(n, lane);
+  __device__ Line() : size(0), n(0), upto(0), total(0) {}
+  __device__ Line(const AttnArgs& a, int unit, int workers, int round, int lane) : size(unit) {
+    const Share sh(a, lane);
+    if (a.batch <= 64) {
+      const int tiles = __builtin_amdgcn_readlane(upto_lane(sh.tiles, lane), 63);
+      if (tiles <= workers) {
+        // as long as needed for one to every worker: from an estimate, in a few steps (a unit to a tile is few enough)
+        float keys = (float)sh.tiles * (float)(sh.hi - sh.lo);
+        for (int o = 32; o > 0; o >>= 1) keys += __shfl_xor(keys, o, 64);
+        size = max(round, uniform((int)fminf(keys / (float)workers, 1.0e9f)) + 63 & ~63);
+        for (;;) {
+          const int all = __builtin_amdgcn_readlane(upto_lane(sh.tiles * sh.units(size), lane), 63);
+          if (all <= workers) break;
+          size = (int)min((long)size * all / workers, 1L << 30) + 64 & ~63;
+        }
+      }
+    }
+    n = sh.tiles * sh.units(size);
+    upto = upto_lane(n, lane);
     total = __builtin_amdgcn_readlane(upto, 63);
-    for (int b0 = 64; b0 < a.batch; b0 += 64) total += __builtin_amdgcn_readlane(units_upto(seq_units(a, b0 + lane, size), lane), 63);
+    for (int b0 = 64; b0 < a.batch; b0 += 64) {
+      const Share next(a, b0 + lane);
+      total += __builtin_amdgcn_readlane(upto_lane(next.tiles * next.units(size), lane), 63);
+    }
   }
   // the sequence that a unit lies in, and the units ahead of that sequence
-  __device__ void find(const AttnArgs& a, int unit, int size, int lane, int& b, int& before) const {
+  __device__ void find(const AttnArgs& a, int unit, int lane, int& b, int& before) const {
     int nn = n, up = upto, ahead = 0;
     for (int b0 = 0;; b0 += 64) {
       const unsigned long long past = __ballot(unit < ahead + up);
@@ -83,11 +100,26 @@ struct Line {
         return;
       }
       ahead += __builtin_amdgcn_readlane(up, 63);
-      nn = seq_units(a, b0 + 64 + lane, size);
-      up = units_upto(nn, lane);
+      const Share next(a, b0 + 64 + lane);
+      nn = next.tiles * next.units(size);
+      up = upto_lane(nn, lane);
     }
   }
 };
+
+// Pieces go through the workspace in 8-byte stores and loads of device scope.  The XCDs' L2s are not coherent with each other, and to release or acquire
+// ordinary ones would write back and invalidate a whole L2, under the feet of the workgroups that stream through it.
+__device__ __forceinline__ void put_piece(float* p, float x, float y) {
+  typedef float floatx2 __attribute__((ext_vector_type(2)));
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, (floatx2){x, y}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uintx2 get_piece(const float* p) {
+  return __builtin_bit_cast(uintx2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ floatx4 get_piece4(const float* p) {
+  const uintx2 a = get_piece(p), b = get_piece(p + 2);
+  return __builtin_bit_cast(floatx4, (uintx4){a[0], a[1], b[0], b[1]});
+}
 
 // FULL: head_dim is DP.  W: waves of a workgroup.
 template <typename T, int DP, bool FULL, int W>
@@ -95,7 +127,8 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
   typedef Mma<T> M;
   typedef typename M::vec vec;
   constexpr int KS = DP / 32, DT = DP / 16, PITCH = DP + 8, ROUND = W * kBlock;
-  static_assert(kBlock * PITCH * 2 >= kRows * DP * 4, "a wave's sums take the place of its values");
+  constexpr int SUMS = DP + 4;   // floats from one row's sums to the next in LDS: 16 rows on different banks
+  static_assert(kBlock * PITCH * 2 >= kRows * SUMS * 4, "a wave's sums take the place of its values");
   __shared__ __attribute__((aligned(16))) T vs[W][kBlock * PITCH];
   __shared__ float sm[W][kRows], sl[W][kRows];
   __shared__ int s_last;
@@ -108,38 +141,46 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
 
   // This workgroup's run of units.
   const int w_no = (int)blockIdx.x;
-  int unit = 0, end = 1, run = 1;
-  const Line line(a, pl.unit, lane, pl.deal != 0);
+  int unit = 0, end = 1, run = 1, size = 0;
+  int b = (int)blockIdx.z, before = 0, tiles = 1, units = 1, keys_lo = 0;   // the sequence at hand, units ahead of it, its tiles, their units, its first key
+  int seq_end = 0;                                                          // the first unit behind it
+  Line line;
   if (pl.deal) {
+    line = Line(a, pl.unit, (int)gridDim.x, ROUND, lane);
+    size = line.size;
     run = uniform(max(1, (line.total + (int)gridDim.x - 1) / (int)gridDim.x));
     unit = w_no * run;
     end = min(line.total, unit + run);
   }
-  int b = 0, before = 0;
-  int seq_end = 0;   // the first unit behind the sequence at hand
 
   for (int piece = 0; unit < end; ++piece) {
-    if (!pl.deal) b = (int)blockIdx.z;
-    else if (unit >= seq_end) line.find(a, unit, pl.unit, lane, b, before);
-    const Seq s(a, b);
-    const Share sh(a, s, pl.unit);
     int in_seq, tile_unit = 0;   // tile of the sequence; its first unit
+    if (pl.deal && unit >= seq_end) line.find(a, unit, lane, b, before);
+    const Seq s(a, b);
+    if (!pl.deal || unit >= seq_end) {
+      const Share sh(a, b);
+      tiles = sh.tiles;
+      keys_lo = sh.lo;
+      if (pl.deal) {
+        units = uniform(sh.units(size));
+        seq_end = before + tiles * units;
+      }
+    }
     if (pl.deal) {
-      seq_end = before + sh.tiles * sh.units;
-      in_seq = uniform((unit - before) / sh.units);
-      tile_unit = before + in_seq * sh.units;
+      in_seq = uniform((unit - before) / units);
+      tile_unit = before + in_seq * units;
     } else {
       in_seq = (int)blockIdx.x * a.kv_heads + (int)blockIdx.y;
-      if (in_seq >= sh.tiles) return;
+      if (in_seq >= tiles) return;
     }
     const int rows = min(s.nq, a.max_q_len) * a.group;
     const int tile = (int)fast_div((unsigned)in_seq, a.fd_kv_heads), hk = in_seq - tile * a.kv_heads, r0 = tile * kRows;
-    const int stop = pl.deal ? min(end, tile_unit + sh.units) : end;
-    const bool whole_tile = !pl.deal || (unit == tile_unit && stop == tile_unit + sh.units);
+    const int stop = pl.deal ? min(end, tile_unit + units) : end;
+    const bool whole_tile = !pl.deal || (unit == tile_unit && stop == tile_unit + units);
     const int i_min = (int)fast_div((unsigned)r0, a.fd_group), i_max = (int)fast_div((unsigned)min(r0 + kRows - 1, rows - 1), a.fd_group);
     // the keys of this piece, as far as the tile's rows see them
-    const int lo = max(s.first(a, i_min), sh.lo + (unit - tile_unit) * pl.unit);
-    const int hi = pl.deal ? min(s.last(a, i_max) + 1, sh.lo + (stop - tile_unit) * pl.unit) : s.last(a, i_max) + 1;
+    const int lo = max(s.first(a, i_min), keys_lo + (unit - tile_unit) * size);
+    const int hi = pl.deal ? min(s.last(a, i_max) + 1, keys_lo + (stop - tile_unit) * size) : s.last(a, i_max) + 1;
     // keys from full_lo to below full_hi are seen by all rows of the tile
     const int full_lo = s.first(a, i_max), full_hi = s.last(a, i_min) + 1;
     // this lane's row
@@ -330,15 +371,16 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       sl[wave][col_c] = l;
     }
     __syncthreads();
+    const int live = min(kRows, rows - r0);
     float mt = kNegInf;
 #pragma unroll
     for (int w = 0; w < W; ++w) mt = fmaxf(mt, sm[w][col_c]);
     const float own = m == kNegInf ? 0.f : pow2((m - mt) * c);
     float* const part = reinterpret_cast<float*>(vs[wave]);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4*>(part + col_c * DP + d * 16 + g_c * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
+    for (int d = 0; d < DT; ++d)
+      if (col_c < live) *reinterpret_cast<floatx4*>(part + col_c * SUMS + d * 16 + g_c * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
     __syncthreads();
-    const int live = min(kRows, rows - r0);
     float* const slots = pl.deal ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) : nullptr;
     float* const mine = pl.deal ? slots + (size_t)(2 * w_no + (piece > 0 ? 1 : 0)) * part_floats<DP>() : nullptr;
 
@@ -360,7 +402,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       float mm = kNegInf, lt = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        o += *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(vs[w]) + cc * DP + d);
+        o += *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(vs[w]) + cc * SUMS + d);
         mm = fmaxf(mm, sm[w][cc]);
       }
 #pragma unroll
@@ -369,50 +411,55 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
         put(cc, d, o, lt);
         continue;
       }
-      *reinterpret_cast<floatx4*>(mine + cc * DP + d) = o;
-      if (d == 0) {
-        mine[kRows * DP + cc] = mm;
-        mine[kRows * DP + kRows + cc] = lt;
-      }
+      put_piece(mine + cc * DP + d, o[0], o[1]);
+      put_piece(mine + cc * DP + d + 2, o[2], o[3]);
+      if (d == 0) put_piece(mine + kRows * DP + 2 * cc, mm, lt);
     }
-    __syncthreads();   // (the next piece takes the waves' LDS; or all of this one's sums are on their way)
     unit = stop;
     if (whole_tile) {
       if (!pl.deal) return;
+      __syncthreads();   // (the next piece takes the waves' LDS)
       continue;
     }
 
-    // The workgroup that counts itself last joins the tile.  The XCDs' L2s are not coherent with each other: the partial results are
-    // released to device scope before the count and acquired after it, by one wave for the workgroup.
-    const int w_first = uniform(tile_unit / run), w_last = uniform((tile_unit + sh.units - 1) / run);
+    // The workgroup that counts itself last, behind every wave's stores, joins the tile.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int w_first = uniform(tile_unit / run), w_last = uniform((tile_unit + units - 1) / run);
     const int pieces = w_last - w_first + 1;
     if (tid == 0) {
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
       unsigned* cnt = static_cast<unsigned*>(a.workspace) + (b * pl.row_tiles * a.kv_heads + in_seq) * 16;
-      const unsigned old = atomicAdd(cnt, 1u);
+      const unsigned old = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       s_last = old == (unsigned)(pieces - 1);
-      if (s_last) {
-        atomicExch(cnt, 0u);
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-      }
+      if (s_last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!s_last) continue;
     // the first of them may have come to this tile behind another one, the others start with it
     auto slot = [&](int u) { return slots + (size_t)(2 * (w_first + u) + (u == 0 && w_first * run < tile_unit ? 1 : 0)) * part_floats<DP>(); };
+    // Where the rows' float4s are fewer than the threads, several threads share one: thread group `sub` of `subs` takes every subs-th piece.  The first
+    // JB of a thread's loads (each a trip to memory: other XCDs wrote the pieces) are on their way while the weights are made.
+    constexpr int THREADS = W * 64, JB = 8, PIECES = most_pieces(DP, W);
+    const int items = live * (DP / 4), subs = max(1, THREADS / items), sub = subs > 1 ? tid_c / items : 0;
+    auto fetch_pieces = [&](int it, int u, floatx4 (&t)[JB]) {
+#pragma unroll
+      for (int e = 0; e < JB; ++e) t[e] = get_piece4(slot(min(u + e * subs, pieces - 1)) + it / (DP / 4) * DP + it % (DP / 4) * 4);
+    };
+    auto wanted = [&](int it) { return it < items && sub < subs && (FULL || it % (DP / 4) * 4 < D); };
+    floatx4 t[JB];
+    if (wanted(tid_c - sub * items)) fetch_pieces(tid_c - sub * items, sub, t);
     // maxima [piece][16] and sums [piece][16]; each wave makes weights of some rows' maxima, then all threads add up the pieces
-    constexpr int THREADS = W * 64;
     float* const weight = reinterpret_cast<float*>(vs[0]);
-    constexpr int PIECES = most_pieces(DP, W);
     float* const lsum = weight + PIECES * kRows;
     static_assert(sizeof(vs) >= (2 * PIECES + 1) * kRows * 4 && PIECES * kRows * 4 >= THREADS * 16, "LDS of the join");
     float* const row_sum = lsum + PIECES * kRows;
-#pragma unroll 4
-    for (int i = tid_c; i < pieces * kRows; i += THREADS) {
-      const float* p = slot(i / kRows) + kRows * DP + i % kRows;
-      weight[i] = p[0];
-      lsum[i] = p[kRows];
-    }
+#pragma unroll 2
+    for (int i = tid_c; i < pieces * kRows; i += THREADS)
+      if (i % kRows < live) {
+        const uintx2 p = get_piece(slot(i / kRows) + kRows * DP + 2 * (i % kRows));
+        weight[i] = __builtin_bit_cast(float, (unsigned)p[0]);
+        lsum[i] = __builtin_bit_cast(float, (unsigned)p[1]);
+      }
     __syncthreads();
     for (int cc = wave; cc < live; cc += W) {
       float mm = kNegInf, lt = 0.f;
@@ -427,20 +474,13 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       if (lane == 0) row_sum[cc] = lt;
     }
     __syncthreads();
-    // where the rows' float4s are fewer than the threads, several threads share one: thread group `sub` of `subs` takes every subs-th piece
-    constexpr int JB = 16;   // loads in flight: each is a round trip to memory, other XCDs wrote the pieces
-    const int items = live * (DP / 4), subs = max(1, THREADS / items);
     floatx4* const shared_sums = reinterpret_cast<floatx4*>(lsum);
     for (int it0 = 0; it0 < items; it0 += THREADS) {
-      const int sub = subs > 1 ? tid_c / items : 0, it = it0 + tid_c - sub * items;
-      const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
-      const bool mine_too = it < items && sub < subs && (FULL || d < D);
+      const int it = it0 + tid_c - sub * items, cc = it / (DP / 4);
       floatx4 o = {0, 0, 0, 0};
-      if (mine_too)
+      if (wanted(it))
         for (int u = sub; u < pieces; u += JB * subs) {
-          floatx4 t[JB];
-#pragma unroll
-          for (int e = 0; e < JB; ++e) t[e] = *reinterpret_cast<const floatx4*>(slot(min(u + e * subs, pieces - 1)) + cc * DP + d);
+          if (it0 > 0 || u > sub) fetch_pieces(it, u, t);
 #pragma unroll
           for (int e = 0; e < JB; ++e) o += u + e * subs < pieces ? t[e] * weight[(u + e * subs) * kRows + cc] : (floatx4){0, 0, 0, 0};
         }
@@ -450,7 +490,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
         if (sub == 0)
           for (int e = 1; e < subs; ++e) o += shared_sums[e * items + it];
       }
-      if (mine_too && sub == 0) put(cc, d, o, row_sum[cc]);
+      if (wanted(it) && sub == 0) put(cc, it % (DP / 4) * 4, o, row_sum[cc]);
     }
     __syncthreads();
   }
