@@ -178,7 +178,6 @@ static relay_status attention_args(const relay_paged_attention_desc* d, relay::A
   a.scale_log2 = (float)((double)d->scale * 1.4426950408889634074);
   a.fd_page = relay::make_fastdiv((uint32_t)d->page_size);
   a.fd_group = relay::make_fastdiv((uint32_t)a.group);
-  a.fd_kv_heads = relay::make_fastdiv((uint32_t)a.kv_heads);
   a.q_token = d->q_token_stride; a.out_token = d->out_token_stride;
   a.page_stride = d->page_stride; a.slot_stride = d->slot_stride; a.head_stride = d->head_stride;
   if (!relay::attn_fits(a)) return fail(RELAY_ERR_SHAPE, "paged attention: batch=%d heads=%d and max_kv_len=%d exceed one launch", d->batch, d->q_heads, d->max_kv_len);

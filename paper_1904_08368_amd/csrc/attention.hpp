@@ -60,7 +60,7 @@ struct AttnArgs {
   int num_pages, page_size, pages_per_seq;
   int max_q_len, max_kv_len, causal, window;
   float scale_log2;              // scale * log2(e)
-  FastDiv fd_page, fd_group, fd_kv_heads;
+  FastDiv fd_page, fd_group;
   int64_t q_token, out_token, page_stride, slot_stride, head_stride;
   void* workspace;
 };
@@ -69,6 +69,7 @@ size_t attn_workspace_bytes(const AttnArgs& a);
 bool attn_fits(const AttnArgs& a);
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t st);
 // the kernel for many rows (paged_attention_tiles.hip)
+size_t attn_tiles_workspace_bytes(const AttnArgs& a);
 hipError_t launch_attention_tiles(const AttnArgs& a, int dtype, hipStream_t st);
 
 // Packed 4-bit weights.  Units in tiles of 16, the reduction in chunks of 128; a tile's chunk is 64 x 16 bytes, the A operands of four

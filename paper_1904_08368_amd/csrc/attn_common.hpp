@@ -86,6 +86,10 @@ __device__ __forceinline__ unsigned only_finite(unsigned w) {
   return w;
 }
 
+// Arrival counters lie 64 bytes apart in front of the workspace, in a region of their own that is the same for every call.
+constexpr int kCounters = 1024;
+constexpr size_t kCounterBytes = (size_t)kCounters * 64;
+
 // One sequence as a workgroup sees it.
 struct Seq {
   int start, nq, kv;   // first row of q; new tokens; keys

@@ -30,6 +30,11 @@ __device__ __forceinline__ void lds_dma16_at(unsigned lds_base, const void* p) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(p) : "memory", "m0");
 }
 
+// The same from a wave-uniform address and 32-bit offsets of the lanes.
+__device__ __forceinline__ void lds_dma16_from(unsigned lds_base, const void* base, unsigned voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(base) : "memory", "m0");
+}
+
 // Touches 64 memory lines of 128 bytes, one per lane, so that they are on their way to this XCD's L2: the four bytes
 // each lane fetches land in a 256-byte dump block of LDS and are never read.
 __device__ __forceinline__ void l2_touch(intx4 rsrc, unsigned dump_base, unsigned voff) {

@@ -1,7 +1,7 @@
 // Attention of new tokens over a paged cache:  o = sum_j softmax_j(scale q.k_j) v_j  over the keys a token sees.
 //
-// attn_rows_kernel: few query rows to a key head (a decode step, a short chunk).  A row is a token and one of the query heads that share the key
-// head, 16 rows to a tile: bound by the bytes of the keys and values, which are read once for a tile's rows.  A workgroup's waves take blocks
+// attn_rows_kernel: at most 16 query rows to a key head, one tile (a decode step, a few tokens at once).  A row is a token and one of the query heads
+// that share the key head.  Bound by the bytes of the keys and values, which are read once.  A workgroup's waves take blocks
 // of 32 keys in turn, each with a softmax of its own: keys go from memory straight into the A operands of S^T = K Q^T, values through a
 // piece of LDS that only their wave uses, so that no wave waits for another before the end.
 //
@@ -18,15 +18,11 @@ namespace relay {
 namespace {
 
 constexpr int kRows = 16, kBlock = 32;
-// Arrival counters lie 64 bytes apart in front of the workspace, in a region of their own that is the same for every call.
-constexpr int kCounters = 1024;
-constexpr size_t kCounterBytes = (size_t)kCounters * 64;
 // workgroups that units are dealt out to, one to a CU, and so the most pieces of a tile; fewer of four waves where eight are the rule
 constexpr int kMostPieces = 256;
 constexpr int most_pieces(int dp, int waves) { return dp <= 128 && waves == 4 ? kMostPieces / 2 : kMostPieces; }
 
 struct RowsPlan {
-  int row_tiles;   // tiles of 16 rows of a sequence, at most
   int deal;        // 1: units of all tiles are dealt out over the grid; 0: a workgroup to a tile
   int unit;        // keys of a unit
 };
@@ -36,7 +32,7 @@ template <int DP> constexpr int part_floats() { return kRows * DP + 2 * kRows; }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// What one sequence brings to the line of units: its tiles (over all key heads), and the keys that its rows see, which are the units of each.
+// What one sequence brings to the line of units: its tiles (one to a key head), and the keys that its rows see, which are the units of each.
 struct Share {
   int tiles, lo, hi;
   __device__ Share(const AttnArgs& a, int b) : tiles(0), lo(0), hi(0) {
@@ -44,7 +40,7 @@ struct Share {
     const Seq s(a, b);
     const int nq = min(s.nq, a.max_q_len);
     if (nq <= 0) return;
-    tiles = (int)(((long)nq * a.group + kRows - 1) / kRows) * a.kv_heads;
+    tiles = a.kv_heads;
     lo = s.first(a, 0);
     hi = s.last(a, nq - 1) + 1;
   }
@@ -142,7 +138,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
   // This workgroup's run of units.
   const int w_no = (int)blockIdx.x;
   int unit = 0, end = 1, run = 1, size = 0;
-  int b = (int)blockIdx.z, before = 0, tiles = 1, units = 1, keys_lo = 0;   // the sequence at hand, units ahead of it, its tiles, their units, its first key
+  int b = (int)blockIdx.y, before = 0, tiles = 1, units = 1, keys_lo = 0;   // the sequence at hand, units ahead of it, its tiles, their units, its first key
   int seq_end = 0;                                                          // the first unit behind it
   Line line;
   if (pl.deal) {
@@ -154,7 +150,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
   }
 
   for (int piece = 0; unit < end; ++piece) {
-    int in_seq, tile_unit = 0;   // tile of the sequence; its first unit
+    int hk, tile_unit = 0;   // key head; its first unit
     if (pl.deal && unit >= seq_end) line.find(a, unit, lane, b, before);
     const Seq s(a, b);
     if (!pl.deal || unit >= seq_end) {
@@ -167,24 +163,23 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       }
     }
     if (pl.deal) {
-      in_seq = uniform((unit - before) / units);
-      tile_unit = before + in_seq * units;
+      hk = uniform((unit - before) / units);
+      tile_unit = before + hk * units;
     } else {
-      in_seq = (int)blockIdx.x * a.kv_heads + (int)blockIdx.y;
-      if (in_seq >= tiles) return;
+      hk = (int)blockIdx.x;
+      if (hk >= tiles) return;   // (no new tokens)
     }
     const int rows = min(s.nq, a.max_q_len) * a.group;
-    const int tile = (int)fast_div((unsigned)in_seq, a.fd_kv_heads), hk = in_seq - tile * a.kv_heads, r0 = tile * kRows;
     const int stop = pl.deal ? min(end, tile_unit + units) : end;
     const bool whole_tile = !pl.deal || (unit == tile_unit && stop == tile_unit + units);
-    const int i_min = (int)fast_div((unsigned)r0, a.fd_group), i_max = (int)fast_div((unsigned)min(r0 + kRows - 1, rows - 1), a.fd_group);
+    const int i_max = min(s.nq, a.max_q_len) - 1;
     // the keys of this piece, as far as the tile's rows see them
-    const int lo = max(s.first(a, i_min), keys_lo + (unit - tile_unit) * size);
+    const int lo = max(s.first(a, 0), keys_lo + (unit - tile_unit) * size);
     const int hi = pl.deal ? min(s.last(a, i_max) + 1, keys_lo + (stop - tile_unit) * size) : s.last(a, i_max) + 1;
     // keys from full_lo to below full_hi are seen by all rows of the tile
-    const int full_lo = s.first(a, i_max), full_hi = s.last(a, i_min) + 1;
+    const int full_lo = s.first(a, i_max), full_hi = s.last(a, 0) + 1;
     // this lane's row
-    const int r = r0 + col, ri = (int)fast_div((unsigned)min(r, rows - 1), a.fd_group);
+    const int r = col, ri = (int)fast_div((unsigned)min(r, rows - 1), a.fd_group);
     const int token = s.start + ri, head = hk * a.group + min(r, rows - 1) - ri * a.group;
     const bool row_ok = r < rows && (unsigned)token < (unsigned)a.tokens;
     const int my_first = s.first(a, ri), my_last = s.last(a, ri);
@@ -371,7 +366,6 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       sl[wave][col_c] = l;
     }
     __syncthreads();
-    const int live = min(kRows, rows - r0);
     float mt = kNegInf;
 #pragma unroll
     for (int w = 0; w < W; ++w) mt = fmaxf(mt, sm[w][col_c]);
@@ -379,23 +373,23 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     float* const part = reinterpret_cast<float*>(vs[wave]);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
-      if (col_c < live) *reinterpret_cast<floatx4*>(part + col_c * SUMS + d * 16 + g_c * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
+      if (col_c < rows) *reinterpret_cast<floatx4*>(part + col_c * SUMS + d * 16 + g_c * 4) = m == kNegInf ? (floatx4){0, 0, 0, 0} : acc[d] * own;
     __syncthreads();
     float* const slots = pl.deal ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kCounterBytes) : nullptr;
     float* const mine = pl.deal ? slots + (size_t)(2 * w_no + (piece > 0 ? 1 : 0)) * part_floats<DP>() : nullptr;
 
     // one float4 of the output; row `cc` of the tile
     auto put = [&](int cc, int d, floatx4 o, float lt) {
-      const int rr = r0 + cc, ii = (int)fast_div((unsigned)rr, a.fd_group);
+      const int ii = (int)fast_div((unsigned)cc, a.fd_group);
       const int tk = s.start + ii;
       if ((unsigned)tk >= (unsigned)a.tokens) return;
       const bool none = s.last(a, ii) < s.first(a, ii);
       const float inv = 1.f / lt;
       uintx2 w = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
       if (none) w = (uintx2){0, 0};
-      *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)tk * a.out_token + (long)(hk * a.group + rr - ii * a.group) * D + d) = w;
+      *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)tk * a.out_token + (long)(hk * a.group + cc - ii * a.group) * D + d) = w;
     };
-    for (int it = tid_c; it < live * (DP / 4); it += W * 64) {
+    for (int it = tid_c; it < rows * (DP / 4); it += W * 64) {
       const int cc = it / (DP / 4), d = it % (DP / 4) * 4;
       if (!FULL && d >= D) continue;
       floatx4 o = {0, 0, 0, 0};
@@ -428,7 +422,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     const int w_first = uniform(tile_unit / run), w_last = uniform((tile_unit + units - 1) / run);
     const int pieces = w_last - w_first + 1;
     if (tid == 0) {
-      unsigned* cnt = static_cast<unsigned*>(a.workspace) + (b * pl.row_tiles * a.kv_heads + in_seq) * 16;
+      unsigned* cnt = static_cast<unsigned*>(a.workspace) + (b * a.kv_heads + hk) * 16;
       const unsigned old = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       s_last = old == (unsigned)(pieces - 1);
       if (s_last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -440,7 +434,7 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     // Where the rows' float4s are fewer than the threads, several threads share one: thread group `sub` of `subs` takes every subs-th piece.  The first
     // JB of a thread's loads (each a trip to memory: other XCDs wrote the pieces) are on their way while the weights are made.
     constexpr int THREADS = W * 64, JB = 8, PIECES = most_pieces(DP, W);
-    const int items = live * (DP / 4), subs = max(1, THREADS / items), sub = subs > 1 ? tid_c / items : 0;
+    const int items = rows * (DP / 4), subs = max(1, THREADS / items), sub = subs > 1 ? tid_c / items : 0;
     auto fetch_pieces = [&](int it, int u, floatx4 (&t)[JB]) {
 #pragma unroll
       for (int e = 0; e < JB; ++e) t[e] = get_piece4(slot(min(u + e * subs, pieces - 1)) + it / (DP / 4) * DP + it % (DP / 4) * 4);
@@ -455,13 +449,13 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
     float* const row_sum = lsum + PIECES * kRows;
 #pragma unroll 2
     for (int i = tid_c; i < pieces * kRows; i += THREADS)
-      if (i % kRows < live) {
+      if (i % kRows < rows) {
         const uintx2 p = get_piece(slot(i / kRows) + kRows * DP + 2 * (i % kRows));
         weight[i] = __builtin_bit_cast(float, (unsigned)p[0]);
         lsum[i] = __builtin_bit_cast(float, (unsigned)p[1]);
       }
     __syncthreads();
-    for (int cc = wave; cc < live; cc += W) {
+    for (int cc = wave; cc < rows; cc += W) {
       float mm = kNegInf, lt = 0.f;
       for (int u = lane; u < pieces; u += 64) mm = fmaxf(mm, weight[u * kRows + cc]);
       for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o, 64));
@@ -507,8 +501,7 @@ struct RowsGrid {
 RowsGrid rows_plan(const AttnArgs& a, bool share) {
   RowsGrid p;
   const int dp = padded_dim(a.head_dim);
-  p.plan.row_tiles = (int)(((long)a.max_q_len * a.group + kRows - 1) / kRows);
-  const long tiles = (long)a.batch * a.kv_heads * p.plan.row_tiles;
+  const long tiles = (long)a.batch * a.kv_heads;
   // the most keys between the first and the last that a sequence's rows see
   const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
   // Eight waves where their registers leave a CU room for them, four where rounds of theirs do not even give half of the CUs one: less to launch
@@ -521,7 +514,7 @@ RowsGrid rows_plan(const AttnArgs& a, bool share) {
   const long units = max(1L, (keys + p.plan.unit - 1) / p.plan.unit);
   p.plan.deal = share && tiles <= kCounters && units > 1 && tiles * units < 1L << 30;
   if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)most_pieces(dp, p.waves)));
-  else p.grid = dim3((unsigned)p.plan.row_tiles, (unsigned)a.kv_heads, (unsigned)a.batch);
+  else p.grid = dim3((unsigned)a.kv_heads, (unsigned)a.batch);
   return p;
 }
 
@@ -550,22 +543,25 @@ hipError_t launch_rows(const AttnArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// More rows than one tile go to the other kernel, whose tiles read the keys once for 128 (us, this kernel with a tile more for every 16 rows / the other: 24 rows
+// of 8 key heads, one sequence of 4000 keys 18.6 / 17.6, of 30000 44.9 / 44.2, 8 sequences of 30000 234 / 171; 96 rows, one of 30000 108 / 44).
+static bool many_rows(const AttnArgs& a) { return (long)a.max_q_len * a.group > kRows; }
+
 size_t attn_workspace_bytes(const AttnArgs& a) {
   if (a.max_q_len == 0) return 0;
+  if (many_rows(a)) return attn_tiles_workspace_bytes(a);
   const RowsGrid p = rows_plan(a, true);
   if (!p.plan.deal) return 0;
   return kCounterBytes + (size_t)p.grid.x * 2 * (size_t)(kRows * padded_dim(a.head_dim) + 2 * kRows) * 4;
 }
 
 bool attn_fits(const AttnArgs& a) {
-  return a.kv_heads < 65536 && a.batch < 65536 && a.max_kv_len <= 1 << 30 && (double)a.max_q_len * a.group * a.kv_heads < 1073741824.0;
+  return a.kv_heads < 65536 && a.batch < 65536 && a.max_kv_len <= 1 << 30 && (double)a.max_q_len * a.group * a.kv_heads < 1073741824.0 &&
+         (double)a.batch * a.kv_heads * ((double)a.max_q_len * a.group / 128 + 1) < 8388608.0;   // (workgroups of the larger tiles)
 }
 
-#ifndef TILEROWS
-#define TILEROWS 32
-#endif
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t st) {
-  if ((long)a.max_q_len * a.group > TILEROWS) return launch_attention_tiles(a, dtype, st);
+  if (many_rows(a)) return launch_attention_tiles(a, dtype, st);
   return dtype == T_F16 ? launch_rows<_Float16>(a, st) : launch_rows<__bf16>(a, st);
 }
 

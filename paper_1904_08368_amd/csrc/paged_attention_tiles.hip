@@ -4,6 +4,8 @@
 // time, staged in LDS for all of them without passing through registers, two buffers, one barrier a tile.  Bound by the matrix cores and, close behind, by the
 // exponentials and the LDS reads: a wave does 32 products of 32 x 32 x 16 on a tile (head_dim 128), 2048 exponentials in 32 instructions of quarter rate,
 // and reads all 32 KB of it.  Two workgroups share a CU, so that one's softmax runs beside the other's products.
+#include <type_traits>
+
 #include "attn_common.hpp"
 #include "lds_dma.hpp"
 
@@ -37,28 +39,59 @@ template <int CH> __device__ __forceinline__ int v_place(int row, int c) {
   return CH == 8 ? c ^ (((row >> 1) & 1) << 2) : c ^ ((row & 3) << 2);
 }
 
-template <typename T, int DP, bool FULL>
-__global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles_kernel(const AttnArgs a, const int groups, const int tiles) {
+// How the work is cut: groups (a sequence's key head), tiles of rows of a group, parts of a tile's keys of `unit` steps each.
+struct TilesPlan {
+  int groups, tiles, parts, unit;
+};
+
+// The workgroups of a CU, by registers and LDS.
+constexpr int workgroups_of_cu(int dp) { return dp <= 64 ? 3 : dp <= 128 ? 2 : 1; }
+constexpr int tile_keys(int dp) { return dp <= 128 ? 64 : 32; }
+
+// The keys of a tile of rows: steps of KEYS from `start` on, and into how many parts they are cut.
+struct Span {
+  int lo, hi, start, steps, parts;
+  template <typename TokenOf>
+  __device__ Span(const AttnArgs& a, const TilesPlan& pl, const Seq& s, int r0, int keys, int align, TokenOf token_of) {
+    lo = s.first(a, token_of(r0));
+    hi = s.last(a, token_of(r0 + kTileRows - 1)) + 1;
+    start = lo & -align;
+    steps = max(0, (hi - start + keys - 1) / keys);
+    parts = max(1, min(pl.parts, (steps + pl.unit - 1) / pl.unit));
+  }
+  // first step of a part
+  __device__ int first(int part) const { return (int)((long)steps * part / parts); }
+};
+
+// What a workgroup leaves of its part of a tile, in floats: the sums [d / 4][thread][4], then the reference and the sum of each row.
+template <int DP> constexpr int cut_floats() { return kTileRows * DP + 2 * kTileRows; }
+
+// FULL: head_dim is DP.  PAGED: the 16 keys that a wave copies of a step lie in one page.
+template <typename T, int DP, bool FULL, bool PAGED>
+__global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_tiles_kernel(const AttnArgs a, const TilesPlan pl) {
   typedef Mma<T> M;
   typedef typename M::vec vec;
     // keys of a tile; chunks of a row; steps of the two products; copies of a wave
-  constexpr int KEYS = DP <= 128 ? 64 : 32, NB = KEYS / 32, CH = DP / 8, KS = DP / 16, DB = DP / 32, PER = KEYS * CH / (kTileWaves * 64);
+  constexpr int KEYS = tile_keys(DP), NB = KEYS / 32, CH = DP / 8, KS = DP / 16, DB = DP / 32, PER = KEYS * CH / (kTileWaves * 64);
   constexpr unsigned long long ALL = KEYS == 64 ? ~0ull : (1ull << KEYS) - 1;
   __shared__ __attribute__((aligned(16))) T kv[2][2][KEYS * DP];    // [buffer][keys, values]
   __shared__ int s_odd, s_odd_at[kOddTiles];   // tiles whose values hold an infinity or a NaN, see below
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
   const int D = FULL ? DP : a.head_dim;
   // Key heads vary fastest, so that those of one XCD (a workgroup in eight) are the same few; the tiles with the most keys go first.
-  const int grp = (int)blockIdx.x % groups, tile = tiles - 1 - (int)blockIdx.x / groups;
+  const int grp = (int)blockIdx.x % pl.groups, cut = (int)blockIdx.x / pl.groups, part = cut % pl.parts, tile = pl.tiles - 1 - cut / pl.parts;
   const int b = grp / a.kv_heads, hk = grp - b * a.kv_heads;
   const Seq s(a, b);
   const int rows = min(s.nq, a.max_q_len) * a.group, r0 = tile * kTileRows;
   if (r0 >= rows) return;
+  auto token_of = [&](int r) { return (int)fast_div((unsigned)min(r, rows - 1), a.fd_group); };
+  const Span span(a, pl, s, r0, KEYS, PAGED ? 16 : 1, token_of);
+  if (part >= span.parts) return;
   const unsigned flip = a.scale_log2 < 0.f ? 0x80008000u : 0u, keep = a.scale_log2 == 0.f ? 0u : 0xffffffffu;
   const float c = keep ? fabsf(a.scale_log2) : 1.f;
-  auto token_of = [&](int r) { return (int)fast_div((unsigned)min(r, rows - 1), a.fd_group); };
-  // keys of the tile, of this wave's rows, and those that all of them see
-  const int lo = s.first(a, token_of(r0)), hi = s.last(a, token_of(r0 + kTileRows - 1)) + 1;
+  // keys of this part, of this wave's rows, and those that all of them see
+  const int hi = min(span.hi, span.start + span.first(part + 1) * KEYS), first = span.start + span.first(part) * KEYS, lo = max(span.lo, first);
+  const int start = lo < hi ? first : hi;
   const int w0 = r0 + wave * 32, iw0 = token_of(w0), iw1 = token_of(w0 + 31);
   const int w_lo = s.first(a, iw0), w_hi = w0 < rows ? s.last(a, iw1) + 1 : 0;
   const int full_lo = s.first(a, token_of(r0 + kTileRows - 1)), full_hi = s.last(a, token_of(r0)) + 1;
@@ -83,24 +116,61 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
     const int j = j0 + lane;
     pageno = pages[fast_div((unsigned)(j < hi ? j : lo), a.fd_page)];
   };
-  // Starts the copy of a tile; the keys that can be read.  The others' places are taken by the tile's first key that is read anyway.
-  auto copy_tile = [&](int j0, int buf) {
-    const int j = min(j0 + lane, hi - 1);
-    const bool ok = lane < KEYS && j0 + lane < hi && (unsigned)pageno < (unsigned)a.num_pages;
-    const int slot = j - (int)fast_div((unsigned)j, a.fd_page) * a.page_size;
-    const long at = 2 * ((long)pageno * a.page_stride + (long)slot * a.slot_stride);
-    const unsigned long long can = __ballot(ok);
-    const long off = ok ? at : 0;
-    const unsigned base = lds_address(&kv[buf][0][0]) + (unsigned)(wave * PER * 1024);
+  // PAGED: where this lane's 16 bytes of each of the wave's copies lie, from the wave's first key on.
+  unsigned k_at[PER], v_at[PER];
+  if constexpr (PAGED)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int place = (wave * PER + i) * 64 + lane, row = place / CH, p = place - row * CH;
-      const long o = __shfl(off, row, 64);
-      const int ck = k_chunk<CH>(row, p), cv = v_place<CH>(row, p);
-      if (FULL || ck * 8 < D) lds_dma16_at(base + i * 1024, kbase + o + ck * 16);
-      if (FULL || cv * 8 < D) lds_dma16_at(base + KEYS * DP * 2 + i * 1024, vbase + o + cv * 16);
+      const int row = (i * 64 + lane) / CH, p = i * 64 + lane - row * CH, all = wave * (KEYS / 4) + row;
+      k_at[i] = 2u * (unsigned)(row * (int)a.slot_stride) + 16u * (unsigned)k_chunk<CH>(all, p);
+      v_at[i] = 2u * (unsigned)(row * (int)a.slot_stride) + 16u * (unsigned)v_place<CH>(all, p);
     }
-    return can;
+  // The copies of a step: where they take from, and the keys that can be read.  In the others' places goes what can be read anyway: other keys of
+  // the page, or of the cache's first.
+  const char *kfrom = kbase, *vfrom = vbase;
+  long from[PAGED ? 1 : PER];
+  auto locate = [&](int j0) {
+    const bool ok = (lane < KEYS) & (j0 + lane >= lo) & (j0 + lane < hi) & ((unsigned)pageno < (unsigned)a.num_pages);
+    if constexpr (PAGED) {
+      const int at = wave * (KEYS / 4), j = j0 + at, page = __builtin_amdgcn_readlane(pageno, at);
+      const bool there = (j < hi) & ((unsigned)page < (unsigned)a.num_pages);
+      const int slot = j - (int)fast_div((unsigned)j, a.fd_page) * a.page_size;
+      const long off = 2 * ((long)(there ? page : 0) * a.page_stride + (long)(there ? slot : 0) * a.slot_stride);
+      kfrom = kbase + off;
+      vfrom = vbase + off;
+    } else {
+      const int j = min(j0 + lane, hi - 1);
+      const int slot = j - (int)fast_div((unsigned)j, a.fd_page) * a.page_size;
+      const long at = 2 * ((long)pageno * a.page_stride + (long)slot * a.slot_stride);
+      const long off = ok ? at : 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) from[i] = __shfl(off, ((wave * PER + i) * 64 + lane) / CH, 64);
+    }
+    return __ballot(ok);
+  };
+  // one of the wave's copies of keys, of values
+  auto copy_keys = [&](int buf, int i) {
+    const int place = (wave * PER + i) * 64 + lane, row = place / CH, c = k_chunk<CH>(row, place - row * CH);
+    const unsigned to = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(&kv[buf][0][0]) + (wave * PER + i) * 1024);
+    if (FULL || c * 8 < D) {
+      if constexpr (PAGED) lds_dma16_from(to, kfrom, k_at[i]);
+      else lds_dma16_at(to, kbase + from[i] + c * 16);
+    }
+  };
+  auto copy_values = [&](int buf, int i) {
+    const int place = (wave * PER + i) * 64 + lane, row = place / CH, c = v_place<CH>(row, place - row * CH);
+    const unsigned to = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_address(&kv[buf][1][0]) + (wave * PER + i) * 1024);
+    if (FULL || c * 8 < D) {
+      if constexpr (PAGED) lds_dma16_from(to, vfrom, v_at[i]);
+      else lds_dma16_at(to, vbase + from[i] + c * 16);
+    }
+  };
+  auto copy_all = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      copy_keys(buf, i);
+      copy_values(buf, i);
+    }
   };
 
   vec qf[KS];
@@ -124,21 +194,24 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
 
   unsigned long long can = 0, can_next = 0;
   if (lo < hi) {
-    look_up(lo);
-    can_next = copy_tile(lo, 0);
-    look_up(lo + KEYS);
+    look_up(start);
+    can_next = locate(start);
+    copy_all(0);
+    look_up(start + KEYS);
   }
-  int buf = 0;
-  for (int j0 = lo; j0 < hi; j0 += KEYS, buf ^= 1) {
-    // this tile's copies have arrived, those of all waves, and no wave reads the other buffer any more
+  int buf = 0, j0 = start;
+  // One step; in between, the copies of the next one, spread out so that no wave waits to issue them.  MORE: there is a next one.
+  auto step = [&](auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    // this step's copies have arrived, those of all waves, and no wave reads the other buffer any more
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     can = can_next;
-    if (j0 + KEYS < hi) {
-      can_next = copy_tile(j0 + KEYS, buf ^ 1);
+    auto next = [&]() {
+      can_next = locate(j0 + KEYS);
       look_up(j0 + 2 * KEYS);
-    }
+    };
     const bool whole = can == ALL && j0 >= full_lo && j0 + KEYS <= full_hi;   // (the same for all waves)
     if (!whole) {
       // Not all rows see all keys.  A product of zero and an infinity would be a NaN, also for the rows that do not see the key: such
@@ -166,29 +239,55 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     }
-    if (j0 >= w_hi || j0 + KEYS <= w_lo) continue;
+    if (j0 >= w_hi || j0 + KEYS <= w_lo) {
+      if constexpr (MORE) {
+        next();
+        copy_all(buf ^ 1);
+      }
+      return;
+    }
     const T* ks = kv[buf][0];
     const T* vs = kv[buf][1];
     floatx16 st[NB];
 #pragma unroll
-    for (int t = 0; t < NB; ++t) {
+    for (int t = 0; t < NB; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) st[t][e] = 0.f;
-      const int row = t * 32 + col;
+    // (product n: step n / NB of the reduction, keys 32 (n % NB) on; keys are read AHEAD products ahead)
+    constexpr int N = NB * KS, AHEAD = 6;
+    auto keys = [&](int n) {
+      const int row = n % NB * 32 + col;
+      return *reinterpret_cast<const vec*>(ks + row * DP + k_place<CH>(row, n / NB * 2 + h) * 8);
+    };
+    vec kf[AHEAD];
+    __builtin_amdgcn_s_setprio(1);   // (products before the other workgroups' softmax: its waves fill the gaps by themselves)
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
-        st[t] = M::mfma32(*reinterpret_cast<const vec*>(ks + row * DP + k_place<CH>(row, 2 * k + h) * 8), qf[k], st[t]);
+    for (int n = 0; n < AHEAD; ++n) kf[n] = keys(n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      st[n % NB] = M::mfma32(kf[n % AHEAD], qf[n / NB], st[n % NB]);
+      if (n + AHEAD < N) kf[n % AHEAD] = keys(n + AHEAD);
+      if constexpr (MORE) {
+        if (n == 1) next();
+        if (n % (N / PER) == N / PER - 1) copy_keys(buf ^ 1, n / (N / PER));
+      }
     }
     if (!whole) {
+      // (counted from this lane's first key of the tile; the compiler would compute what depends on the lane ahead of the loop, and keep it in 100 registers)
+      int h4 = 4 * h;
+      asm volatile("" : "+v"(h4));
+      const unsigned long long mine = can >> h4;
+      const int from = my_first - j0 - h4, to = my_last - j0 - h4;
 #pragma unroll
       for (int t = 0; t < NB; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int u = t * 32 + 8 * (e / 4) + 4 * h + e % 4, j = j0 + u;
-          const bool seen = (can >> u & 1) && j >= my_first && j <= my_last;
+          const int u = t * 32 + 8 * (e / 4) + e % 4;
+          const bool seen = (mine >> u & 1) && u >= from && u <= to;
           st[t][e] = seen ? st[t][e] : kNegInf;
         }
     }
+    __builtin_amdgcn_s_setprio(0);
     float bm = st[0][0];
 #pragma unroll
     for (int t = 0; t < NB; ++t)
@@ -226,11 +325,20 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
       const uintx2 v1 = lds_transposed(vs + rb * DP + v_place<CH>(rb, d * 4 + vch) * 8 + vhalf);
       return (uintx4){v0[0], v0[1], v1[0], v1[1]};
     };
+    constexpr int N2 = 2 * NB * DB, AHEAD2 = 4;
+    uintx4 vf[AHEAD2];
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t)
+    for (int n = 0; n < AHEAD2; ++n) vf[n] = values(n / DB, n % DB);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = M::mfma32(__builtin_bit_cast(vec, values(t, d)), pf[t], acc[d]);
-  }
+    for (int n = 0; n < N2; ++n) {
+      acc[n % DB] = M::mfma32(__builtin_bit_cast(vec, vf[n % AHEAD2]), pf[n / DB], acc[n % DB]);
+      if (n + AHEAD2 < N2) vf[n % AHEAD2] = values((n + AHEAD2) / DB, (n + AHEAD2) % DB);
+      if constexpr (MORE)
+        if (n % (N2 / PER) == 0) copy_values(buf ^ 1, n / (N2 / PER));
+    }
+  };
+  for (; j0 + KEYS < hi; j0 += KEYS, buf ^= 1) step(std::true_type());
+  if (j0 < hi) step(std::false_type());
   l = sum_halves(l);
 
   // Values that were left out, tile by tile (a tile may stand in the list once for each wave: an infinity or a NaN added again is the same), or of all
@@ -239,10 +347,10 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
   const int found = __builtin_amdgcn_readfirstlane(s_odd);
   if (found) {
     const bool all = found > kOddTiles;
-    for (int n = 0; n < (all ? (hi - lo + KEYS - 1) / KEYS : found); ++n) {
-      const int j0 = all ? lo + n * KEYS : __builtin_amdgcn_readfirstlane(s_odd_at[n]);
+    for (int n = 0; n < (all ? (hi - start + KEYS - 1) / KEYS : found); ++n) {
+      const int j0 = all ? start + n * KEYS : __builtin_amdgcn_readfirstlane(s_odd_at[n]);
       look_up(j0);
-      const bool ok = lane < KEYS && j0 + lane < hi && (unsigned)pageno < (unsigned)a.num_pages;
+      const bool ok = lane < KEYS && j0 + lane >= lo && j0 + lane < hi && (unsigned)pageno < (unsigned)a.num_pages;
       const unsigned long long readable = __ballot(ok);
       if (all && readable == ALL && j0 >= full_lo && j0 + KEYS <= full_hi) continue;
 #pragma unroll 1
@@ -262,6 +370,19 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
       }
     }
   }
+  if (span.parts > 1) {
+    float* const mine = static_cast<float*>(a.workspace) + kCounterBytes / 4 + ((size_t)(grp * pl.tiles + tile) * pl.parts + part) * cut_floats<DP>();
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<floatx4*>(mine + ((d * 4 + e / 4) * kTileWaves * 64 + tid) * 4) = (floatx4){acc[d][e], acc[d][e + 1], acc[d][e + 2], acc[d][e + 3]};
+    if (h == 0) {
+      mine[kTileRows * DP + 2 * (wave * 32 + col)] = ref;
+      mine[kTileRows * DP + 2 * (wave * 32 + col) + 1] = l;
+    }
+    return;
+  }
   if (!row_ok) return;
   const bool none = my_last < my_first;
   const float inv = 1.f / l;
@@ -277,13 +398,105 @@ __global__ __launch_bounds__(kTileWaves * 64, DP <= 128 ? 2 : 1) void attn_tiles
     }
 }
 
+// Joins the parts of a tile, in their order; each thread the places of the same thread above, STEP of its float4s.
+constexpr int kJoinStep = 2, kJoinBatch = 8;
+template <typename T, int DP>
+__global__ __launch_bounds__(kTileWaves * 64) void attn_join_kernel(const AttnArgs a, const TilesPlan pl, const int align) {
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, col = lane & 31;
+  const int grp = (int)blockIdx.x % pl.groups, tile = (int)blockIdx.x / pl.groups, b = grp / a.kv_heads, hk = grp - b * a.kv_heads;
+  const Seq s(a, b);
+  const int rows = min(s.nq, a.max_q_len) * a.group, r0 = tile * kTileRows;
+  if (r0 >= rows) return;
+  auto token_of = [&](int r) { return (int)fast_div((unsigned)min(r, rows - 1), a.fd_group); };
+  const Span span(a, pl, s, r0, tile_keys(DP), align, token_of);
+  if (span.parts == 1) return;
+  const int r = r0 + wave * 32 + col, ri = token_of(r), token = s.start + ri, head = hk * a.group + min(r, rows - 1) - ri * a.group;
+  const float* const parts = static_cast<const float*>(a.workspace) + kCounterBytes / 4 + (size_t)(grp * pl.tiles + tile) * pl.parts * cut_floats<DP>();
+  const float* const stats = parts + kTileRows * DP + 2 * (wave * 32 + col);
+  // (kJoinBatch parts at a time are on their way; those past the last are it again, and do not count)
+  float m = kNegInf, l = 0.f;
+  for (int u = 0; u < span.parts; u += kJoinBatch) {
+    float mu[kJoinBatch];
+#pragma unroll
+    for (int e = 0; e < kJoinBatch; ++e) mu[e] = stats[(size_t)min(u + e, span.parts - 1) * cut_floats<DP>()];
+#pragma unroll
+    for (int e = 0; e < kJoinBatch; ++e) m = fmaxf(m, mu[e]);
+  }
+  floatx4 o[kJoinStep];
+#pragma unroll
+  for (int i = 0; i < kJoinStep; ++i) o[i] = (floatx4){0, 0, 0, 0};
+  const int first = (int)blockIdx.y * kJoinStep;
+  for (int u = 0; u < span.parts; u += kJoinBatch) {
+    float mu[kJoinBatch], lu[kJoinBatch];
+    floatx4 x[kJoinBatch][kJoinStep];
+#pragma unroll
+    for (int e = 0; e < kJoinBatch; ++e) {
+      const size_t at = (size_t)min(u + e, span.parts - 1) * cut_floats<DP>();
+      mu[e] = stats[at];
+      lu[e] = stats[at + 1];
+#pragma unroll
+      for (int i = 0; i < kJoinStep; ++i) x[e][i] = *reinterpret_cast<const floatx4*>(parts + at + ((first + i) * kTileWaves * 64 + tid) * 4);
+    }
+#pragma unroll
+    for (int e = 0; e < kJoinBatch; ++e)
+      if (u + e < span.parts) {
+        const float w = mu[e] == kNegInf ? 0.f : pow2(mu[e] - m);
+        l += mu[e] == kNegInf ? lu[e] : lu[e] * w;   // (a part without a finite score brings zero, or a NaN)
+#pragma unroll
+        for (int i = 0; i < kJoinStep; ++i) o[i] += w * x[e][i];
+      }
+  }
+  if (r >= rows || (unsigned)token >= (unsigned)a.tokens) return;
+  const bool none = s.last(a, ri) < s.first(a, ri);
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int i = 0; i < kJoinStep; ++i) {
+    const int ch = (first + i) * 8 + 4 * h;
+    uintx2 w = {pack2<T>(o[i][0] * inv, o[i][1] * inv), pack2<T>(o[i][2] * inv, o[i][3] * inv)};
+    if (none) w = (uintx2){0, 0};
+    if (ch < a.head_dim) *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)token * a.out_token + (long)head * a.head_dim + ch) = w;
+  }
+}
+
+int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+
+// A part has 256 keys at least, and a tile 32 parts at most: beyond that the join costs more than the shorter parts save (us, at least 256 / 512 / 1024
+// keys: 24 rows of 8 key heads over 4000 keys 17.6 / 20.4 / 29.8, over 30000 keys 50.9 / 50.8 / 44.2, which are 64 / 59 / 30 parts).
+constexpr int kLeastKeys = 256, kMostParts = 32;
+
+TilesPlan tiles_plan(const AttnArgs& a, bool share) {
+  const int dp = padded_dim(a.head_dim), keys = tile_keys(dp);
+  TilesPlan p;
+  p.groups = a.batch * a.kv_heads;
+  p.tiles = (int)(((long)a.max_q_len * a.group + kTileRows - 1) / kTileRows);
+  // steps of the longest tile
+  const long tokens = min((long)a.max_q_len, (long)kTileRows / a.group + 2), reach = a.causal && a.window > 0 ? a.window + tokens : a.max_kv_len;
+  const long longest = max(1L, (min(reach, (long)a.max_kv_len) + keys - 1) / keys + 1);
+  const long room = share ? min((long)kMostParts, 256L * workgroups_of_cu(dp) / max(1L, (long)p.groups * p.tiles)) : 1;
+  p.unit = (int)max((long)kLeastKeys / keys, (longest + max(room, 1L) - 1) / max(room, 1L));
+  p.parts = room > 1 ? (int)((longest + p.unit - 1) / p.unit) : 1;
+  return p;
+}
+
+// 16 keys of a step lie in one page, and a lane's offset within them in 31 bits
+bool one_page(const AttnArgs& a) { return a.page_size % 16 == 0 && a.slot_stride < 1 << 26; }
+
+template <typename T, int DP, bool PAGED>
+hipError_t launch_paged(const AttnArgs& a, hipStream_t st) {
+  const TilesPlan p = tiles_plan(a, a.workspace != nullptr);
+  const dim3 grid((unsigned)(p.groups * p.tiles * p.parts)), block(kTileWaves * 64);
+  if (a.head_dim == DP) hipLaunchKernelGGL((attn_tiles_kernel<T, DP, true, PAGED>), grid, block, 0, st, a, p);
+  else hipLaunchKernelGGL((attn_tiles_kernel<T, DP, false, PAGED>), grid, block, 0, st, a, p);
+  if (p.parts > 1) {
+    const dim3 join((unsigned)(p.groups * p.tiles), DP / 8 / kJoinStep);
+    hipLaunchKernelGGL((attn_join_kernel<T, DP>), join, block, 0, st, a, p, PAGED ? 16 : 1);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, int DP>
 hipError_t launch_dim(const AttnArgs& a, hipStream_t st) {
-  const int groups = a.batch * a.kv_heads, tiles = (int)(((long)a.max_q_len * a.group + kTileRows - 1) / kTileRows);
-  const dim3 grid((unsigned)(groups * tiles)), block(kTileWaves * 64);
-  if (a.head_dim == DP) hipLaunchKernelGGL((attn_tiles_kernel<T, DP, true>), grid, block, 0, st, a, groups, tiles);
-  else hipLaunchKernelGGL((attn_tiles_kernel<T, DP, false>), grid, block, 0, st, a, groups, tiles);
-  return hipGetLastError();
+  return one_page(a) ? launch_paged<T, DP, true>(a, st) : launch_paged<T, DP, false>(a, st);
 }
 
 template <typename T>
@@ -293,6 +506,13 @@ hipError_t launch_type(const AttnArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+size_t attn_tiles_workspace_bytes(const AttnArgs& a) {
+  const TilesPlan p = tiles_plan(a, true);
+  if (p.parts == 1) return 0;
+  const int dp = padded_dim(a.head_dim);
+  return kCounterBytes + (size_t)p.groups * p.tiles * p.parts * (size_t)(kTileRows * dp + 2 * kTileRows) * 4;
+}
 
 hipError_t launch_attention_tiles(const AttnArgs& a, int dtype, hipStream_t st) {
   return dtype == T_F16 ? launch_type<_Float16>(a, st) : launch_type<__bf16>(a, st);
