@@ -112,7 +112,8 @@ typedef struct {
   int64_t page_stride, slot_stride, head_stride;    /* of k_cache and of v_cache */
 } relay_paged_attention_desc;
 
-/* The products, the softmax between them and the look-up of the pages as one launch (paper Section 4.1; intermediate results stay off memory).
+/* The products, the softmax between them and the look-up of the pages as one launch (paper Section 4.1; intermediate results stay off memory),
+ * with a second one behind it where more than 16 rows of a key head have their keys shared out.
  * Sequence b has the rows q_starts[b] .. q_starts[b+1]-1 of q (nq of them) as its newest tokens and kv_lens[b] keys in the cache, the new
  * tokens' own among them (relay_rope_append has stored them).  Its token i stands at position p = kv_lens[b] - nq + i and
  *   out = sum_j softmax_j(scale * q . k_j) v_j   over keys 0 <= j < kv_lens[b], j <= p if causal, j > p - window if window > 0
@@ -124,7 +125,7 @@ typedef struct {
  *   page_table int32 [batch][pages_per_seq]; q_starts int32 [batch+1], ascending; kv_lens int32 [batch]
  * All tensors 16-byte aligned, strides multiples of 16 bytes.  out must not overlap an input.
  * Where there are few rows and many keys, a sequence's keys are shared out over workgroups that leave partial sums in the
- * workspace; the last one to arrive joins them in a fixed order, so results do not depend on timing.  Workspace contract as of
+ * workspace; they are joined in a fixed order, so results do not depend on timing.  Workspace contract as of
  * relay_workspace_bytes: 256-byte aligned, at least relay_paged_attention_workspace_bytes(d), zero before its first use, left ready
  * for the next call of any descriptor that asks for no more; NULL is valid (no sharing out, slower). */
 relay_status relay_paged_attention_workspace_bytes(const relay_paged_attention_desc* d, size_t* bytes);
