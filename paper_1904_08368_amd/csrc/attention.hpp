@@ -97,6 +97,7 @@ struct W4Args {
   const void* res;
   void* y;
   int m, n, k, group, zeros, relu;
+  int wide;   // four neighbours of y, the residual and the bias can be read and written at once (launch_w4 finds out)
   int64_t x_stride, y_stride;
 };
 hipError_t launch_w4_pack(const W4Args& a, int dtype, const uint8_t* codes, const void* scales, const uint8_t* zeros, void* packed, hipStream_t st);

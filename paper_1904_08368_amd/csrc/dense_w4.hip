@@ -7,17 +7,17 @@
 //
 // Few rows of x: bound by the codes' bytes.  The waves of a workgroup share 16 units' rows out among them along the reduction, each
 // streams its part straight into the A operands (the packed order), and they add up through LDS.
+#include <type_traits>
+
 #include "attention.hpp"
 #include "lds_dma.hpp"
 
-#ifndef FW
-#define FW 8
-#endif
 namespace relay {
 namespace {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bfx8 __attribute__((ext_vector_type(8)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
@@ -58,6 +58,26 @@ __device__ __forceinline__ void finish(const W4Args& a, int m, int j, float v) {
   if (a.res) v += (float)static_cast<const T*>(a.res)[(long)m * a.y_stride + j];
   if (a.relu) v = v > 0.f ? v : 0.f;
   static_cast<T*>(a.y)[(long)m * a.y_stride + j] = (T)v;
+}
+
+// the tail of four units from j on
+template <typename T>
+__device__ __forceinline__ void finish4(const W4Args& a, int m, int j, floatx4 v) {
+  typedef T four __attribute__((ext_vector_type(4)));
+  if (!a.wide) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < a.n) finish<T>(a, m, j + e, v[e]);
+    return;
+  }
+  if (j >= a.n) return;
+  const long at = (long)m * a.y_stride + j;
+  if (a.bias) v += *reinterpret_cast<const floatx4*>(a.bias + j);
+  if (a.res) v += __builtin_convertvector(*reinterpret_cast<const four*>(static_cast<const T*>(a.res) + at), floatx4);
+  if (a.relu)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = v[e] > 0.f ? v[e] : 0.f;
+  *reinterpret_cast<four*>(static_cast<T*>(a.y) + at) = __builtin_convertvector(v, four);
 }
 
 // Up to MR rows (1 or 4): bound by the codes' bytes, and close behind by the memory pipe, which takes a 16-byte load of a wave in 16 clocks whatever its
@@ -259,9 +279,7 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
     for (int u = 0; u < W; ++u) v += reinterpret_cast<const floatx4*>(lds[u])[i];
     const int row = m0 + (which % RT) * 16 + (ln & 15), j0 = (tile0 + which / RT) * 16 + 4 * (ln >> 4);
     if (row >= a.m) continue;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j0 + e < a.n) finish<T>(a, row, j0 + e, v[e]);
+    finish4<T>(a, row, j0, v);
   }
 }
 
@@ -318,10 +336,13 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
         lds_dma16_at(to + (CP + (wave == 0 ? 0 : SP)) * 16, ps + (size_t)g0 * (wave == 0 ? 32 : 16));
     }
   };
+  // fp16 subtracts the zero points exactly, two to an instruction, and needs no sums of x; bf16 has no such instruction.
+  constexpr bool EXACT = std::is_same<T, _Float16>::value;
   const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
   const Widen<T> widen;
   const int halves = (a.k + 63) / 64;
-  floatx4 sum[4][4], acc[4][4], xsum[4];
+  floatx4 sum[4][4], acc[4][4], xsum[EXACT ? 1 : 4];
+  halfx2 zero[EXACT ? 4 : 1];   // -(16 + zero point) of this lane's unit of each tile, for the group at hand
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -348,6 +369,14 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
     }
   };
   const floatx4 none = {0, 0, 0, 0};
+  auto zeros_of = [&](int chunk, int s) {
+    const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
+    const unsigned char* const zp = reinterpret_cast<const unsigned char*>(&wl[chunk & 1][CP + SP + wu * 16 + gr]) + col;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      zero[t] = __builtin_bit_cast(halfx2, 0xc800c800u + zp[t * 64] * 0x00400040u);   // (n = 16 .. 31 is the half 0x4800 + 64 n)
+    }
+  };
   auto scales_of = [&](int chunk, int s, int t, float (&k)[4], float (&z)[4]) {
     const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
     const four sc = (reinterpret_cast<const four*>(&wl[chunk & 1][CP + wu * 32]) + g)[(t * 4 + gr) * 4];   // [tile][group][4 g ..]
@@ -366,21 +395,32 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], fmaf(z[e], xsum[r][e], acc[t][r][e]), sum[t][r][e]);
+        for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], EXACT ? acc[t][r][e] : fmaf(z[e], xsum[r][e], acc[t][r][e]), sum[t][r][e]);
     }
   };
   auto step = [&](int chunk, int s, bool fresh) {
     const uintx4* const xrow = &xl[slot][(wr * 64 + col) * 8];
     const unsigned* const cl = reinterpret_cast<const unsigned*>(&wl[chunk & 1][wu * 256 + lane]) + s;
     vec xb[4];
+    if constexpr (EXACT)
+      if (fresh) zeros_of(chunk, s);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       xb[r] = __builtin_bit_cast(vec, xrow[r * 128 + ((4 * (s & 1) + g) ^ (col >> 1))]);
-      xsum[r] = C::mfma(ones, xb[r], fresh ? none : xsum[r]);
+      if constexpr (!EXACT) xsum[r] = C::mfma(ones, xb[r], fresh ? none : xsum[r]);
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const vec wv = widen(cl[t * 256]);
+      vec wv = widen(cl[t * 256]);
+      if constexpr (EXACT) {
+        uintx4 u = __builtin_bit_cast(uintx4, wv);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned ue = u[e];
+          u[e] = __builtin_bit_cast(unsigned, __builtin_bit_cast(halfx2, ue) + zero[t]);
+        }
+        wv = __builtin_bit_cast(vec, u);
+      }
       if constexpr (FL == 1) {   // (a tile's sums are used up at once and take a fourth of the registers, which reads ahead of them would fill)
         __builtin_amdgcn_sched_barrier(0);
         floatx4 p[4];
@@ -391,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], fmaf(z[e], xsum[r][e], p[r][e]), sum[t][r][e]);
+          for (int r = 0; r < 4; ++r) sum[t][r][e] = fmaf(k[e], EXACT ? p[r][e] : fmaf(z[e], xsum[r][e], p[r][e]), sum[t][r][e]);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
@@ -419,12 +459,7 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
     const int row = m0 + wr * 64 + r * 16 + col;
     if (row >= a.m) continue;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int j0 = (tile0 + wu * 4 + t) * 16 + 4 * g;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (j0 + e < a.n) finish<T>(a, row, j0 + e, sum[t][r][e]);
-    }
+    for (int t = 0; t < 4; ++t) finish4<T>(a, row, (tile0 + wu * 4 + t) * 16 + 4 * g, sum[t][r]);
   }
 }
 
@@ -515,14 +550,17 @@ bool rows_pay(const W4Args& a, const W4Layout& l) {
 
 template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
-  if (a.m == 1) return launch_few<T, 1, FW>(a, l, st);
-  if (a.m <= 4) return launch_few<T, 4, FW>(a, l, st);
+  if (a.m == 1) return launch_few<T, 1, 8>(a, l, st);
+  if (a.m <= 4) return launch_few<T, 4, 8>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
   return rows_pay(a, l) ? launch_rows<T, 2, 2, 8, 1>(a, l, st) : launch_tiles<T>(a, l, st);
 }
 }  // namespace
 
-hipError_t launch_w4(const W4Args& a, int dtype, hipStream_t st) {
+hipError_t launch_w4(const W4Args& args, int dtype, hipStream_t st) {
+  W4Args a = args;
+  a.wide = a.n % 4 == 0 && a.y_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.res)) % 8 == 0 &&
+           reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   const W4Layout l = w4_layout(a.n, a.k, a.group, a.zeros != 0);
   return dtype == T_F16 ? launch_type<_Float16>(a, l, st) : launch_type<__bf16>(a, l, st);
 }
