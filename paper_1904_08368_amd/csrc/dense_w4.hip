@@ -287,17 +287,22 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
 // memory and two halves of a chunk ahead (64 of the reduction each, one barrier to each): x in a ring of three halves, so that two workgroups fit a CU; codes,
 // scales and zero points, which two waves share, in two buffers of a chunk.  A word of codes is widened once for four matrix instructions.  The sums of a group and
 // those of all groups are both kept in registers, 64 each.  blockIdx.x runs over the units: workgroups that share rows of x follow each other.
+// PARTS 2: eight waves, of which four and four share the reduction out, for launches of so few tiles that a CU has one.
 // FL as above.
-template <typename T, int FL>
-__global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
+template <typename T, int FL, int PARTS>
+__global__ __launch_bounds__(256 * PARTS, 2) void w4_tiles_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
   typedef W4Type<T> C;
   typedef typename C::vec vec;
   typedef T four __attribute__((ext_vector_type(4)));
   constexpr int ROWS = 128, TILES = 8, XP = ROWS * 8, CP = TILES * 64, SP = TILES * 8, ZP = TILES * 4;   // 16-byte pieces of a buffer
   constexpr int RING = 3;   // halves of x on their way or in use
-  __shared__ __attribute__((aligned(16))) uintx4 xl[RING][XP], wl[2][CP + SP + ZP];
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  constexpr int XB = RING * XP, WB = CP + SP + ZP, BUF = XB + 2 * WB;
+  __shared__ __attribute__((aligned(16))) uintx4 buffers[PARTS][BUF];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) & 3;
+  const int part = PARTS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8) : 0;
   const int wu = wave & 1, wr = wave >> 1;
+  uintx4* const xl = buffers[part];        // [RING][XP]
+  uintx4* const wl = buffers[part] + XB;   // [2][WB]
   const int g = lane >> 4, col = lane & 15;
   const int tile0 = (int)blockIdx.x * TILES, m0 = (int)blockIdx.y * ROWS;
   const char* base = static_cast<const char*>(a.packed);
@@ -319,15 +324,19 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
   const bool pwanted = wave == 0 || (wave == 1 && a.zeros && lane < ZP);
   const char* const ps = wave == 0 ? base + l.scales_at + ((size_t)min(tile0 + ptile, l.tiles - 1) * l.groups * 2 + piece) * 16
                                    : base + l.zeros_at + ((size_t)min(tile0 + (ptile & 7), l.tiles - 1) * l.groups + piece) * 16;
-  const unsigned x_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&xl[0][0];
-  const unsigned w_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&wl[0][0];
+  const unsigned x_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&buffers[0][0] + (unsigned)(part * BUF * 16);
+  const unsigned w_at = x_at + XB * 16;
   auto copy_x = [&](int half, int slot) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (half * 64 + xk[i] < a.k) lds_dma16_at(x_at + (unsigned)(slot * XP * 16 + (wave * 4 + i) * 1024), xs[i] + (long)half * 64);
+    if (half * 64 + 64 > a.k)   // pieces that lie behind k: zeros
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (half * 64 + xk[i] >= a.k) xl[slot * XP + (wave * 4 + i) * 64 + lane] = (uintx4){0, 0, 0, 0};
   };
   auto copy_w = [&](int chunk) {
-    const unsigned to = w_at + (unsigned)((chunk & 1) * (int)sizeof(wl[0]));
+    const unsigned to = w_at + (unsigned)((chunk & 1) * WB * 16);
 #pragma unroll
     for (int i = 0; i < 2; ++i) lds_dma16_at(to + (unsigned)(wave * 2 + i) * 1024u, ws[i] + (size_t)chunk * 1024);
     if (wave < 2) {
@@ -340,38 +349,36 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
   constexpr bool EXACT = std::is_same<T, _Float16>::value;
   const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
   const Widen<T> widen;
-  const int halves = (a.k + 63) / 64;
+  // this part's chunks first .. last - 1, `turns` at most; its halves end with end - 1
+  const int turns = (l.chunks + PARTS - 1) / PARTS, first = part * turns, last = min(l.chunks, first + turns), end = min((a.k + 63) / 64, 2 * last);
   floatx4 sum[4][4], acc[4][4], xsum[EXACT ? 1 : 4];
   halfx2 zero[EXACT ? 4 : 1];   // -(16 + zero point) of this lane's unit of each tile, for the group at hand
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int t = 0; t < 4; ++t) sum[t][r] = (floatx4){0, 0, 0, 0};
-  if (!a.zeros && lane < ZP) wl[wave & 1][CP + SP + lane] = (uintx4){0x18181818u, 0x18181818u, 0x18181818u, 0x18181818u};   // (16 + 8, to stay)
-  copy_x(0, 0);
-  copy_w(0);
-  if (halves > 1) copy_x(1, 1);
+  if (!a.zeros && lane < ZP) wl[(wave & 1) * WB + CP + SP + lane] = (uintx4){0x18181818u, 0x18181818u, 0x18181818u, 0x18181818u};   // (16 + 8, to stay)
+  if (PARTS == 1 || first < last) {
+    copy_x(2 * first, 0);
+    copy_w(first);
+    if (2 * first + 1 < end) copy_x(2 * first + 1, 1);
+  }
   // Half `half` has arrived, all waves' copies of it, and no wave reads the buffers any more that are filled next.  A wave's copies return in order: behind
   // those of this half it has asked for the next half of x (four) and, since an even half, for a chunk's codes (two and, wave 0, the scales).
   int slot = 0;   // of the half at hand in the ring
   auto arrive = [&](int half, bool odd) {
-    if (half + 2 >= halves) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (half + 2 >= end) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     else if (!odd) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
     else if (wave) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(7) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (half + 2 < halves) copy_x(half + 2, slot == 0 ? 2 : slot - 1);
-    if (half + 1 == halves && halves * 64 > a.k) {   // pieces that lie behind k are not copied: zeros
-      for (int i = (int)threadIdx.x; i < XP; i += 256)
-        if (half * 64 + ((i & 7) ^ ((i >> 4) & 7)) * 8 >= a.k) xl[slot][i] = (uintx4){0, 0, 0, 0};
-      __syncthreads();
-    }
+    if (half + 2 < end) copy_x(half + 2, slot == 0 ? 2 : slot - 1);
   };
   const floatx4 none = {0, 0, 0, 0};
   auto zeros_of = [&](int chunk, int s) {
     const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
-    const unsigned char* const zp = reinterpret_cast<const unsigned char*>(&wl[chunk & 1][CP + SP + wu * 16 + gr]) + col;
+    const unsigned char* const zp = reinterpret_cast<const unsigned char*>(&wl[(chunk & 1) * WB + CP + SP + wu * 16 + gr]) + col;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       zero[t] = __builtin_bit_cast(halfx2, 0xc800c800u + zp[t * 64] * 0x00400040u);   // (n = 16 .. 31 is the half 0x4800 + 64 n)
@@ -379,8 +386,8 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
   };
   auto scales_of = [&](int chunk, int s, int t, float (&k)[4], float (&z)[4]) {
     const int gr = min((int)fast_div((unsigned)(chunk * 4 + s), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
-    const four sc = (reinterpret_cast<const four*>(&wl[chunk & 1][CP + wu * 32]) + g)[(t * 4 + gr) * 4];   // [tile][group][4 g ..]
-    const unsigned zp = (reinterpret_cast<const unsigned*>(&wl[chunk & 1][CP + SP + wu * 16]) + g)[(t * 4 + gr) * 4];
+    const four sc = (reinterpret_cast<const four*>(&wl[(chunk & 1) * WB + CP + wu * 32]) + g)[(t * 4 + gr) * 4];   // [tile][group][4 g ..]
+    const unsigned zp = (reinterpret_cast<const unsigned*>(&wl[(chunk & 1) * WB + CP + SP + wu * 16]) + g)[(t * 4 + gr) * 4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       k[e] = (float)sc[e];
@@ -399,8 +406,8 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
     }
   };
   auto step = [&](int chunk, int s, bool fresh) {
-    const uintx4* const xrow = &xl[slot][(wr * 64 + col) * 8];
-    const unsigned* const cl = reinterpret_cast<const unsigned*>(&wl[chunk & 1][wu * 256 + lane]) + s;
+    const uintx4* const xrow = &xl[slot * XP + (wr * 64 + col) * 8];
+    const unsigned* const cl = reinterpret_cast<const unsigned*>(&wl[(chunk & 1) * WB + wu * 256 + lane]) + s;
     vec xb[4];
     if constexpr (EXACT)
       if (fresh) zeros_of(chunk, s);
@@ -438,21 +445,36 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(const W4Args a, const 
       }
     }
   };
-  for (int chunk = 0; chunk < l.chunks; ++chunk) {
+  for (int turn = 0; turn < turns; ++turn) {   // (the same for all waves: each has to meet every barrier)
+    const int chunk = first + turn;
     arrive(2 * chunk, false);
-    if (chunk + 1 < l.chunks) copy_w(chunk + 1);
-    step(chunk, 0, true);
-    step(chunk, 1, FL == 1);
-    if (FL == 2) apply(chunk, 1);
-    slot = slot == 2 ? 0 : slot + 1;
-    if (2 * chunk + 1 < halves) {
-      arrive(2 * chunk + 1, true);
+    if (PARTS == 1 || chunk < last) {
+      if (chunk + 1 < last) copy_w(chunk + 1);
+      step(chunk, 0, true);
+      step(chunk, 1, FL == 1);
+      if (FL == 2) apply(chunk, 1);
+      slot = slot == 2 ? 0 : slot + 1;
+    }
+    if (PARTS > 1 || 2 * chunk + 1 < end) arrive(2 * chunk + 1, true);
+    if (2 * chunk + 1 < end) {
       step(chunk, 2, FL <= 2);
       step(chunk, 3, FL == 1);
       if (FL == 2) apply(chunk, 3);
       slot = slot == 2 ? 0 : slot + 1;
     }
-    if (FL == 4) apply(chunk, 0);
+    if (FL == 4 && (PARTS == 1 || chunk < last)) apply(chunk, 0);
+  }
+  if constexpr (PARTS > 1) {
+    floatx4* const other = reinterpret_cast<floatx4*>(&buffers[0][0]) + ((int)threadIdx.x & 255);
+    static_assert(PARTS == 2 && sizeof(buffers) >= 16 * 256 * 16, "the second part's sums");
+    __syncthreads();
+    if (part)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) other[i * 256] = sum[i / 4][i % 4];
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i / 4][i % 4] += other[i * 256];
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -527,24 +549,26 @@ hipError_t launch_rows(const W4Args& a, const W4Layout& l, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, int PARTS>
 hipError_t launch_tiles(const W4Args& a, const W4Layout& l, hipStream_t st) {
   const int per_group = a.group / 32;
   const FastDiv fd = make_fastdiv((uint32_t)per_group);
-  const dim3 grid((unsigned)((l.tiles + 7) / 8), (unsigned)((a.m + 127) / 128)), block(256);
-  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 4>), grid, block, 0, st, a, l, fd);
-  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 2>), grid, block, 0, st, a, l, fd);
-  else hipLaunchKernelGGL((w4_tiles_kernel<T, 1>), grid, block, 0, st, a, l, fd);
+  const dim3 grid((unsigned)((l.tiles + 7) / 8), (unsigned)((a.m + 127) / 128)), block(256 * PARTS);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 4, PARTS>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_tiles_kernel<T, 2, PARTS>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((w4_tiles_kernel<T, 1, PARTS>), grid, block, 0, st, a, l, fd);
   return hipGetLastError();
 }
 
-// More than 16 rows: 32 at a time on the kernel whose waves share the reduction out, or as tiles of 128 x 128, each of which walks the whole reduction:
-// 1.85 us a chunk where a CU has one of them, 2.6 where it has two.  The other kernel takes 2.5 us and 0.73 ns a workgroup and chunk.  Measured, rows / tiles,
-// us, groups of 128: 8192 units by 8192, 64 rows 26 / 116, 128 rows 49 / 118, 256 rows 94 / 119; 4096 x 4096, 300 rows 33 / 63; 28000 x 4096, 64 rows
-// 48 / 63; 1500 x 2000 in groups of 64, 200 rows 11 / 39.
+// More than 16 rows: 32 at a time on the kernel whose waves share the reduction out, or as tiles of 128 x 128, each of which walks the whole reduction: where
+// a CU has one of them at most, in two parts at 4 us and 1.25 us a chunk (in one part 1.7 us a chunk), where it has two, 2.35 us a chunk. The other kernel
+// takes 2.5 us and 0.67 ns a workgroup and chunk. Measured, rows / tiles, us, groups of 128: 8192 units by 8192, 64 rows 25 / 82, 128 rows 48 / 82, 256 rows
+// 90 / 83, 512 rows 178 / 85; 4096 x 4096, 300 rows 31 / 44; 28000 x 4096, 64 rows 46 / 45; 1500 x 2000 in groups of 64, 200 rows 10 / 26.
+long tiles_of(const W4Args& a, const W4Layout& l) { return ((l.tiles + 7L) / 8) * ((a.m + 127) / 128); }
 bool rows_pay(const W4Args& a, const W4Layout& l) {
-  const long tiles = ((l.tiles + 7L) / 8) * ((a.m + 127) / 128), rows = ((l.tiles + 1L) / 2) * ((a.m + 31) / 32);
-  const double t_tiles = l.chunks * (tiles <= 256 ? 1.85 : 2.6 * (double)((tiles + 511) / 512)), t_rows = 2.5 + 0.73e-3 * (double)rows * l.chunks;
+  const long tiles = tiles_of(a, l), rows = ((l.tiles + 1L) / 2) * ((a.m + 31) / 32);
+  const double t_tiles = tiles <= 256 ? 4 + 1.25 * l.chunks : 2.35 * l.chunks * (double)((tiles + 511) / 512);
+  const double t_rows = 2.5 + 0.67e-3 * (double)rows * l.chunks;
   return t_rows < t_tiles;
 }
 
@@ -553,7 +577,8 @@ hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
   if (a.m == 1) return launch_few<T, 1, 8>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, 8>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
-  return rows_pay(a, l) ? launch_rows<T, 2, 2, 8, 1>(a, l, st) : launch_tiles<T>(a, l, st);
+  if (rows_pay(a, l)) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
+  return tiles_of(a, l) <= 256 ? launch_tiles<T, 2>(a, l, st) : launch_tiles<T, 1>(a, l, st);
 }
 }  // namespace
 
