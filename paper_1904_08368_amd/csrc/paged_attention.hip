@@ -504,15 +504,21 @@ RowsGrid rows_plan(const AttnArgs& a, bool share) {
   const long tiles = (long)a.batch * a.kv_heads;
   // the most keys between the first and the last that a sequence's rows see
   const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
-  // Eight waves where their registers leave a CU room for them, four where rounds of theirs do not even give half of the CUs one: less to launch
-  // and to join (us, four / eight waves: one sequence of 700 keys, 8 key heads 12.0 / 14.9, 1500 keys 12.7 / 15.4; 8 sequences of 3000 keys 36.7 / 32.7).
-  p.waves = dp > 128 || tiles * ((keys + 4 * kBlock - 1) / (4 * kBlock)) <= most_pieces(dp, 4) ? 4 : 8;
+  // Keys are shared out where there are more than eight waves take at once, unless there are tiles for three workgroups out of four and no sequence is long: then
+  // finding the shares and joining costs more than it evens out (us, shared out / a workgroup to a tile: one sequence of 200 keys, 8 key heads 11.6 / 8.6;
+  // 24 of up to 1500 33.2 / 28.7, 16 of them 22.9 / 27.5; 200 of up to 900, 4 key heads 72 / 55, 128 of up to 4000 131 / 146).
+  p.plan.deal = share && tiles <= kCounters && keys > 8 * kBlock && (tiles < kMostPieces * 3 / 4 || keys > 64 * kBlock);
+  // Eight waves where their registers leave a CU room for them.  Four where rounds of theirs do not even give half of the CUs one: less to launch
+  // and to join (us, four / eight waves: one sequence of 700 keys, 8 key heads 11.8 / 14.5, 1500 keys 12.0 / 14.8; 8 sequences of 3000 keys 35.9 / 23.4).
+  // Four, too, where every CU gets two tiles or more: one's end runs beside the other's stream (200 sequences of up to 900 keys, 4 key heads 54.5 / 58.6).
+  const bool four = p.plan.deal ? tiles * ((keys + 4 * kBlock - 1) / (4 * kBlock)) <= most_pieces(dp, 4) : tiles >= 2 * kMostPieces;
+  p.waves = dp > 128 || four ? 4 : 8;
   const int round = p.waves * kBlock;
   // A unit is a round of the waves; where there are more of those than workgroups, a quarter of one, so that their shares come out more even
-  // (one sequence of 100001 keys, 4 key heads: 1564 rounds are seven to a workgroup, 6251 quarters 25).
+  // (48 sequences of up to 8192 keys, 8 key heads: 211 us, of whole rounds 213; 100 of up to 2000, 2 key heads 40.1 and 41.3).
   p.plan.unit = tiles * ((keys + round - 1) / round) > kMostPieces ? round / 4 : round;
-  const long units = max(1L, (keys + p.plan.unit - 1) / p.plan.unit);
-  p.plan.deal = share && tiles <= kCounters && units > 1 && tiles * units < 1L << 30;
+  const long units = (keys + p.plan.unit - 1) / p.plan.unit;
+  if (tiles * units >= 1L << 30) p.plan.deal = 0;
   if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)most_pieces(dp, p.waves)));
   else p.grid = dim3((unsigned)a.kv_heads, (unsigned)a.batch);
   return p;

@@ -71,13 +71,15 @@ def test_infinite_values_everywhere(B, workspace, ps):
 @pytest.mark.parametrize("lens,hq,hkv", [([(1, 40 + 7 * i) for i in range(70)], 4, 4),           # more tiles than workgroups
                                          ([(1, 3000)] * 2 + [(1, 5)] * 70 + [(2, 900)], 2, 1),   # more sequences than lanes
                                          ([(1, 2000), (0, 50), (1, 1), (4, 700), (1, 0)], 4, 1),
-                                         ([(1, 33 * i) for i in range(1, 64)], 8, 4)])
+                                         ([(1, 33 * i) for i in range(1, 64)], 8, 4),
+                                         ([(1, 30 + 7 * i) for i in range(70)] + [(1, 2100), (2, 64)], 4, 4),
+                                         ([(1, 100)] * 40 + [(1, 2300)] + [(3, 200)] * 40, 6, 3)])
 @pytest.mark.parametrize("dim", [64, 136])
 def test_sequences_in_one_line(B, lens, hq, hkv, dim):
     c = _case("bf16", lens, hq, hkv, dim, 16)
     _both(B, c)
     got, s = _run(B, c)
-    assert s["ws"].numel() > 0
+    assert s["ws"].numel() > 0 or c["max_kv"] <= 2048   # (many short sequences are not shared out)
     first = got.clone()
     for _ in range(3):
         got.fill_(7)
