@@ -464,6 +464,7 @@ int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 25
 
 // A part has 256 keys at least, and a tile 32 parts at most: beyond that the join costs more than the shorter parts save (us, at least 256 / 512 / 1024
 // keys: 24 rows of 8 key heads over 4000 keys 17.6 / 20.4 / 29.8, over 30000 keys 50.9 / 50.8 / 44.2, which are 64 / 59 / 30 parts).
+// All parts of a launch find room on the chip at once (as many, or half as many more: 512 tokens over 30000 keys 269 / 309, chunks of 509 tokens over 9001 45 / 47).
 constexpr int kLeastKeys = 256, kMostParts = 32;
 
 TilesPlan tiles_plan(const AttnArgs& a, bool share) {
