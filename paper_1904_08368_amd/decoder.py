@@ -67,11 +67,12 @@ class Step:
         self.per_seq = -(-max_kv_len // cache.page_size)
         device = cache.k.device
 
-        def ints(*shape):
-            return torch.zeros(shape, dtype=torch.int32, device=device)
+        def ints(*shape, value=0):
+            return torch.full(shape, value, dtype=torch.int32, device=device)
 
-        self.page_table, self.q_starts, self.kv_lens = ints(batch, self.per_seq), ints(batch + 1), ints(batch)
-        self.positions, self.slots = ints(tokens), ints(tokens)
+        # (no tokens yet: run before the first extend(), say to warm up before a capture, a step stores nothing)
+        self.page_table, self.q_starts, self.kv_lens = ints(batch, self.per_seq, value=-1), ints(batch + 1), ints(batch)
+        self.positions, self.slots = ints(tokens), ints(tokens, value=-1)
 
     def extend(self, seqs: Sequence[int], new: Sequence[int]) -> None:
         """new[b] more tokens of sequence seqs[b], in this order in the rows of the layers' input; rows behind the last are padding."""
