@@ -127,14 +127,26 @@ def quantize4(w: torch.Tensor, group: int):
 
 
 class Workspace:
-    """Scratch that grows to the largest call; for calls that follow each other on one stream."""
+    """Scratch that grows to the largest call; for calls that follow each other on one stream.
+
+    A captured step holds the address of the buffer it was captured with, so a buffer that a larger one has replaced stays alive as long as the
+    workspace (each is at least twice as large as the one before: together they are below two of the last).  A call that needs more while
+    a graph is captured gets scratch of the graph's own, cleared on every replay: the fill that clears a buffer is only recorded then, and calls outside
+    of the graph would find whatever the memory held before.  Run a step once before it is captured, and it needs none."""
 
     def __init__(self):
         self.buffer: Optional[torch.Tensor] = None
+        self._outgrown: List[torch.Tensor] = []
 
     def of(self, nbytes: int, device) -> Optional[torch.Tensor]:
-        if nbytes and (self.buffer is None or self.buffer.numel() < nbytes):
-            self.buffer = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if not nbytes or (self.buffer is not None and self.buffer.numel() >= nbytes):
+            return self.buffer
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if self.buffer is not None:
+            self._outgrown.append(self.buffer)
+            nbytes = max(nbytes, 2 * self.buffer.numel())
+        self.buffer = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         return self.buffer
 
 
