@@ -117,8 +117,8 @@ typedef struct {
  * Sequence b has the rows q_starts[b] .. q_starts[b+1]-1 of q (nq of them) as its newest tokens and kv_lens[b] keys in the cache, the new
  * tokens' own among them (relay_rope_append has stored them).  Its token i stands at position p = kv_lens[b] - nq + i and
  *   out = sum_j softmax_j(scale * q . k_j) v_j   over keys 0 <= j < kv_lens[b], j <= p if causal, j > p - window if window > 0
- * Key j lies in slot j % page_size of page page_table[b][j / page_size].  A token that sees no key gets zeros.  Keys that a
- * token does not see do not reach its result, whatever they hold (infinities and NaN included).  Scores, the softmax and the sums
+ * Key j lies in slot j % page_size of page page_table[b][j / page_size].  A token that sees no key gets zeros (and so does one whose scores
+ * are all -infinity).  Keys that a token does not see do not reach its result, whatever they hold (infinities and NaN included).  Scores, the softmax and the sums
  * are fp32; the probabilities are rounded to the tensor's type for the product with v, whose sums are fp32.
  * A page number outside 0 .. num_pages-1, or a key past pages_per_seq pages, is not read: such keys count as unseen.
  *   q, out [tokens][q_heads][head_dim] with the token strides given; k_cache, v_cache, strides as relay_rope_append

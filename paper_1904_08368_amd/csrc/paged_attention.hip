@@ -385,10 +385,9 @@ __global__ __launch_bounds__(W * 64, DP <= 128 ? 2 : 1) void attn_rows_kernel(co
       const int ii = (int)fast_div((unsigned)cc, a.fd_group);
       const int tk = s.start + ii;
       if ((unsigned)tk >= (unsigned)a.tokens) return;
-      const bool none = s.last(a, ii) < s.first(a, ii);
       const float inv = 1.f / lt;
       uintx2 w = {pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
-      if (none) w = (uintx2){0, 0};
+      if (lt == 0.f) w = (uintx2){0, 0};   // (no key that is seen and can be read)
       *reinterpret_cast<uintx2*>(static_cast<T*>(a.out) + (long)tk * a.out_token + (long)(hk * a.group + cc - ii * a.group) * D + d) = w;
     };
     for (int it = tid_c; it < rows * (DP / 4); it += W * 64) {

@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_ti
     return;
   }
   if (!row_ok) return;
-  const bool none = my_last < my_first;
+  const bool none = l == 0.f;   // no key that is seen and can be read
   const float inv = 1.f / l;
   T* const out = static_cast<T*>(a.out) + (long)token * a.out_token + (long)head * D;
 #pragma unroll
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void attn_join_kernel(const AttnAr
       }
   }
   if (r >= rows || (unsigned)token >= (unsigned)a.tokens) return;
-  const bool none = s.last(a, ri) < s.first(a, ri);
+  const bool none = l == 0.f;
   const float inv = 1.f / l;
 #pragma unroll
   for (int i = 0; i < kJoinStep; ++i) {
