@@ -104,7 +104,7 @@ typedef struct {
   int32_t head_dim;           /* a multiple of 8, 8 .. 256 */
   int32_t num_pages, page_size, pages_per_seq;
   int32_t max_q_len;          /* no sequence has more new tokens, */
-  int32_t max_kv_len;         /* ... nor more keys, than this: the launch is sized by them, what lies beyond is not computed */
+  int32_t max_kv_len;         /* ... nor more keys, than this: the launch is sized by them, tokens beyond are not computed, keys beyond not seen */
   int32_t causal;             /* 1: a token sees no key behind its own position */
   int32_t window;             /* > 0: only the last `window` keys up to its own position; 0: all */
   float scale;

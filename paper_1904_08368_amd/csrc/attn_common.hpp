@@ -90,17 +90,21 @@ __device__ __forceinline__ unsigned only_finite(unsigned w) {
 constexpr int kCounters = 1024;
 constexpr size_t kCounterBytes = (size_t)kCounters * 64;
 
-// One sequence as a workgroup sees it.
+// One sequence as a workgroup sees it.  Its tokens' positions go by its true length; keys past the table's pages, or past the bound that the launch
+// was sized by, are not there to be seen.
 struct Seq {
-  int start, nq, kv;   // first row of q; new tokens; keys
+  int start, nq, kv;   // first row of q; new tokens; keys that can be read
+  int before;          // keys ahead of the first new token: its position
   __device__ Seq(const AttnArgs& a, int b) {
     start = a.q_starts[b];
     nq = a.q_starts[b + 1] - start;
-    kv = min(max(a.kv_lens[b], 0), a.max_kv_len);
+    const int length = max(a.kv_lens[b], 0);
+    kv = min(length, a.max_kv_len);
+    before = length - nq;
   }
   // keys that token i sees: first, last (none if last < first)
-  __device__ int first(const AttnArgs& a, int i) const { return a.window > 0 ? max(0, kv - nq + i - a.window + 1) : 0; }
-  __device__ int last(const AttnArgs& a, int i) const { return a.causal ? min(kv - 1, kv - nq + i) : kv - 1; }
+  __device__ int first(const AttnArgs& a, int i) const { return a.window > 0 ? min(kv, max(0, before + i - a.window + 1)) : 0; }
+  __device__ int last(const AttnArgs& a, int i) const { return a.causal ? min(kv - 1, before + i) : kv - 1; }
 };
 
 }  // namespace relay
