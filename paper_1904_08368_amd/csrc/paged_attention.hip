@@ -12,6 +12,7 @@
 // joins them in the order of the line.
 // Measured (key heads of 128 channels): 48 sequences of up to 8192 keys, 8 key heads, bf16, 211 us = 5.1 TB/s; one of 100001 keys, 4 key heads, fp16, 54 us, of which it streams
 // 33 at 6 TB/s; one of 700 keys 11.8 us, of 200 8.7: a launch is 5, the rest one trip to memory after another.
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -499,12 +500,13 @@ struct RowsGrid {
   int waves;
 };
 
+// (std::min: the unqualified one takes ints on the host, and a window may be up to 2^31 - 1)
 RowsGrid rows_plan(const AttnArgs& a, bool share) {
   RowsGrid p;
   const int dp = padded_dim(a.head_dim);
   const long tiles = (long)a.batch * a.kv_heads;
   // the most keys between the first and the last that a sequence's rows see
-  const long keys = a.window > 0 && a.causal ? min((long)a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
+  const long keys = a.window > 0 && a.causal ? std::min<long>(a.max_kv_len, (long)a.window + a.max_q_len) : a.max_kv_len;
   // Keys are shared out where there are more than eight waves take at once, unless there are tiles for three workgroups out of four and no sequence is long: then
   // finding the shares and joining costs more than it evens out (us, shared out / a workgroup to a tile: one sequence of 200 keys, 8 key heads 11.6 / 8.6;
   // 24 of up to 1500 33.2 / 28.7, 16 of them 22.9 / 27.5; 200 of up to 900, 4 key heads 72 / 55, 128 of up to 4000 131 / 146).
@@ -520,7 +522,7 @@ RowsGrid rows_plan(const AttnArgs& a, bool share) {
   p.plan.unit = tiles * ((keys + round - 1) / round) > kMostPieces ? round / 4 : round;
   const long units = (keys + p.plan.unit - 1) / p.plan.unit;
   if (tiles * units >= 1L << 30) p.plan.deal = 0;
-  if (p.plan.deal) p.grid = dim3((unsigned)min(tiles * units, (long)most_pieces(dp, p.waves)));
+  if (p.plan.deal) p.grid = dim3((unsigned)std::min<long>(tiles * units, most_pieces(dp, p.waves)));
   else p.grid = dim3((unsigned)a.kv_heads, (unsigned)a.batch);
   return p;
 }

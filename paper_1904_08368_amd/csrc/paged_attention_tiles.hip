@@ -5,6 +5,7 @@
 // instructions: on a step a wave does 32 products of 32 x 32 x 16 (head_dim 128) in 1024 clocks, and 2048 exponentials and what belongs to them in 900.  Two workgroups
 // share a CU, so that one's softmax runs beside the other's products.  Where there are few tiles their keys are cut into parts, and a second
 // kernel joins them.  Measured: 8192 tokens, 16 heads over 4 key heads, fp16, 290 us = 940 TFLOP/s; 512 tokens over 30000 keys, 32 over 8, 264 us; 64 tokens over them 55 us.
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -467,16 +468,17 @@ int padded_dim(int d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 25
 // All parts of a launch find room on the chip at once (as many, or half as many more: 512 tokens over 30000 keys 269 / 309, chunks of 509 tokens over 9001 45 / 47).
 constexpr int kLeastKeys = 256, kMostParts = 32;
 
+// (std::min and std::max: the unqualified ones take ints on the host, and a window may be up to 2^31 - 1)
 TilesPlan tiles_plan(const AttnArgs& a, bool share) {
   const int dp = padded_dim(a.head_dim), keys = tile_keys(dp);
   TilesPlan p;
   p.groups = a.batch * a.kv_heads;
   p.tiles = (int)(((long)a.max_q_len * a.group + kTileRows - 1) / kTileRows);
   // steps of the longest tile
-  const long tokens = min((long)a.max_q_len, (long)kTileRows / a.group + 2), reach = a.causal && a.window > 0 ? a.window + tokens : a.max_kv_len;
-  const long longest = max(1L, (min(reach, (long)a.max_kv_len) + keys - 1) / keys + 1);
-  const long room = share ? min((long)kMostParts, 256L * workgroups_of_cu(dp) / max(1L, (long)p.groups * p.tiles)) : 1;
-  p.unit = (int)max((long)kLeastKeys / keys, (longest + max(room, 1L) - 1) / max(room, 1L));
+  const long tokens = std::min<long>(a.max_q_len, (long)kTileRows / a.group + 2), reach = a.causal && a.window > 0 ? a.window + tokens : a.max_kv_len;
+  const long longest = std::max<long>(1, (std::min<long>(reach, a.max_kv_len) + keys - 1) / keys + 1);
+  const long room = share ? std::max<long>(1, std::min<long>(kMostParts, 256L * workgroups_of_cu(dp) / std::max<long>(1, (long)p.groups * p.tiles))) : 1;
+  p.unit = (int)std::max<long>(kLeastKeys / keys, (longest + room - 1) / room);
   p.parts = room > 1 ? (int)((longest + p.unit - 1) / p.unit) : 1;
   return p;
 }
