@@ -102,8 +102,8 @@ struct Seq {
     kv = min(length, a.max_kv_len);
     before = length - nq;
   }
-  // keys that token i sees: first, last (none if last < first)
-  __device__ int first(const AttnArgs& a, int i) const { return a.window > 0 ? min(kv, max(0, before + i - a.window + 1)) : 0; }
+  // keys that token i sees: first, last (none if last < first).  (A window of up to 2^31 - 1 behind a token ahead of the first key: 64 bits.)
+  __device__ int first(const AttnArgs& a, int i) const { return a.window > 0 ? (int)min((long)kv, max(0L, (long)before + i - a.window + 1)) : 0; }
   __device__ int last(const AttnArgs& a, int i) const { return a.causal ? min(kv - 1, before + i) : kv - 1; }
 };
 
