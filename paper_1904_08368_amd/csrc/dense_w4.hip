@@ -51,6 +51,30 @@ struct Widen {
   }
 };
 
+// One sum from the weights themselves, code by code.  Where it is taken: an infinity among x, or values whose sums with the numbers 16 + code leave fp32's range,
+// make the two sides of the formula above infinite, and their difference a NaN whatever the weights are.  Such sums, and no others, are not finite, and are
+// formed again before the tail; what is read is small beside a launch unless most of x is such values, and one NaN ends it.
+template <typename T>
+__device__ __forceinline__ float sum_by_weights(const W4Args& a, const W4Layout& l, int m, int j) {
+  const unsigned char* const base = static_cast<const unsigned char*>(a.packed);
+  const unsigned* const codes = reinterpret_cast<const unsigned*>(base) + ((size_t)(j >> 4) * l.chunks * 64 + (j & 15)) * 4;
+  const size_t params = (size_t)(j >> 4) * l.groups * 16 + (j & 15);
+  const T* const x = static_cast<const T*>(a.x) + (long)m * a.x_stride;
+  float sum = 0.f;
+  for (int g = 0; g < l.groups && sum == sum; ++g) {
+    const float scale = (float)reinterpret_cast<const T*>(base + l.scales_at)[params + (size_t)g * 16];
+    const int zero = a.zeros ? base[l.zeros_at + params + (size_t)g * 16] - 16 : 8, end = min(a.k - g * a.group, a.group) + g * a.group;
+    for (int i = g * a.group; i < end; i += 8) {   // (a word of the packed order: chunk i / 128, step of 32, quarter of 8)
+      const unsigned w = __builtin_rotateright32(codes[((size_t)(i >> 7) * 64 + 16 * (i >> 3 & 3)) * 4 + (i >> 5 & 3)], W4Type<T>::kAt);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)x[i + e], (float)((int)(w >> (16 * (e & 1) + 4 * (e >> 1)) & 15u) - zero) * scale, sum);
+    }
+  }
+  return sum;
+}
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) < __builtin_inff(); }
+__device__ __forceinline__ bool is_finite(floatx4 v) { return is_finite(v[0]) && is_finite(v[1]) && is_finite(v[2]) && is_finite(v[3]); }
+
 // the tail of one output
 template <typename T>
 __device__ __forceinline__ void finish(const W4Args& a, int m, int j, float v) {
@@ -160,6 +184,7 @@ __global__ __launch_bounds__(W * 64) void w4_few_kernel(const W4Args a, const W4
   float v = 0.f;
 #pragma unroll
   for (int u = 0; u < W; ++u) v += reinterpret_cast<const float*>(lds[u])[r * 16 + j];
+  if (__builtin_expect(!is_finite(v), 0)) v = sum_by_weights<T>(a, l, r, tile * 16 + j);
   finish<T>(a, r, tile * 16 + j, v);
 }
 
@@ -279,6 +304,13 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
     for (int u = 0; u < W; ++u) v += reinterpret_cast<const floatx4*>(lds[u])[i];
     const int row = m0 + (which % RT) * 16 + (ln & 15), j0 = (tile0 + which / RT) * 16 + 4 * (ln >> 4);
     if (row >= a.m) continue;
+    if (__builtin_expect(!is_finite(v), 0))
+#pragma unroll 1
+      for (int j = j0; j < min(j0 + 4, a.n); ++j) {
+        const float again = sum_by_weights<T>(a, l, row, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = j == j0 + e ? again : v[e];
+      }
     finish4<T>(a, row, j0, v);
   }
 }
@@ -476,13 +508,22 @@ __global__ __launch_bounds__(256 * PARTS, 2) void w4_tiles_kernel(const W4Args a
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum[i / 4][i % 4] += other[i * 256];
   }
+  unsigned again = 0;   // fours with a sum that is not finite, see sum_by_weights; none where zero points are subtracted exactly
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int row = m0 + wr * 64 + r * 16 + col;
     if (row >= a.m) continue;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) finish4<T>(a, row, (tile0 + wu * 4 + t) * 16 + 4 * g, sum[t][r]);
+    for (int t = 0; t < 4; ++t) {
+      if (!EXACT && __builtin_expect(!is_finite(sum[t][r]), 0)) again |= 1u << (r * 4 + t);
+      else finish4<T>(a, row, (tile0 + wu * 4 + t) * 16 + 4 * g, sum[t][r]);
+    }
   }
+  if constexpr (!EXACT)
+    for (; again; again &= again - 1) {
+      const int i = __builtin_ctz(again), row = m0 + wr * 64 + (i >> 2) * 16 + col, j0 = (tile0 + wu * 4 + (i & 3)) * 16 + 4 * g;
+      for (int j = j0; j < min(j0 + 4, a.n); ++j) finish<T>(a, row, j, sum_by_weights<T>(a, l, row, j));
+    }
 }
 
 // a thread packs one word: eight codes, or one scale, or one zero point
