@@ -8,6 +8,7 @@ There is no fallback: if the library is missing or a call fails, an exception is
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Sequence, Optional, Tuple
 
@@ -636,6 +637,11 @@ class QDenseW4Desc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "m", "n", "k", "group", "has_zeros")] + [("flags", C.c_uint32)] + \
         [(n, C.c_int64) for n in ("x_stride", "y_stride")]
 
+    @functools.cached_property
+    def packed_bytes(self) -> int:
+        """What relay_qdense_w4 reads of the packed weights (asked for once: it depends on n, k, group, dtype and has_zeros)."""
+        return relay_qdense_w4_packed_bytes(self)
+
 
 def dtype_of(t) -> int:
     """relay_dtype of a floating-point tensor."""
@@ -692,8 +698,10 @@ def qdense_w4_desc(x, y, group: int, zeros=None, bias=None, residual=None, relu=
     """Descriptor of relay_qdense_w4 from its tensors: x [m, k], y [m, n] with contiguous rows; residual with y's strides."""
     if x.stride(1) != 1 or y.stride(1) != 1 or x.shape[0] != y.shape[0] or x.dtype != y.dtype:
         raise RelayError(2, "x [m, k] and y [m, n] must have one type and contiguous rows")
-    if residual is not None and (residual.shape != y.shape or residual.stride() != y.stride()):
-        raise RelayError(2, "residual must have the shape and strides of y")
+    if residual is not None and (residual.shape != y.shape or residual.stride() != y.stride() or residual.dtype != y.dtype):
+        raise RelayError(2, "residual must have the type, shape and strides of y")
+    if bias is not None and (dtype_of(bias) != RELAY_F32 or bias.numel() != y.shape[1] or not bias.is_contiguous()):
+        raise RelayError(2, "bias must be float32 [n]")
     return QDenseW4Desc(dtype_of(x), x.shape[0], y.shape[1], x.shape[1], group, 0 if zeros is None else 1,
                         flags_of(bias, None, residual, relu), x.stride(0), y.stride(0))
 
@@ -730,11 +738,18 @@ def relay_qdense_w4_packed_bytes(d: QDenseW4Desc) -> int:
 
 
 def relay_prepack_qdense_w4(d: QDenseW4Desc, codes, scales, zeros, packed) -> None:
+    groups = -(-d.k // d.group)
+    for name, t, kind, width in (("codes", codes, "torch.uint8", d.k // 2), ("scales", scales, None, groups), ("zeros", zeros, "torch.uint8", groups)):
+        if t is not None and (tuple(t.shape) != (d.n, width) or not t.is_contiguous() or
+                              (str(t.dtype) != kind if kind else dtype_of(t) != d.dtype)):
+            raise RelayError(2, f"{name}: {tuple(t.shape)} of {t.dtype} do not go with n={d.n}, k={d.k}, group={d.group} and the descriptor's type")
     _check(lib().relay_prepack_qdense_w4(C.addressof(d), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(packed),
                                          packed.numel() * packed.element_size(), _stream()))
 
 
 def relay_qdense_w4(d: QDenseW4Desc, x, packed, bias, residual, y) -> None:
+    if packed is not None and packed.nbytes < d.packed_bytes:
+        raise RelayError(6, f"packed weights of {packed.nbytes} bytes, {d.packed_bytes} needed")
     _check(lib().relay_qdense_w4(C.addressof(d), _ptr(x), _ptr(packed), _ptr(bias), _ptr(residual), _ptr(y), _stream()))
 
 

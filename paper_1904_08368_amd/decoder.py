@@ -105,11 +105,14 @@ class Dense4:
     def __init__(self, codes, scales, zeros, group: int, k: int, bias: Optional[torch.Tensor] = None):
         self.n, self.k, self.group, self.zeros, self.bias, self.dtype = codes.shape[0], k, group, zeros, bias, scales.dtype
         x, y = (torch.empty((0, e), dtype=self.dtype, device=codes.device) for e in (k, self.n))
-        d = B.qdense_w4_desc(x, y, group, zeros)
+        d = B.qdense_w4_desc(x, y, group, zeros, bias)
         self.packed = torch.empty(B.relay_qdense_w4_packed_bytes(d), dtype=torch.uint8, device=codes.device)
         B.relay_prepack_qdense_w4(d, codes, scales, zeros, self.packed)
 
     def __call__(self, x, y, residual=None):
+        # (the packed order depends on all of these, and nothing of it is left in the packed bytes)
+        if x.dtype != self.dtype or x.shape[1] != self.k or y.shape[1] != self.n:
+            raise ValueError(f"x {tuple(x.shape)} of {x.dtype} and y {tuple(y.shape)} do not go with a layer of {self.n} units by {self.k} in {self.dtype}")
         B.relay_qdense_w4(B.qdense_w4_desc(x, y, self.group, self.zeros, self.bias, residual), x, self.packed, self.bias, residual, y)
         return y
 
