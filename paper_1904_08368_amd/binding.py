@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import sys
 from typing import Sequence, Optional, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -663,13 +664,45 @@ def rope_table_desc(rows, rotary_dim, base=10000.0, first=0, scaling=ROPE_PLAIN,
     return RopeTableDesc(rows, first, rotary_dim, scaling, base, factor, slow, fast, original_len, magnitude)
 
 
+def _table(cos_sin):
+    if dtype_of(cos_sin) != RELAY_F32 or cos_sin.dim() != 3 or cos_sin.shape[2] != 2 or not cos_sin.is_contiguous():
+        raise RelayError(2, f"cos_sin must be float32 [rows, rotary_dim/2, 2], contiguous, not {tuple(cos_sin.shape)} of {cos_sin.dtype}")
+    return cos_sin.shape[0], 2 * cos_sin.shape[1]
+
+
+def _one_type(**tensors):
+    if len({t.dtype for t in tensors.values()}) > 1:
+        raise RelayError(3, "one type for all of " + ", ".join(f"{n} ({t.dtype})" for n, t in tensors.items()))
+
+
+def _missing(*operands) -> Exception:
+    """What stands for an AttributeError of a call whose operands are asked for their addresses."""
+    return RelayError(1, "every operand but the workspace is required") if any(t is None for t in operands) else sys.exc_info()[1]
+
+
+_INT32 = None
+
+
+def _refuse_index(name, t, count):
+    """Positions, slots, page numbers and lengths are read as int32, one after another.  What is not that ends here; called where a look at the
+    tensor found it wanting, or where none was taken yet."""
+    global _INT32
+    import torch
+    _INT32 = torch.int32
+    if t is None:
+        raise RelayError(1, f"{name} is required")
+    if t.dtype is not _INT32 or t.numel() < count or not t.is_contiguous():
+        raise RelayError(2, f"{name} must be int32, contiguous, of {count} elements, not {tuple(t.shape)} of {t.dtype}")
+
+
 def rope_desc(x, cos_sin, y, style=ROPE_HALF, inverse=False) -> RopeDesc:
     """Descriptor of relay_rope from its tensors: x, y [tokens, heads, head_dim] (any strides of the first two axes), cos_sin
     [rows, rotary_dim/2, 2].  Kept for calls with tensors of the same shapes and strides."""
     if x.shape != y.shape or x.dtype != y.dtype or x.stride(2) != 1 or y.stride(2) != 1:
         raise RelayError(2, "x and y must have one shape and type and contiguous heads")
-    return RopeDesc(dtype_of(x), x.shape[0], x.shape[1], x.shape[2], 2 * cos_sin.shape[1], style, 1 if inverse else 0,
-                    cos_sin.shape[0], x.stride(0), x.stride(1), y.stride(0), y.stride(1))
+    rows, rotary_dim = _table(cos_sin)
+    return RopeDesc(dtype_of(x), x.shape[0], x.shape[1], x.shape[2], rotary_dim, style, 1 if inverse else 0,
+                    rows, x.stride(0), x.stride(1), y.stride(0), y.stride(1))
 
 
 def rope_append_desc(q, k, v, cos_sin, q_out, cache, style=ROPE_HALF) -> RopeAppendDesc:
@@ -677,7 +710,11 @@ def rope_append_desc(q, k, v, cos_sin, q_out, cache, style=ROPE_HALF) -> RopeApp
     cache: k_cache (v_cache has the same shape and strides), [pages, page_size, kv_heads, head_dim] in any order in memory."""
     if k.shape != v.shape or q.shape != q_out.shape or cache.shape[2:] != k.shape[1:] or cache.stride(3) != 1:
         raise RelayError(2, "shapes of q, k, v and the cache do not go together")
-    return RopeAppendDesc(dtype_of(q), q.shape[0], q.shape[1], k.shape[1], q.shape[2], 2 * cos_sin.shape[1], style, cos_sin.shape[0],
+    if q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+        raise RelayError(2, f"q {tuple(q.shape)} and k {tuple(k.shape)}: other tokens or channels")
+    _one_type(q=q, k=k, v=v, q_out=q_out, cache=cache)
+    rows, rotary_dim = _table(cos_sin)
+    return RopeAppendDesc(dtype_of(q), q.shape[0], q.shape[1], k.shape[1], q.shape[2], rotary_dim, style, rows,
                           cache.shape[0], cache.shape[1], _contiguous_heads(q, "q"), _contiguous_heads(k, "k"), _contiguous_heads(v, "v"),
                           _contiguous_heads(q_out, "q_out"), cache.stride(0), cache.stride(1), cache.stride(2))
 
@@ -689,6 +726,8 @@ def paged_attention_desc(q, cache, page_table, out, max_q_len: int, max_kv_len: 
     if q.shape != out.shape or cache.shape[3] != q.shape[2] or cache.stride(3) != 1 or page_table.stride(1) != 1 or \
             (page_table.shape[0] > 1 and page_table.stride(0) != page_table.shape[1]):
         raise RelayError(2, "shapes of q, out, the cache and the page table do not go together")
+    _one_type(q=q, out=out, cache=cache)
+    _refuse_index("page_table", page_table, page_table.numel())
     return PagedAttentionDesc(dtype_of(q), page_table.shape[0], q.shape[0], q.shape[1], cache.shape[2], q.shape[2], cache.shape[0],
                               cache.shape[1], page_table.shape[1], max_q_len, max_kv_len, 1 if causal else 0, window, scale,
                               _contiguous_heads(q, "q"), _contiguous_heads(out, "out"), cache.stride(0), cache.stride(1), cache.stride(2))
@@ -710,13 +749,27 @@ def relay_rope_table(d: RopeTableDesc, cos_sin) -> None:
     _check(lib().relay_rope_table(C.addressof(d), _ptr(cos_sin), _stream()))
 
 
+# (The looks at the index tensors and the addresses are written out in these calls: as calls of their own they take half a microsecond of
+# an eager call's three.)
 def relay_rope(d: RopeDesc, x, cos_sin, positions, y) -> None:
-    _check(lib().relay_rope(C.addressof(d), _ptr(x), _ptr(cos_sin), _ptr(positions), _ptr(y), _stream()))
+    n = d.tokens
+    if positions is None or positions.dtype is not _INT32 or positions.numel() < n or not positions.is_contiguous():
+        _refuse_index("positions", positions, n)
+    _check(lib().relay_rope(C.addressof(d), _ptr(x), _ptr(cos_sin), positions.data_ptr(), _ptr(y), _stream()))
 
 
 def relay_rope_append(d: RopeAppendDesc, q, k, v, cos_sin, positions, slots, q_out, k_cache, v_cache) -> None:
-    _check(lib().relay_rope_append(C.addressof(d), _ptr(q), _ptr(k), _ptr(v), _ptr(cos_sin), _ptr(positions), _ptr(slots), _ptr(q_out),
-                                   _ptr(k_cache), _ptr(v_cache), _stream()))
+    n = d.tokens
+    if positions is None or positions.dtype is not _INT32 or positions.numel() < n or not positions.is_contiguous():
+        _refuse_index("positions", positions, n)
+    if slots is None or slots.dtype is not _INT32 or slots.numel() < n or not slots.is_contiguous():
+        _refuse_index("slots", slots, n)
+    try:
+        status = lib().relay_rope_append(C.addressof(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), cos_sin.data_ptr(), positions.data_ptr(),
+                                         slots.data_ptr(), q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _stream())
+    except AttributeError:
+        raise _missing(q, k, v, cos_sin, q_out, k_cache, v_cache)
+    _check(status)
 
 
 def relay_paged_attention_workspace_bytes(d: PagedAttentionDesc) -> int:
@@ -726,9 +779,19 @@ def relay_paged_attention_workspace_bytes(d: PagedAttentionDesc) -> int:
 
 
 def relay_paged_attention(d: PagedAttentionDesc, q, k_cache, v_cache, page_table, q_starts, kv_lens, out, workspace=None) -> None:
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().relay_paged_attention(C.addressof(d), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(q_starts),
-                                       _ptr(kv_lens), _ptr(out), _ptr(workspace) if ws_bytes else None, ws_bytes, _stream()))
+    n = d.batch
+    if q_starts is None or q_starts.dtype is not _INT32 or q_starts.numel() <= n or not q_starts.is_contiguous():
+        _refuse_index("q_starts", q_starts, n + 1)
+    if kv_lens is None or kv_lens.dtype is not _INT32 or kv_lens.numel() < n or not kv_lens.is_contiguous():
+        _refuse_index("kv_lens", kv_lens, n)
+    ws_bytes = 0 if workspace is None else workspace.nbytes
+    try:
+        status = lib().relay_paged_attention(C.addressof(d), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
+                                             q_starts.data_ptr(), kv_lens.data_ptr(), out.data_ptr(),
+                                             workspace.data_ptr() if ws_bytes else None, ws_bytes, _stream())
+    except AttributeError:
+        raise _missing(q, k_cache, v_cache, page_table, out)
+    _check(status)
 
 
 def relay_qdense_w4_packed_bytes(d: QDenseW4Desc) -> int:
