@@ -118,12 +118,15 @@ class Dense4:
 
 
 def quantize4(w: torch.Tensor, group: int):
-    """codes, scales and zero points of a weight matrix [n, k], each group of a row between its least and its largest value."""
+    """codes, scales and zero points of a weight matrix [n, k], each group of a row between its least and its largest value.
+
+    The least scale: fp16's 2^-20, which it still holds to 5 bits (its least normal number, 2^-14, would take all of a group's codes from
+    weights below 2^-15), bf16's least normal number."""
     n, k = w.shape
     groups = -(-k // group)
     parts = torch.nn.functional.pad(w.float(), (0, groups * group - k), value=0.0).view(n, groups, group)
     lo, hi = parts.amin(2).clamp(max=0.0), parts.amax(2).clamp(min=0.0)
-    scales = ((hi - lo) / 15).clamp(min=2.0 ** -14).to(w.dtype)
+    scales = ((hi - lo) / 15).clamp(min=2.0 ** -20 if w.dtype == torch.float16 else torch.finfo(w.dtype).tiny).to(w.dtype)
     zeros = (-lo / scales.float()).round().clamp(0, 15)
     codes = (parts / scales.float()[..., None] + zeros[..., None]).round().clamp(0, 15).to(torch.uint8).view(n, -1)[:, :k]
     return (codes[:, 0::2] | codes[:, 1::2] << 4).contiguous(), scales.contiguous(), zeros.to(torch.uint8).contiguous()
