@@ -49,6 +49,8 @@ class PagedCache:
 
     def extend(self, seqs: Sequence[int], new: Sequence[int]) -> None:
         """Room for `new` more tokens of each sequence; all of it or, if the pages do not suffice, none."""
+        if len(set(seqs)) != len(seqs) or len(new) != len(seqs) or min(new, default=0) < 0:
+            raise ValueError("each sequence once, with its number of new tokens")
         need = [-(-(self.length[s] + n) // self.page_size) - len(self.pages[s]) for s, n in zip(seqs, new)]
         if sum(need) > len(self.free):
             raise MemoryError(f"{sum(need)} pages needed, {len(self.free)} free")
