@@ -119,7 +119,8 @@ typedef struct {
  *   out = sum_j softmax_j(scale * q . k_j) v_j   over keys 0 <= j < kv_lens[b], j <= p if causal, j > p - window if window > 0
  * Key j lies in slot j % page_size of page page_table[b][j / page_size].  A token that sees no key gets zeros (and so does one whose scores
  * are all -infinity).  Keys that a token does not see do not reach its result, whatever they hold (infinities and NaN included).  Scores, the softmax and the sums
- * are fp32; the probabilities are rounded to the tensor's type for the product with v, whose sums are fp32.
+ * are fp32; the probabilities are rounded to the tensor's type for the product with v, whose sums are fp32 (and, where there are more than 16 rows to a key
+ * head, for their own sum too).
  * A page number outside 0 .. num_pages-1, or a key past pages_per_seq pages, is not read: such keys count as unseen.
  *   q, out [tokens][q_heads][head_dim] with the token strides given; k_cache, v_cache, strides as relay_rope_append
  *   page_table int32 [batch][pages_per_seq]; q_starts int32 [batch+1], ascending; kv_lens int32 [batch]

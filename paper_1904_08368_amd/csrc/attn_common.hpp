@@ -22,6 +22,12 @@ template <> struct Mma<_Float16> {
   typedef halfx8 vec;
   typedef _Float16 pair __attribute__((ext_vector_type(2)));
   static constexpr unsigned kExp = 0x7c007c00u;   // exponent bits of two elements
+  // Probabilities are taken this power of two larger (bf16 reaches as far down as fp32 and needs none), so that fp16 still holds those 2^-22 of the largest to
+  // its full precision in the kernel for few rows, 2^-18 of the reference in the other, where one may be up to 2^8 by itself.  No further: scores of 10^8 leave an exponent that is
+  // off by some units, and fp16 ends at 2^16.
+  static constexpr float kShiftRows = 8.f, kShiftTiles = 4.f;
+  // c + the two elements of a word.  (The instruction does not round to nearest: for the few words of a step, not for a sum over all of them.)
+  static __device__ __forceinline__ float add2(unsigned w, float c) { return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, w), (pair){1, 1}, c, false); }
   static __device__ __forceinline__ floatx4 mfma16(vec a, vec b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ floatx16 mfma32(vec a, vec b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
@@ -29,6 +35,8 @@ template <> struct Mma<__bf16> {
   typedef bfx8 vec;
   typedef __bf16 pair __attribute__((ext_vector_type(2)));
   static constexpr unsigned kExp = 0x7f807f80u;
+  static constexpr float kShiftRows = 0.f, kShiftTiles = 0.f;
+  static __device__ __forceinline__ float add2(unsigned w, float c) { return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, 0x3f803f80u), c, false); }
   static __device__ __forceinline__ floatx4 mfma16(vec a, vec b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ floatx16 mfma32(vec a, vec b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };

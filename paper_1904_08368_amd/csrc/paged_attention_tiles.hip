@@ -191,7 +191,10 @@ __global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_ti
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
   // ref: what the exponents are taken relative to.  It follows the maximum only when that has outgrown it by 2^8: until then the sums need no
-  // rescaling, and probabilities of up to 256 are as exact as those of up to 1.
+  // rescaling.  Probabilities are rounded to the tensor's type for the product with the values, as its operands are.  So the largest, which would be 1 and exact if
+  // the reference were the maximum, is rounded too; l adds the rounded ones, so that what rounding does to a weight that is most of a row's it does
+  // to both sides of the quotient.  Relative error with the unrounded ones in l / as it is / of the exact result rounded: 8192 tokens, fp16, 2.7e-4 / 2.5e-4 / 2.1e-4, chunks
+  // over 9001 keys, bf16, 2.2e-3 / 2.1e-3 / 1.7e-3.  The additions stand between the second product's instructions: before them they took 3 % more time, there 0.3 %.
   float ref = kNegInf, l = 0.f;
 
   unsigned long long can = 0, can_next = 0;
@@ -305,7 +308,7 @@ __global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_ti
 #pragma unroll
       for (int d = 0; d < DB; ++d) acc[d] *= alpha;
     }
-    const float base = ref == kNegInf ? 0.f : ref;
+    const float base = ref == kNegInf ? 0.f : ref - M::kShiftTiles;
     vec pf[2 * NB];
     float sum = 0.f;
 #pragma unroll
@@ -314,12 +317,10 @@ __global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_ti
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float p0 = pow2(fmaf(st[t / 2][8 * (t & 1) + 2 * e], c, -base)), p1 = pow2(fmaf(st[t / 2][8 * (t & 1) + 2 * e + 1], c, -base));
-        sum += p0 + p1;
         w[e] = pack2<T>(p0, p1);
       }
       pf[t] = __builtin_bit_cast(vec, w);
     }
-    l += sum;
     // values: this lane's piece of the rows 16 t + 4 h .. + 3 and of the rows 8 further on
     const int vrow = 4 * h + ((lane & 15) >> 2), vch = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vhalf = (lane & 1) * 4;
     auto values = [&](int t, int d) {
@@ -336,9 +337,12 @@ __global__ __launch_bounds__(kTileWaves * 64, workgroups_of_cu(DP)) void attn_ti
     for (int n = 0; n < N2; ++n) {
       acc[n % DB] = M::mfma32(__builtin_bit_cast(vec, vf[n % AHEAD2]), pf[n / DB], acc[n % DB]);
       if (n + AHEAD2 < N2) vf[n % AHEAD2] = values((n + AHEAD2) / DB, (n + AHEAD2) % DB);
+#pragma unroll
+      for (int e = n % DB * 4 / DB; e < (n % DB + 1) * 4 / DB; ++e) sum = M::add2(__builtin_bit_cast(uintx4, pf[n / DB])[e], sum);
       if constexpr (MORE)
         if (n % (N2 / PER) == 0) copy_values(buf ^ 1, n / (N2 / PER));
     }
+    l += sum;
   };
   for (; j0 + KEYS < hi; j0 += KEYS, buf ^= 1) step(std::true_type());
   if (j0 < hi) step(std::false_type());
