@@ -155,7 +155,8 @@ hipError_t launch_type(const RopeArgs& a, int piece, hipStream_t st) {
 }
 
 __global__ __launch_bounds__(256) void rope_table_kernel(const RopeTableArgs a) {
-  const int i = (int)(blockIdx.x * 64 + (threadIdx.x & 63)), r0 = (int)(blockIdx.y * 4 + (threadIdx.x >> 6));
+  const int i = (int)(blockIdx.x * 64 + (threadIdx.x & 63));
+  const long r0 = blockIdx.y * 4 + (threadIdx.x >> 6);   // (up to 2^31 - 1 rows, and a stride on top)
   if (i >= a.pairs) return;
   const double kTwoPi = 6.283185307179586476925286766559;
   double base = a.base;
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const RopeTableArgs a) 
     const double g = fmin(fmax((turns - a.slow) / (a.fast - a.slow), 0.0), 1.0);
     f = (1.0 - g) * f / a.factor + g * f;
   }
-  for (int r = r0; r < a.rows; r += (int)gridDim.y * 4) {
+  for (long r = r0; r < a.rows; r += gridDim.y * 4) {
     double s, c;
     sincos(((double)a.first + (double)r) * f, &s, &c);
     reinterpret_cast<float2*>(a.out)[(size_t)r * a.pairs + i] = make_float2((float)(a.magnitude * c), (float)(a.magnitude * s));
