@@ -171,7 +171,8 @@ class AttentionLayer:
         self.workspace = Workspace() if workspace is None else workspace
         device = qkv.packed.device
         self._qkv = torch.empty((max_tokens, qkv.n), dtype=qkv.dtype, device=device)
-        self._attn = torch.empty((max_tokens, q_heads * head_dim), dtype=qkv.dtype, device=device)
+        # (rows of padding are read by the second projection and written by nothing: what the memory held before would be their input)
+        self._attn = torch.zeros((max_tokens, q_heads * head_dim), dtype=qkv.dtype, device=device)
 
     def __call__(self, x, index: int, step: Step, y=None):
         """x [step.tokens, width] -> y; `index`: this layer's cache."""
