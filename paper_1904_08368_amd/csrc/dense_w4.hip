@@ -188,12 +188,12 @@ __global__ __launch_bounds__(W * 64) void w4_few_kernel(const W4Args a, const W4
   finish<T>(a, r, tile * 16 + j, v);
 }
 
-// More rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; DEPTH chunks of
-// codes and of x are on their way.  x comes in whole rows of a chunk, 256 bytes to 16 lanes, and is turned into B operands in a piece of LDS
+// More rows.  NT tiles of 16 units and RT tiles of 16 rows to a wave, W waves share the reduction out in chunks of 128; the next chunk of
+// codes and of x is on its way.  x comes in whole rows of a chunk, 256 bytes to 16 lanes, and is turned into B operands in a piece of LDS
 // that only its wave uses: asked for as the operands want it, 64 bytes to a row, sixteen rows of a large power of two apart, it came
 // out of few channels of the caches (8192 units by 8192, 16 rows: 20 us, with twice the units to a wave 15; in whole rows 10).
 // FL: steps of 32 between two applications of the scales, 4 where groups are whole chunks, 2 or 1 where they are not.
-template <typename T, int NT, int RT, int W, int DEPTH, int FL>
+template <typename T, int NT, int RT, int W, int FL>
 __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
   typedef W4Type<T> C;
   typedef typename C::vec vec;
@@ -220,30 +220,28 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
   const T* const x = static_cast<const T*>(a.x) + (long)m0 * a.x_stride + col * 8;
   const int rows = a.m - m0;
   typedef T four __attribute__((ext_vector_type(4)));
-  uintx4 codes[DEPTH][NT], xv[DEPTH][XL];
-  four sc[DEPTH][4 / FL][NT];
-  unsigned zp[DEPTH][4 / FL][NT];
-  auto load = [&](int chunk, int d) {
+  uintx4 codes[NT], xv[XL];
+  four sc[4 / FL][NT];
+  unsigned zp[4 / FL][NT];
+  auto load = [&](int chunk) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) codes[d][t] = w[t][(size_t)chunk * 64];
+    for (int t = 0; t < NT; ++t) codes[t] = w[t][(size_t)chunk * 64];
 #pragma unroll
     for (int f = 0; f < 4 / FL; ++f) {
       const int at = min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1) * 16;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        sc[d][f][t] = *reinterpret_cast<const four*>(scales[t] + at);
-        zp[d][f][t] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros[t] + at) : 0x18181818u;
+        sc[f][t] = *reinterpret_cast<const four*>(scales[t] + at);
+        zp[f][t] = a.zeros ? *reinterpret_cast<const unsigned*>(zeros[t] + at) : 0x18181818u;
       }
     }
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-      xv[d][i] = (uintx4){0, 0, 0, 0};
-      if (4 * i + g < rows && chunk * 128 + col * 8 < a.k) xv[d][i] = *reinterpret_cast<const uintx4*>(x + (long)(4 * i + g) * a.x_stride + chunk * 128);
+      xv[i] = (uintx4){0, 0, 0, 0};
+      if (4 * i + g < rows && chunk * 128 + col * 8 < a.k) xv[i] = *reinterpret_cast<const uintx4*>(x + (long)(4 * i + g) * a.x_stride + chunk * 128);
     }
   };
-#pragma unroll
-  for (int d = 0; d < DEPTH; ++d)
-    if (first + d < last) load(first + d, d);
+  if (first < last) load(first);
   uintx4* const mine = lds[wave];
   const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
   const Widen<T> widen;
@@ -252,44 +250,39 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < RT; ++r) sum[t][r] = (floatx4){0, 0, 0, 0};
-  for (int c0 = first; c0 < last; c0 += DEPTH) {
+  for (int chunk = first; chunk < last; ++chunk) {
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const int chunk = c0 + d;
-      if (chunk >= last) break;
+    for (int i = 0; i < XL; ++i) mine[(4 * i + g) * 16 + (col ^ ((4 * i + g) & 15))] = xv[i];
 #pragma unroll
-      for (int i = 0; i < XL; ++i) mine[(4 * i + g) * 16 + (col ^ ((4 * i + g) & 15))] = xv[d][i];
+    for (int f = 0; f < 4 / FL; ++f) {
+      floatx4 acc[NT][RT], xs[RT];
+      const floatx4 none = {0, 0, 0, 0};
 #pragma unroll
-      for (int f = 0; f < 4 / FL; ++f) {
-        floatx4 acc[NT][RT], xs[RT];
-        const floatx4 none = {0, 0, 0, 0};
+      for (int s = f * FL; s < (f + 1) * FL; ++s) {
+        const bool fresh = s == f * FL;
+        vec xb[RT];
 #pragma unroll
-        for (int s = f * FL; s < (f + 1) * FL; ++s) {
-          const bool fresh = s == f * FL;
-          vec xb[RT];
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            xb[r] = __builtin_bit_cast(vec, mine[(r * 16 + col) * 16 + ((4 * s + g) ^ col)]);
-            xs[r] = C::mfma(ones, xb[r], fresh ? none : xs[r]);
-          }
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const vec wv = widen(codes[d][t][s]);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
-          }
+        for (int r = 0; r < RT; ++r) {
+          xb[r] = __builtin_bit_cast(vec, mine[(r * 16 + col) * 16 + ((4 * s + g) ^ col)]);
+          xs[r] = C::mfma(ones, xb[r], fresh ? none : xs[r]);
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+          const vec wv = widen(codes[t][s]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float z = -(float)((zp[d][f][t] >> (8 * i)) & 255u), k = (float)sc[d][f][t][i];
-#pragma unroll
-            for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(k, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
-          }
+          for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
+        }
       }
-      if (chunk + DEPTH < last) load(chunk + DEPTH, d);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float z = -(float)((zp[f][t] >> (8 * i)) & 255u), k = (float)sc[f][t][i];
+#pragma unroll
+          for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(k, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
+        }
     }
+    if (chunk + 1 < last) load(chunk + 1);
   }
   floatx4* const part = reinterpret_cast<floatx4*>(mine);
 #pragma unroll
@@ -579,14 +572,14 @@ hipError_t launch_few(const W4Args& a, const W4Layout& l, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T, int NT, int RT, int W, int DEPTH>
+template <typename T, int NT, int RT, int W>
 hipError_t launch_rows(const W4Args& a, const W4Layout& l, hipStream_t st) {
   const int per_group = a.group / 32;
   const FastDiv fd = make_fastdiv((uint32_t)per_group);
   const dim3 grid((unsigned)((l.tiles + NT - 1) / NT), (unsigned)((a.m + 16 * RT - 1) / (16 * RT))), block(W * 64);
-  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, DEPTH, 4>), grid, block, 0, st, a, l, fd);
-  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, DEPTH, 2>), grid, block, 0, st, a, l, fd);
-  else hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, 1, 1>), grid, block, 0, st, a, l, fd);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((w4_rows_kernel<T, NT, RT, W, 1>), grid, block, 0, st, a, l, fd);
   return hipGetLastError();
 }
 
@@ -617,8 +610,8 @@ template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
   if (a.m == 1) return launch_few<T, 1, 8>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, 8>(a, l, st);
-  if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8, 1>(a, l, st) : launch_rows<T, 2, 1, 8, 1>(a, l, st);
-  if (rows_pay(a, l)) return launch_rows<T, 2, 2, 8, 1>(a, l, st);
+  if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8>(a, l, st) : launch_rows<T, 2, 1, 8>(a, l, st);
+  if (rows_pay(a, l)) return launch_rows<T, 2, 2, 8>(a, l, st);
   return tiles_of(a, l) <= 256 ? launch_tiles<T, 2>(a, l, st) : launch_tiles<T, 1>(a, l, st);
 }
 }  // namespace
