@@ -3,7 +3,9 @@
 // Codes enter the matrix cores as the exact 16-bit numbers 16 + code: the four bits are moved to the top of the
 // mantissa of 16.0, one shift and one and-or for two of them.  With S = sum_{i in g} x[m,i], which a product with ones gives,
 //   sum x (code - zero) = sum x (16 + code) - (16 + zero) S
-// so the weights are never rounded and a group's scale multiplies an fp32 sum.  The offset of 16 costs the sums three bits of fp32 at most.
+// so the weights are never rounded and a group's scale multiplies an fp32 sum.  The two sides are larger than their difference, so a group's sum is off by up to
+// (group + 4) 2^-24 sum |x| (32 + code + zero), where the weights alone would have |code - zero| in that place: beside an output of 16 bits that is small unless codes stand
+// close to their zero points.  The tiles of fp16 subtract the zero points from the codes instead, exactly, and pay none of it.
 //
 // Few rows of x: bound by the codes' bytes.  The waves of a workgroup share 16 units' rows out among them along the reduction, each
 // streams its part straight into the A operands (the packed order), and they add up through LDS.
@@ -106,7 +108,7 @@ __device__ __forceinline__ void finish4(const W4Args& a, int m, int j, floatx4 v
 
 // Up to MR rows (1 or 4): bound by the codes' bytes, and close behind by the memory pipe, which takes a 16-byte load of a wave in 16 clocks whatever its
 // lanes ask for.  So beside the codes' loads there are few others: what a wave needs of x, scales and zero points for SC chunks of its
-// part of the reduction comes in whole 16-byte pieces and goes through LDS that only this wave uses.  One row by 32768 x 8192, bf16: 29 us = 4.7 TB/s (31 with a load of
+// part of the reduction comes in whole 16-byte pieces and goes through LDS that only this wave uses.  One row by 32768 x 8192, bf16: 29 to 31 us by box = 4.4 to 4.7 TB/s (31 where this took 29 with a load of
 // x and of scales to every chunk, 40 with four of x).
 // W waves share the reduction out.  FL: steps of 32 between two applications of the scales, 4 where groups are whole chunks, 2 or 1 where they are not.
 template <typename T, int MR, int W, int FL>
@@ -317,7 +319,8 @@ __global__ __launch_bounds__(W * 64, 2) void w4_rows_kernel(const W4Args a, cons
 // scales and zero points, which two waves share, in two buffers of a chunk.  A word of codes is widened once for four matrix instructions.  The sums of a group and
 // those of all groups are both kept in registers, 64 each.  blockIdx.x runs over the units: workgroups that share rows of x follow each other.
 // PARTS 2: eight waves, of which four and four share the reduction out, for launches of so few tiles that a CU has one.
-// FL as above.  1500 rows, 8192 units by 4096, fp16: 121 us = 828 TFLOP/s; 1024 rows, 8192 by 8192 150 us = 915.
+// FL as above.  1500 rows, 8192 units by 4096, fp16: 123 us = 820 TFLOP/s; 1024 rows, 8192 by 8192 152 us = 902;
+// 1500 rows in bf16, groups of 32, 197 us = 510: that type has no exact subtraction, and such groups a scale at every step.
 template <typename T, int FL, int PARTS>
 __global__ __launch_bounds__(256 * PARTS, 2) void w4_tiles_kernel(const W4Args a, const W4Layout l, const FastDiv per_group) {
   typedef W4Type<T> C;
@@ -600,8 +603,15 @@ hipError_t launch_tiles(const W4Args& a, const W4Layout& l, hipStream_t st) {
 
 // More than 16 rows: 32 at a time on the kernel whose waves share the reduction out, or as tiles of 128 x 128, each of which walks the whole reduction: where
 // a CU has one of them at most, in two parts at 4 us and 1.25 us a chunk (in one part 1.7 us a chunk), where it has two, 2.35 us a chunk. The other kernel
-// takes 2.5 us and 0.67 ns a workgroup and chunk. Measured, rows / tiles, us, groups of 128: 8192 units by 8192, 64 rows 25 / 82, 128 rows 48 / 82, 256 rows
-// 90 / 83, 512 rows 178 / 85; 4096 x 4096, 300 rows 31 / 44; 28000 x 4096, 64 rows 46 / 45; 1500 x 2000 in groups of 64, 200 rows 10 / 26.
+// takes 2.5 us and 0.67 ns a workgroup and chunk.  Measured, rows / tiles, us, of the two for each call the quicker, unless marked (!):
+//   8192 units by 8192, fp16, groups of 128: 64 rows 28 / 84, 128 rows 53 / 85, 256 rows 101 / 85, 512 rows 196 / 88; bf16 the same but for tiles of 89 to 91;
+//     groups of 64: 29 / 89, 57 / 90, 110 / 90, 216 / 93, bf16 29 / 103, 58 / 104, 109 / 104, 215 / 105;
+//     groups of 32: 40 / 110, 68 / 110, 127 / 111, 245 / 112, bf16 36 / 131, 68 / 131, 128 / 131 (! tiles), 249 / 132
+//   4096 units by 4096, groups of 128 / 32: 300 rows 33 / 45, 44 / 58
+//   28000 units by 4096, groups of 128: 48 rows 47 / 46 (! rows), 128 rows 92 / 47, 300 rows 213 / 122; groups of 32 64 / 59 (! rows), 125 / 60, 294 / 162
+//   1504 units by 2000: 300 rows 11 / 26.
+// A chunk of tiles takes up to 1.5 times as long in bf16 and groups of 32 as the rule counts, one of the other kernel up to 1.3 times: where the two are close the
+// rule is off by 8 % at most in these.
 long tiles_of(const W4Args& a, const W4Layout& l) { return ((l.tiles + 7L) / 8) * ((a.m + 127) / 128); }
 bool rows_pay(const W4Args& a, const W4Layout& l) {
   const long tiles = tiles_of(a, l), rows = ((l.tiles + 1L) / 2) * ((a.m + 31) / 32);
@@ -612,6 +622,9 @@ bool rows_pay(const W4Args& a, const W4Layout& l) {
 
 template <typename T>
 hipError_t launch_type(const W4Args& a, const W4Layout& l, hipStream_t st) {
+  // Up to four rows on the kernel for few (us, it / the other at 4 rows: 4096 units by 4096 5.2 / 5.4, 8192 by 8192 10.7 / 11.5, in groups of 32 13.3 / 13.4; 32768 by 4096 19.5 / 19.8,
+  // in groups of 32 23 / 30; 32768 by 8192 35 / 29, in groups of 32 42 / 49).  Up to 16, two tiles of units to a workgroup where that leaves every CU one (us, one / two
+  // tiles: 4096 units by 8192, 16 rows 10.6 / 11.6, 4112 by 8192 12.5 / 11.7, 8192 by 4096 8.8 / 8.6, 6 rows 7.1 / 8.0, 28000 by 4096 22.8 / 20.2, 6 rows 19 / 17.7).
   if (a.m == 1) return launch_few<T, 1, 8>(a, l, st);
   if (a.m <= 4) return launch_few<T, 4, 8>(a, l, st);
   if (a.m <= 16) return l.tiles <= 256 ? launch_rows<T, 1, 1, 8>(a, l, st) : launch_rows<T, 2, 1, 8>(a, l, st);

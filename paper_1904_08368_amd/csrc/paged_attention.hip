@@ -10,8 +10,8 @@
 // workgroups, a unit is made as long as lets every workgroup have one; else units are short and a run goes over several tiles.  A tile
 // that lies within one run is finished by it; of others each workgroup leaves sums, maximum and weight in the workspace, and the one that arrives last
 // joins them in the order of the line.
-// Measured (key heads of 128 channels): 48 sequences of up to 8192 keys, 8 key heads, bf16, 211 us = 5.1 TB/s; one of 100001 keys, 4 key heads, fp16, 54 us, of which it streams
-// 33 at 6 TB/s; one of 700 keys 11.8 us, of 200 8.7: a launch is 5, the rest one trip to memory after another.
+// Measured (key heads of 128 channels): 48 sequences of up to 8192 keys, 8 key heads, bf16, 212 us = 5.1 TB/s; one of 100001 keys, 4 key heads, fp16, 54 us, of which it streams
+// 33 at 6 TB/s; one of 700 keys 11.9 us, of 200 8.7: an almost empty kernel is 2.4, the rest one trip to memory after another.
 #include <algorithm>
 #include <type_traits>
 

@@ -2,9 +2,10 @@
 //
 // 128 rows of a key head (a row is a token and one of the query heads that share the key head) to a workgroup, 32 to each of its four waves; 64 keys at a
 // time, staged in LDS for all of them without passing through registers, two buffers, one barrier a step.  Bound by the matrix cores and, beside them, by vector
-// instructions: on a step a wave does 32 products of 32 x 32 x 16 (head_dim 128) in 1024 clocks, and 2048 exponentials and what belongs to them in 900.  Two workgroups
+// instructions: on a step a wave does 32 products of 32 x 32 x 16 (head_dim 128) in 1024 clocks, and 2048 exponentials and what belongs to them in 990.  Two workgroups
 // share a CU, so that one's softmax runs beside the other's products.  Where there are few tiles their keys are cut into parts, and a second
-// kernel joins them.  Measured: 8192 tokens, 16 heads over 4 key heads, fp16, 290 us = 940 TFLOP/s; 512 tokens over 30000 keys, 32 over 8, 264 us; 64 tokens over them 55 us.
+// kernel joins them.  Measured: 8192 tokens, 16 heads over 4 key heads, fp16, 293 to 303 us by box = 938 to 907 TFLOP/s; 512 tokens over 30000 keys, 32 over 8, 270 to 277 us; 64 tokens over
+// them 55 us.  Other heads: 2 x 4096 tokens, 16 over 4 of 64, fp16, 96 us = 717 TFLOP/s; 4 x 2048 of 96, bf16, 56 us = 565; 2 x 2048 of 256, bf16, 124 us = 457 (one workgroup to a CU).
 #include <algorithm>
 #include <type_traits>
 
