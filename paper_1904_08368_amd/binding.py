@@ -644,19 +644,26 @@ class QDenseW4Desc(C.Structure):
         return relay_qdense_w4_packed_bytes(self)
 
 
+_DTYPES = {}   # relay_dtype of torch's types, filled in when the first is asked for
+
+
 def dtype_of(t) -> int:
     """relay_dtype of a floating-point tensor."""
-    name = str(t.dtype)
-    codes = {"torch.float32": RELAY_F32, "torch.float16": RELAY_F16, "torch.bfloat16": RELAY_BF16}
-    if name not in codes:
-        raise RelayError(3, f"no relay_dtype for {name}")
-    return codes[name]
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        import torch
+        _DTYPES.update({torch.float32: RELAY_F32, torch.float16: RELAY_F16, torch.bfloat16: RELAY_BF16})
+        if t.dtype not in _DTYPES:
+            raise RelayError(3, f"no relay_dtype for {t.dtype}")
+        code = _DTYPES[t.dtype]
+    return code
 
 
 def _contiguous_heads(t, name):
-    if t.stride(-1) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise RelayError(2, f"{name}: the heads of a token must be contiguous, strides {tuple(t.stride())}")
-    return t.stride(0)
+    token, head, channel = t.stride()
+    if channel != 1 or (head != t.shape[2] and t.shape[1] > 1):
+        raise RelayError(2, f"{name}: the heads of a token must be contiguous, strides {t.stride()}")
+    return token
 
 
 def rope_table_desc(rows, rotary_dim, base=10000.0, first=0, scaling=ROPE_PLAIN, factor=1.0, slow=1.0, fast=32.0,
@@ -665,14 +672,16 @@ def rope_table_desc(rows, rotary_dim, base=10000.0, first=0, scaling=ROPE_PLAIN,
 
 
 def _table(cos_sin):
-    if dtype_of(cos_sin) != RELAY_F32 or cos_sin.dim() != 3 or cos_sin.shape[2] != 2 or not cos_sin.is_contiguous():
+    rows, *pair = cos_sin.shape
+    if dtype_of(cos_sin) != RELAY_F32 or len(pair) != 2 or pair[1] != 2 or not cos_sin.is_contiguous():
         raise RelayError(2, f"cos_sin must be float32 [rows, rotary_dim/2, 2], contiguous, not {tuple(cos_sin.shape)} of {cos_sin.dtype}")
-    return cos_sin.shape[0], 2 * cos_sin.shape[1]
+    return rows, 2 * pair[0]
 
 
-def _one_type(**tensors):
-    if len({t.dtype for t in tensors.values()}) > 1:
-        raise RelayError(3, "one type for all of " + ", ".join(f"{n} ({t.dtype})" for n, t in tensors.items()))
+def _one_type(dtype, **others):
+    for name, t in others.items():
+        if t.dtype is not dtype:
+            raise RelayError(3, f"{name} is of {t.dtype}, q of {dtype}")
 
 
 def _missing(*operands) -> Exception:
@@ -708,29 +717,32 @@ def rope_desc(x, cos_sin, y, style=ROPE_HALF, inverse=False) -> RopeDesc:
 def rope_append_desc(q, k, v, cos_sin, q_out, cache, style=ROPE_HALF) -> RopeAppendDesc:
     """Descriptor of relay_rope_append from its tensors.  q, q_out [tokens, q_heads, head_dim], k, v [tokens, kv_heads, head_dim];
     cache: k_cache (v_cache has the same shape and strides), [pages, page_size, kv_heads, head_dim] in any order in memory."""
-    if k.shape != v.shape or q.shape != q_out.shape or cache.shape[2:] != k.shape[1:] or cache.stride(3) != 1:
-        raise RelayError(2, "shapes of q, k, v and the cache do not go together")
-    if q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
-        raise RelayError(2, f"q {tuple(q.shape)} and k {tuple(k.shape)}: other tokens or channels")
-    _one_type(q=q, k=k, v=v, q_out=q_out, cache=cache)
+    tokens, q_heads, dim = q.shape
+    pages, page_size, kv_heads, _ = cache.shape
+    page, slot, head, channel = cache.stride()
+    if k.shape != v.shape or q.shape != q_out.shape or k.shape != (tokens, kv_heads, dim) or cache.shape[3] != dim or channel != 1:
+        raise RelayError(2, f"q {tuple(q.shape)}, k {tuple(k.shape)}, v, q_out and the cache {tuple(cache.shape)} do not go together")
+    _one_type(q.dtype, k=k, v=v, q_out=q_out, cache=cache)
     rows, rotary_dim = _table(cos_sin)
-    return RopeAppendDesc(dtype_of(q), q.shape[0], q.shape[1], k.shape[1], q.shape[2], rotary_dim, style, rows,
-                          cache.shape[0], cache.shape[1], _contiguous_heads(q, "q"), _contiguous_heads(k, "k"), _contiguous_heads(v, "v"),
-                          _contiguous_heads(q_out, "q_out"), cache.stride(0), cache.stride(1), cache.stride(2))
+    return RopeAppendDesc(dtype_of(q), tokens, q_heads, kv_heads, dim, rotary_dim, style, rows, pages, page_size, _contiguous_heads(q, "q"),
+                          _contiguous_heads(k, "k"), _contiguous_heads(v, "v"), _contiguous_heads(q_out, "q_out"), page, slot, head)
 
 
 def paged_attention_desc(q, cache, page_table, out, max_q_len: int, max_kv_len: int, scale: float, causal=True,
                          window=0) -> PagedAttentionDesc:
     """Descriptor of relay_paged_attention from its tensors: q, out [tokens, q_heads, head_dim], cache as rope_append_desc,
     page_table [batch, pages_per_seq]."""
-    if q.shape != out.shape or cache.shape[3] != q.shape[2] or cache.stride(3) != 1 or page_table.stride(1) != 1 or \
-            (page_table.shape[0] > 1 and page_table.stride(0) != page_table.shape[1]):
+    tokens, q_heads, dim = q.shape
+    pages, page_size, kv_heads, _ = cache.shape
+    page, slot, head, channel = cache.stride()
+    batch, per_seq = page_table.shape
+    if q.shape != out.shape or cache.shape[3] != dim or channel != 1 or not page_table.is_contiguous():
         raise RelayError(2, "shapes of q, out, the cache and the page table do not go together")
-    _one_type(q=q, out=out, cache=cache)
-    _refuse_index("page_table", page_table, page_table.numel())
-    return PagedAttentionDesc(dtype_of(q), page_table.shape[0], q.shape[0], q.shape[1], cache.shape[2], q.shape[2], cache.shape[0],
-                              cache.shape[1], page_table.shape[1], max_q_len, max_kv_len, 1 if causal else 0, window, scale,
-                              _contiguous_heads(q, "q"), _contiguous_heads(out, "out"), cache.stride(0), cache.stride(1), cache.stride(2))
+    _one_type(q.dtype, out=out, cache=cache)
+    if page_table.dtype is not _INT32:
+        _refuse_index("page_table", page_table, 0)
+    return PagedAttentionDesc(dtype_of(q), batch, tokens, q_heads, kv_heads, dim, pages, page_size, per_seq, max_q_len, max_kv_len,
+                              1 if causal else 0, window, scale, _contiguous_heads(q, "q"), _contiguous_heads(out, "out"), page, slot, head)
 
 
 def qdense_w4_desc(x, y, group: int, zeros=None, bias=None, residual=None, relu=False) -> QDenseW4Desc:

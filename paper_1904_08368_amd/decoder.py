@@ -115,7 +115,9 @@ class Dense4:
         # (the packed order depends on all of these, and nothing of it is left in the packed bytes)
         if x.dtype != self.dtype or x.shape[1] != self.k or y.shape[1] != self.n:
             raise ValueError(f"x {tuple(x.shape)} of {x.dtype} and y {tuple(y.shape)} do not go with a layer of {self.n} units by {self.k} in {self.dtype}")
-        B.relay_qdense_w4(B.qdense_w4_desc(x, y, self.group, self.zeros, self.bias, residual), x, self.packed, self.bias, residual, y)
+        d = B.qdense_w4_desc(x, y, self.group, self.zeros, self.bias, residual)
+        d.packed_bytes = self.packed.nbytes   # (known here: not asked for again)
+        B.relay_qdense_w4(d, x, self.packed, self.bias, residual, y)
         return y
 
 
