@@ -348,10 +348,11 @@ def _plain_sample(s):
     if s["min_p"] is not None:
         keep &= w >= s["min_p"].double()[:, None]
     keep = torch.where(greedy, rank == 0, keep)
-    kept = torch.zeros_like(w).scatter_(1, order, w * keep)
+    kept = w * keep
     cum = torch.cumsum(kept, 1)
-    token = (cum <= s["uniform"].double()[:, None] * cum[:, -1:]).sum(1)
-    return token.to(torch.int32), (kept.gather(1, token[:, None])[:, 0] / cum[:, -1]).float()
+    # the uniform number names a place in the kept tokens' mass, the likeliest first
+    at = (cum <= s["uniform"].double()[:, None] * cum[:, -1:]).sum(1, keepdim=True)
+    return order.gather(1, at)[:, 0].to(torch.int32), (kept.gather(1, at)[:, 0] / cum[:, -1]).float()
 
 
 PLAIN = {"norm": _plain_norm, "route": _plain_route, "experts": _plain_experts, "sample": _plain_sample}
@@ -437,9 +438,8 @@ def _exact_sample(s):
             mass = np.cumsum(w[:n])
             n = int(np.searchsorted(mass, top_p[r] * mass[-1], side="left")) + 1
         n = max(1, min(n, int(np.count_nonzero(w >= min_p[r]))))
-        at = np.argsort(order[:n])                      # back to the order of the vocabulary
-        cum = np.cumsum(w[:n][at])
-        out[r] = w[at[int(np.searchsorted(cum, u[r] * cum[-1], side="right"))]] / cum[-1]
+        cum = np.cumsum(w[:n])
+        out[r] = w[int(np.searchsorted(cum, u[r] * cum[-1], side="right"))] / cum[-1]
     return torch.from_numpy(out).to(DEV)
 
 
