@@ -1,0 +1,52 @@
+/*
+ * relay_decoder.h -- fused primitive operators of a decoder's step beside its attention layer: the norms of a block with the residual
+ * stream, a mixture of experts with 4-bit weights, the choice of the next token.
+ *
+ * The calling convention of relay_fused.h and relay_attention.h holds here too: static shapes in a descriptor, device pointers that the
+ * caller owns, preallocated outputs and scratch, work enqueued on `hip_stream`, argument checks on the host before any HIP call, a status and a
+ * message on failure (paper Section 3.3, "Backends").  Strides are in elements, the innermost extent is contiguous.  What a program chooses on
+ * the device (experts, settings of a row) is checked there: what names nothing is skipped.  A call without tokens or rows is valid and launches nothing.
+ * Workspaces: 256-byte aligned, at least as many bytes as the call's _workspace_bytes says, zero before their first use, left ready for the next call
+ * of any descriptor that asks for no more.  Calls that may run at the same time need workspaces of their own.
+ *
+ * One block, beside its attention layer: relay_residual_norm -> relay_route -> relay_experts_w4 -> relay_residual_norm.
+ */
+#ifndef RELAY_DECODER_H_
+#define RELAY_DECODER_H_
+
+#include "relay_attention.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- norms of a block, with its gate and the residual stream ---------------------------------------------------- */
+enum { RELAY_NORM_NONE = 0, RELAY_NORM_RMS = 1, RELAY_NORM_LAYER = 2 };
+
+typedef struct {
+  int32_t dtype;              /* of x, residual, gate, sum and y: RELAY_F16, RELAY_BF16 or RELAY_F32 */
+  int32_t tokens, channels;   /* rows of 1 element to 65536 bytes */
+  int32_t post, pre;          /* RELAY_NORM_*: of the block's output x; of the sum, for the next block */
+  float post_eps, pre_eps;    /* >= 0 */
+  float branch_scale, residual_scale;
+  int64_t x_stride, residual_stride, gate_stride, sum_stride, y_stride;   /* of rows; gate_stride 0: one gate for all tokens */
+} relay_residual_norm_desc;
+
+/* What stands between two blocks, as one primitive function (the elementwise operators and the reductions they feed form one group, paper Section 4.1):
+ *   s = residual_scale * residual + branch_scale * gate * post(x),   sum = s,   y = pre(s)
+ *   RMS:   v / sqrt(mean(v^2) + eps) * weight + bias        LAYER: (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias
+ * over the channels of a token, in fp32, each output rounded once; y is made from s before its rounding.
+ *   x, residual, gate, sum, y [tokens][channels]; weights and biases fp32 [channels]
+ *   residual, gate NULL: not there.  A weight NULL: ones, a bias NULL: zeros; both must be NULL for RELAY_NORM_NONE.
+ *   sum NULL: not written.  y must be given exactly if pre is not RELAY_NORM_NONE; one of sum and y must be.
+ * sum and y may be x, residual or gate with the same stride (gate only if it has a row for every token); sum and y must not overlap otherwise, nor each other.
+ * Any alignment of the element type.  Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (kinds, aliasing), _DEVICE. */
+relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* x, const void* residual, const void* gate,
+                                 const float* post_weight, const float* post_bias, const float* pre_weight, const float* pre_bias,
+                                 void* sum, void* y, void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* RELAY_DECODER_H_ */

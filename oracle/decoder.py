@@ -1,0 +1,48 @@
+"""CPU oracle -- TEST INFRASTRUCTURE ONLY: a decoder's operators beside its attention layer in 64 bits, straight from their formulas.
+
+Tensors are numpy arrays of float64 (values of the 16-bit types are exact in it).  Beside its results each function returns what a test of
+rounded results needs: a bound of the errors of 32-bit steps, formed step by step beside the values.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+
+E32 = 2.0 ** -24   # half a step of fp32, relative
+DEPTH = 64         # additions that a term of a row's sum passes through at most: 32 of a thread, 6 of a wave, 16 of waves
+
+
+def norm(v, dv, kind, eps, weight=None, bias=None):
+    """v [tokens, channels] with absolute errors dv -> the normed rows and their errors; kind "rms" or "layer"."""
+    w = np.ones(v.shape[1]) if weight is None else weight.astype(np.float64)
+    z = np.zeros(v.shape[1]) if bias is None else bias.astype(np.float64)
+    c, dc = v, dv
+    if kind == "layer":
+        m = v.mean(1, keepdims=True)
+        dm = dv.mean(1, keepdims=True) + (DEPTH + 2) * E32 * (np.abs(v) + dv).mean(1, keepdims=True)
+        c, dc = v - m, dv + dm + E32 * (np.abs(v - m) + dv + dm)
+    q = (c * c).mean(1, keepdims=True)
+    dq = (2 * np.abs(c) * dc + dc * dc).mean(1, keepdims=True)
+    dq = dq + (DEPTH + 2) * E32 * (q + dq)
+    k = 1 / np.sqrt(q + eps)
+    dk = 1 / np.sqrt(np.maximum(q - dq, 0) + eps) - k    # (the side on which the root is steeper)
+    dk = dk + 4 * E32 * (k + dk)
+    out = c * k * w + z
+    err = ((np.abs(c) + dc) * (k + dk) - np.abs(c) * k) * np.abs(w)
+    return out, err + 3 * E32 * (np.abs(c * k * w) + err + np.abs(z))
+
+
+def residual_norm(x, residual=None, gate=None, post=None, pre=None, branch_scale=1.0, residual_scale=1.0):
+    """post, pre: None or (kind, eps, weight, bias).  Returns (s, ds, y, dy): the sum before its rounding and the normed sum."""
+    v, dv = x, np.zeros_like(x)
+    if post is not None:
+        v, dv = norm(v, dv, *post)
+    if gate is not None:
+        v, dv = v * gate, dv * np.abs(gate) + E32 * (np.abs(v) + dv) * np.abs(gate)
+    v, dv = v * branch_scale, (dv + E32 * (np.abs(v) + dv)) * abs(branch_scale)
+    if residual is not None:
+        v = v + residual * residual_scale
+        dv = dv + E32 * (np.abs(v) + dv)
+    y, dy = (None, None) if pre is None else norm(v, dv, *pre)
+    return v, dv, y, dy

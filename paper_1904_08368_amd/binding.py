@@ -1,6 +1,6 @@
 """ctypes binding of librelayfused.so: argument marshalling only.
 
-Each function has the name of the C entry point it calls (include/relay_fused.h, include/relay_attention.h) and
+Each function has the name of the C entry point it calls (include/relay_fused.h, include/relay_attention.h, include/relay_decoder.h) and
 takes torch tensors on the GPU purely as (pointer, shape) carriers; PyTorch supplies device
 memory and the stream, every step of the computation runs in the library's own kernels.
 There is no fallback: if the library is missing or a call fails, an exception is raised.
@@ -121,6 +121,7 @@ SIGNATURES = {
     "relay_qdense_w4_packed_bytes": [_P, C.POINTER(_SZ)],
     "relay_prepack_qdense_w4": [_P, _P, _P, _P, _P, _SZ, _P],
     "relay_qdense_w4": [_P, _P, _P, _P, _P, _P, _P],
+    "relay_residual_norm": [_P] * 11,
     "relay_launch_list_create": [_P, C.POINTER(_P)],
     "relay_launch_list_run": [_P, _P],
     "relay_launch_list_destroy": [_P],
@@ -826,6 +827,59 @@ def relay_qdense_w4(d: QDenseW4Desc, x, packed, bias, residual, y) -> None:
     if packed is not None and packed.nbytes < d.packed_bytes:
         raise RelayError(6, f"packed weights of {packed.nbytes} bytes, {d.packed_bytes} needed")
     _check(lib().relay_qdense_w4(C.addressof(d), _ptr(x), _ptr(packed), _ptr(bias), _ptr(residual), _ptr(y), _stream()))
+
+
+# ------------------------------------------------ a decoder's step beside its attention layer
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+
+
+class ResidualNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "channels", "post", "pre")] + \
+        [(n, C.c_float) for n in ("post_eps", "pre_eps", "branch_scale", "residual_scale")] + \
+        [(n, C.c_int64) for n in ("x_stride", "residual_stride", "gate_stride", "sum_stride", "y_stride")]
+
+
+def _row_stride(name, t, like):
+    """Stride of the rows of t [tokens, channels], which has the type and shape of `like`."""
+    if t is None:
+        return like.shape[1]
+    if t.dtype is not like.dtype or t.shape != like.shape or t.stride(1) != 1:
+        raise RelayError(2, f"{name}: {tuple(t.shape)} of {t.dtype} with strides {t.stride()} does not go with x {tuple(like.shape)} of {like.dtype}")
+    return t.stride(0)
+
+
+def residual_norm_desc(x, residual, gate, sum, y, post=NORM_NONE, pre=NORM_RMS, post_eps=1e-5, pre_eps=1e-5, branch_scale=1.0,
+                       residual_scale=1.0) -> ResidualNormDesc:
+    """Descriptor of relay_residual_norm from its tensors, [tokens, channels] with contiguous rows; gate may be [1, channels] (one for all
+    tokens); residual, gate, sum and y may be None."""
+    if x.dim() != 2 or x.stride(1) != 1:
+        raise RelayError(2, f"x must be [tokens, channels] with contiguous rows, not {tuple(x.shape)} with strides {x.stride()}")
+    one = gate is not None and gate.shape[0] == 1 and x.shape[0] != 1
+    gate_stride = _row_stride("gate", gate.expand(x.shape) if one else gate, x)
+    return ResidualNormDesc(dtype_of(x), x.shape[0], x.shape[1], post, pre, post_eps, pre_eps, branch_scale, residual_scale, x.stride(0),
+                            _row_stride("residual", residual, x), gate_stride, _row_stride("sum", sum, x), _row_stride("y", y, x))
+
+
+_FLOAT32 = None
+
+
+def _refuse_floats(name, t, count):
+    """Weights, biases and settings are read as float32, one after another.  What is not that ends here; called where a look at the tensor
+    found it wanting, or where none was taken yet."""
+    global _FLOAT32
+    import torch
+    _FLOAT32 = torch.float32
+    if t.dtype is not _FLOAT32 or t.numel() < count or not t.is_contiguous():
+        raise RelayError(2, f"{name} must be float32, contiguous, of {count} elements, not {tuple(t.shape)} of {t.dtype}")
+
+
+def relay_residual_norm(d: ResidualNormDesc, x, residual, gate, post_weight, post_bias, pre_weight, pre_bias, sum, y) -> None:
+    n = d.channels
+    for name, t in (("post_weight", post_weight), ("post_bias", post_bias), ("pre_weight", pre_weight), ("pre_bias", pre_bias)):
+        if t is not None and (t.dtype is not _FLOAT32 or t.numel() < n or not t.is_contiguous()):
+            _refuse_floats(name, t, n)
+    _check(lib().relay_residual_norm(C.addressof(d), _ptr(x), _ptr(residual), _ptr(gate), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
+                                     _ptr(pre_bias), _ptr(sum), _ptr(y), _stream()))
 
 
 def relay_launch_list_create(hip_graph: int) -> int:

@@ -1,0 +1,66 @@
+// C-ABI layer of a decoder's operators beside its attention layer (relay_decoder.h): argument checks on the host, then dispatch.
+#include <cmath>
+#include <cstring>
+
+#include "../../include/relay_decoder.h"
+#include "api_common.hpp"
+#include "decoder_ops.hpp"
+
+namespace {
+
+using relay::aligned;
+using relay::device_status;
+using relay::fail;
+
+size_t esize(int dtype) { return dtype == RELAY_F32 ? 4 : dtype == RELAY_F16 || dtype == RELAY_BF16 ? 2 : 0; }
+
+// a stride that keeps rows of `what` apart
+bool apart(int64_t stride, int rows, int64_t what) { return rows <= 1 ? stride >= 0 : stride >= what; }
+
+}  // namespace
+
+extern "C" {
+
+relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* x, const void* residual, const void* gate,
+                                 const float* post_weight, const float* post_bias, const float* pre_weight, const float* pre_bias,
+                                 void* sum, void* y, void* hip_stream) {
+  if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
+  const size_t es = esize(d->dtype);
+  if (!es) return fail(RELAY_ERR_DTYPE, "residual norm takes F16, BF16 or F32");
+  if (d->tokens < 0 || d->channels <= 0 || d->channels * es > relay::kNormRowBytes)
+    return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d channels=%d, rows of up to %zu bytes)", d->tokens, d->channels, relay::kNormRowBytes);
+  if (d->post < RELAY_NORM_NONE || d->post > RELAY_NORM_LAYER || d->pre < RELAY_NORM_NONE || d->pre > RELAY_NORM_LAYER)
+    return fail(RELAY_ERR_UNSUPPORTED, "unknown norm (post=%d pre=%d)", d->post, d->pre);
+  // (written so that a NaN is refused)
+  if (!(d->post_eps >= 0) || !(d->pre_eps >= 0) || !std::isfinite(d->post_eps) || !std::isfinite(d->pre_eps) || !std::isfinite(d->branch_scale) ||
+      !std::isfinite(d->residual_scale))
+    return fail(RELAY_ERR_SHAPE, "eps must be at least 0, eps and scales finite");
+  if (d->x_stride < 0 || d->residual_stride < 0 || d->gate_stride < 0 || !apart(d->sum_stride, d->tokens, sum ? d->channels : 0) ||
+      !apart(d->y_stride, d->tokens, y ? d->channels : 0))
+    return fail(RELAY_ERR_SHAPE, "strides must not be negative, those of sum and y not below a row");
+  if (d->tokens == 0) return RELAY_OK;
+  if (!x) return fail(RELAY_ERR_NULL, "x is required");
+  if (!y != (d->pre == RELAY_NORM_NONE)) return fail(RELAY_ERR_NULL, "y must be given exactly if there is a norm of the sum");
+  if (!sum && !y) return fail(RELAY_ERR_NULL, "one of sum and y is required");
+  if ((d->post == RELAY_NORM_NONE && (post_weight || post_bias)) || (d->pre == RELAY_NORM_NONE && (pre_weight || pre_bias)))
+    return fail(RELAY_ERR_UNSUPPORTED, "weights and biases of a norm that is not there");
+  if (!aligned(x, es) || !aligned(residual, es) || !aligned(gate, es) || !aligned(sum, es) || !aligned(y, es) || !aligned(post_weight, 4) ||
+      !aligned(post_bias, 4) || !aligned(pre_weight, 4) || !aligned(pre_bias, 4))
+    return fail(RELAY_ERR_ALIGN, "tensors must be aligned to their type");
+  if (sum == y) return fail(RELAY_ERR_UNSUPPORTED, "sum and y must not alias each other");
+  // a row is read whole by the threads that write it, so an output may stand where an input does, row on row
+  const struct { const void* in; int64_t stride; } inputs[] = {{x, d->x_stride}, {residual, d->residual_stride}, {gate, d->gate_stride}};
+  for (const auto& i : inputs)
+    if (i.in && d->tokens > 1 && ((i.in == sum && i.stride != d->sum_stride) || (i.in == y && i.stride != d->y_stride)))
+      return fail(RELAY_ERR_UNSUPPORTED, "an output in the place of an input needs its stride");
+  relay::NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = d->tokens; a.channels = d->channels; a.post = d->post; a.pre = d->pre;
+  a.post_eps = d->post_eps; a.pre_eps = d->pre_eps; a.branch_scale = d->branch_scale; a.residual_scale = d->residual_scale;
+  a.x = x; a.res = residual; a.gate = gate; a.sum = sum; a.y = y;
+  a.post_weight = post_weight; a.post_bias = post_bias; a.pre_weight = pre_weight; a.pre_bias = pre_bias;
+  a.x_stride = d->x_stride; a.res_stride = d->residual_stride; a.gate_stride = d->gate_stride; a.sum_stride = d->sum_stride; a.y_stride = d->y_stride;
+  return device_status(relay::launch_residual_norm(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "residual norm launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,31 @@
+// Internal interface between the C-ABI layer of a decoder's operators (api_decoder.cpp) and their gfx950 kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "attention.hpp"
+
+namespace relay {
+
+enum : int { N_NONE = 0, N_RMS = 1, N_LAYER = 2 };  // RELAY_NORM_*
+
+struct NormArgs {
+  int tokens, channels;
+  int post, pre;
+  float post_eps, pre_eps, branch_scale, residual_scale;
+  const void* x;
+  const void* res;
+  const void* gate;
+  const float* post_weight;
+  const float* post_bias;
+  const float* pre_weight;
+  const float* pre_bias;
+  void* sum;
+  void* y;
+  int64_t x_stride, res_stride, gate_stride, sum_stride, y_stride;
+};
+constexpr size_t kNormRowBytes = 65536;   // what a workgroup's registers hold of a row
+hipError_t launch_residual_norm(const NormArgs& a, int dtype, hipStream_t st);
+
+}  // namespace relay

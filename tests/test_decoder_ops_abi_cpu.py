@@ -1,0 +1,81 @@
+"""The entry points of a decoder's operators beside its attention layer without a GPU: what they refuse, with which status, before any HIP call; calls
+that launch nothing; tensors that a descriptor cannot describe."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_1904_08368_amd import binding as B
+
+FAKE = 0x7F0000001000            # a non-NULL, 4096-byte aligned address that is never dereferenced
+at = lambda i: FAKE + (i << 24)
+
+
+def _status(fn, *args):
+    return getattr(B.lib(), fn)(*args)
+
+
+def _with(d, **kw):
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return C.byref(d)
+
+
+# ---------------------------------------------------------------------------------- norms
+def _norm(**kw):
+    return _with(B.ResidualNormDesc(B.RELAY_F16, 4, 64, B.NORM_RMS, B.NORM_LAYER, 1e-5, 1e-5, 1.0, 1.0, 64, 64, 0, 64, 64), **kw)
+
+
+def _call_norm(d, **kw):
+    names = ("x", "residual", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias", "sum", "y")
+    return _status("relay_residual_norm", d, *[kw.get(n, at(i)) for i, n in enumerate(names)], None)
+
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=B.RELAY_I8), 3), (dict(dtype=7), 3), (dict(tokens=-1), 2), (dict(channels=0), 2), (dict(channels=32769), 2),
+    (dict(dtype=B.RELAY_F32, channels=16385), 2), (dict(post=3), 4), (dict(pre=-1), 4), (dict(post_eps=-1e-6), 2), (dict(pre_eps=NAN), 2),
+    (dict(post_eps=INF), 2), (dict(branch_scale=INF), 2), (dict(residual_scale=NAN), 2), (dict(x_stride=-1), 2), (dict(residual_stride=-64), 2),
+    (dict(gate_stride=-1), 2), (dict(sum_stride=63), 2), (dict(y_stride=0), 2)])
+def test_norm_refuses(kw, status):
+    assert _call_norm(_norm(**kw)) == status and B.lib().relay_last_error()
+
+
+def test_norm_pointers():
+    assert _call_norm(None) == 1
+    assert _call_norm(_norm(), x=None) == 1
+    assert _call_norm(_norm(), y=None) == 1                                                  # a norm without a place for it
+    assert _call_norm(_norm(pre=B.NORM_NONE), pre_weight=None, pre_bias=None) == 1           # ... and a place without a norm
+    assert _call_norm(_norm(pre=B.NORM_NONE), pre_weight=None, pre_bias=None, y=None, sum=None) == 1
+    assert _call_norm(_norm(pre=B.NORM_NONE), pre_bias=None, y=None) == 4                    # a weight without its norm
+    assert _call_norm(_norm(post=B.NORM_NONE)) == 4
+    for name in ("x", "residual", "gate", "post_weight", "post_bias", "pre_weight", "pre_bias", "sum", "y"):
+        assert _call_norm(_norm(), **{name: at(20) + 1}) == 5
+    assert _call_norm(_norm(), post_weight=at(20) + 2) == 5
+    assert _call_norm(_norm(), sum=at(8)) == 4                                               # one place for both outputs
+    assert _call_norm(_norm(x_stride=128), sum=at(0)) == 4                                   # in place with other strides
+    assert _call_norm(_norm(), y=at(2)) == 4                                                 # in place of a gate that all tokens share
+    assert _call_norm(_norm(tokens=0), x=None, y=None, sum=None) == 0
+
+
+def _f16(*shape):
+    return torch.zeros(shape, dtype=torch.float16)
+
+
+def test_norm_descriptors():
+    x = _f16(4, 64)
+    d = B.residual_norm_desc(x, x, _f16(1, 64), None, x)
+    assert (d.gate_stride, d.x_stride, d.sum_stride) == (0, 64, 64)
+    assert B.residual_norm_desc(x, None, _f16(4, 128)[:, :64], x, None).gate_stride == 128
+    for bad in (lambda: B.residual_norm_desc(x.t(), None, None, None, x.t()), lambda: B.residual_norm_desc(x, x.float(), None, None, x),
+                lambda: B.residual_norm_desc(x, _f16(4, 65), None, None, x), lambda: B.residual_norm_desc(x, None, None, _f16(3, 64), x),
+                lambda: B.residual_norm_desc(x, None, None, None, _f16(64, 4).t()), lambda: B.residual_norm_desc(x.int(), None, None, None, x.int()),
+                lambda: B.residual_norm_desc(x, None, _f16(2, 64), None, x), lambda: B.residual_norm_desc(x[0], None, None, None, x[0])):
+        with pytest.raises((B.RelayError, RuntimeError)):
+            bad()
+    w = torch.ones(64)
+    for bad in (w.double(), w[:63], torch.ones(128)[::2], w.half()):
+        with pytest.raises(B.RelayError):
+            B.relay_residual_norm(d, x, x, None, None, None, bad, None, None, x)
