@@ -45,6 +45,32 @@ relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* 
                                  const float* post_weight, const float* post_bias, const float* pre_weight, const float* pre_bias,
                                  void* sum, void* y, void* hip_stream);
 
+/* ---- the next token --------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t dtype;              /* of the logits: RELAY_F16, RELAY_BF16 or RELAY_F32 */
+  int32_t rows, vocab;        /* vocab 1 .. 2^20 */
+  int64_t logits_stride;
+} relay_sample_desc;
+
+/* One token of each row, in one primitive function from the logits (paper Section 4.1).  With w_i = exp((l_i - max l) / temperature), tokens in descending order of their logits, equal ones in the order of their numbers:
+ *   top_k:  the first top_k of them                                       (0 or less: all)
+ *   top_p:  of these the shortest run from the first on whose w add up to at least top_p times the sum over them   (1 or more: all)
+ *   min_p:  of these the ones with w >= min_p                              (0 or less: all)
+ * the first is always kept, and the token is the first kept one at which the running sum of w exceeds uniform times the sum over the kept.
+ * temperature 0 (or less): the first.  uniform: in 0 <= u < 1 (less counts as 0, more as the number before 1).  A setting that is NaN is off, a NaN temperature is 1, a NaN uniform 0.
+ * A logit that is NaN counts as -infinity; tokens of -infinity are never named.  A row without any other gets token -1 and probability 0; a
+ * logit of +infinity shares the row with its like.
+ * Weights are evaluated in 64 bits and added up as integers, as multiples of 2^-62 vocab (vocab rounded up to a power of two; 2^-51 where that is more) of the
+ * largest, so that a result does not depend on the order of a sum; a weight below half of that is zero.
+ *   logits [rows][vocab], any alignment of the type; temperature, top_p, min_p fp32, top_k int32, each [rows] or NULL (1, all, all, all); uniform
+ *   fp32 [rows], or NULL: the first of each row
+ *   tokens int32 [rows]; probs fp32 [rows] or NULL: w of the token over the sum of w over the kept
+ * Workspace: NULL is valid (few rows then take longer).  Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (aliasing), _WORKSPACE, _DEVICE. */
+relay_status relay_sample_workspace_bytes(const relay_sample_desc* d, size_t* bytes);
+relay_status relay_sample(const relay_sample_desc* d, const void* logits, const float* temperature, const int32_t* top_k, const float* top_p,
+                          const float* min_p, const float* uniform, int32_t* tokens, float* probs, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

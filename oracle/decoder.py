@@ -46,3 +46,30 @@ def residual_norm(x, residual=None, gate=None, post=None, pre=None, branch_scale
         dv = dv + E32 * (np.abs(v) + dv)
     y, dy = (None, None) if pre is None else norm(v, dv, *pre)
     return v, dv, y, dy
+
+
+def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, uniform=0.0):
+    """One row: the token, its probability among the kept, and how many are kept."""
+    l = np.where(np.isnan(logits), -np.inf, logits)
+    if not (l > -np.inf).any():
+        return -1, 0.0, 0
+    order = np.argsort(-l, kind="stable")
+    if math.isnan(temperature):
+        temperature = 1.0
+    if temperature <= 0:
+        return int(order[0]), 1.0, 1
+    d = np.where(l[order] == l[order[0]], 0.0, l[order] - (l[order[0]] if np.isfinite(l[order[0]]) else np.finfo(np.float64).max))
+    with np.errstate(under="ignore"):
+        w = np.where(np.isneginf(d), 0.0, np.exp(np.where(np.isneginf(d), 0.0, d / temperature)))
+    n = len(w)
+    if 0 < top_k < n:
+        n = top_k
+    if top_p < 1:
+        mass = np.cumsum(w[:n])
+        n = int(np.searchsorted(mass, top_p * mass[-1], side="left")) + 1 if top_p > 0 else 1
+    if min_p > 0:
+        n = max(1, min(n, int((w >= min(min_p, 1.0)).sum())))
+    cum = np.cumsum(w[:n])
+    u = 0.0 if math.isnan(uniform) else min(max(uniform, 0.0), 1 - 2.0 ** -24)
+    at = int(np.searchsorted(cum, u * cum[-1], side="right"))
+    return int(order[at]), float(w[at] / cum[-1]), n

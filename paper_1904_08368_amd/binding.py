@@ -122,6 +122,8 @@ SIGNATURES = {
     "relay_prepack_qdense_w4": [_P, _P, _P, _P, _P, _SZ, _P],
     "relay_qdense_w4": [_P, _P, _P, _P, _P, _P, _P],
     "relay_residual_norm": [_P] * 11,
+    "relay_sample_workspace_bytes": [_P, C.POINTER(_SZ)],
+    "relay_sample": [_P] * 10 + [_SZ, _P],
     "relay_launch_list_create": [_P, C.POINTER(_P)],
     "relay_launch_list_run": [_P, _P],
     "relay_launch_list_destroy": [_P],
@@ -880,6 +882,37 @@ def relay_residual_norm(d: ResidualNormDesc, x, residual, gate, post_weight, pos
             _refuse_floats(name, t, n)
     _check(lib().relay_residual_norm(C.addressof(d), _ptr(x), _ptr(residual), _ptr(gate), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
                                      _ptr(pre_bias), _ptr(sum), _ptr(y), _stream()))
+
+
+class SampleDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "vocab")] + [("logits_stride", C.c_int64)]
+
+
+def sample_desc(logits) -> SampleDesc:
+    """Descriptor of relay_sample from its logits [rows, vocab] with contiguous rows."""
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise RelayError(2, f"logits must be [rows, vocab] with contiguous rows, not {tuple(logits.shape)} with strides {logits.stride()}")
+    return SampleDesc(dtype_of(logits), logits.shape[0], logits.shape[1], logits.stride(0))
+
+
+def relay_sample_workspace_bytes(d: SampleDesc) -> int:
+    b = _SZ()
+    _check(lib().relay_sample_workspace_bytes(C.addressof(d), C.byref(b)))
+    return b.value
+
+
+def relay_sample(d: SampleDesc, logits, temperature, top_k, top_p, min_p, uniform, tokens, probs=None, workspace=None) -> None:
+    n = d.rows
+    for name, t in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p), ("uniform", uniform), ("probs", probs)):
+        if t is not None and (t.dtype is not _FLOAT32 or t.numel() < n or not t.is_contiguous()):
+            _refuse_floats(name, t, n)
+    if top_k is not None and (top_k.dtype is not _INT32 or top_k.numel() < n or not top_k.is_contiguous()):
+        _refuse_index("top_k", top_k, n)
+    if tokens is None or tokens.dtype is not _INT32 or tokens.numel() < n or not tokens.is_contiguous():
+        _refuse_index("tokens", tokens, n)
+    ws_bytes = 0 if workspace is None else workspace.nbytes
+    _check(lib().relay_sample(C.addressof(d), _ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(tokens),
+                              _ptr(probs), workspace.data_ptr() if ws_bytes else None, ws_bytes, _stream()))
 
 
 def relay_launch_list_create(hip_graph: int) -> int:

@@ -28,4 +28,20 @@ struct NormArgs {
 constexpr size_t kNormRowBytes = 65536;   // what a workgroup's registers hold of a row
 hipError_t launch_residual_norm(const NormArgs& a, int dtype, hipStream_t st);
 
+struct SampleArgs {
+  int rows, vocab;
+  int64_t logits_stride;
+  const void* logits;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniform;
+  int32_t* tokens;
+  float* probs;
+  int scale_bits;   // set by the launcher
+};
+constexpr int kVocab = 1 << 20;
+hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
+
 }  // namespace relay

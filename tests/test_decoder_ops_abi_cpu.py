@@ -79,3 +79,45 @@ def test_norm_descriptors():
     for bad in (w.double(), w[:63], torch.ones(128)[::2], w.half()):
         with pytest.raises(B.RelayError):
             B.relay_residual_norm(d, x, x, None, None, None, bad, None, None, x)
+
+
+# ------------------------------------------------------------------------------- sampling
+def _sample(**kw):
+    return _with(B.SampleDesc(B.RELAY_BF16, 3, 100, 100), **kw)
+
+
+def _call_sample(d, ws=None, ws_bytes=0, **kw):
+    names = ("logits", "temperature", "top_k", "top_p", "min_p", "uniform", "tokens", "probs")
+    return _status("relay_sample", d, *[kw.get(n, at(i)) for i, n in enumerate(names)], ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [(dict(dtype=B.RELAY_I8), 3), (dict(rows=-1), 2), (dict(vocab=0), 2), (dict(vocab=(1 << 20) + 1), 2), (dict(logits_stride=-1), 2)])
+def test_sample_refuses(kw, status):
+    b = C.c_size_t()
+    assert _call_sample(_sample(**kw)) == status
+    assert _status("relay_sample_workspace_bytes", _sample(**kw), C.byref(b)) == status
+
+
+def test_sample_pointers():
+    assert _call_sample(None) == 1 and _call_sample(_sample(), logits=None) == 1 and _call_sample(_sample(), tokens=None) == 1
+    assert _status("relay_sample_workspace_bytes", _sample(), None) == 1
+    for name in ("logits", "temperature", "top_k", "top_p", "min_p", "uniform", "tokens", "probs"):
+        assert _call_sample(_sample(), **{name: at(20) + 1}) == 5
+    assert _call_sample(_sample(), tokens=at(0)) == 4 and _call_sample(_sample(), probs=at(6)) == 4 and _call_sample(_sample(), probs=at(0)) == 4
+    assert _call_sample(_sample(rows=0), logits=None, tokens=None) == 0
+
+
+def test_sample_operands():
+    l = torch.zeros(3, 100)
+    d = B.sample_desc(l)
+    assert (d.rows, d.vocab, d.logits_stride) == (3, 100, 100) and B.sample_desc(torch.zeros(3, 128)[:, :100]).logits_stride == 128
+    for bad in (l.t(), l[0], l.int()):
+        with pytest.raises(B.RelayError):
+            B.sample_desc(bad)
+    good = dict(temperature=torch.ones(3), top_k=torch.ones(3, dtype=torch.int32), top_p=torch.ones(3), min_p=torch.ones(3), uniform=torch.ones(3),
+                tokens=torch.zeros(3, dtype=torch.int32), probs=torch.zeros(3))
+    for name, bad in (("temperature", torch.ones(2)), ("top_k", torch.ones(3)), ("top_k", torch.ones(3, dtype=torch.int64)), ("top_p", torch.ones(3).half()),
+                      ("min_p", torch.ones(6)[::2]), ("uniform", torch.ones(3).double()), ("tokens", torch.zeros(3, dtype=torch.int64)),
+                      ("tokens", torch.zeros(2, dtype=torch.int32)), ("tokens", None), ("probs", torch.zeros(2))):
+        with pytest.raises(B.RelayError):
+            B.relay_sample(d, l, **{**good, name: bad})
