@@ -45,6 +45,30 @@ relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* 
                                  const float* post_weight, const float* post_bias, const float* pre_weight, const float* pre_bias,
                                  void* sum, void* y, void* hip_stream);
 
+/* ---- the router of a mixture of experts ------------------------------------------------------------------------- */
+enum { RELAY_SCORE_SOFTMAX = 0, RELAY_SCORE_SIGMOID = 1 };
+
+typedef struct {
+  int32_t dtype;              /* of x and w: RELAY_F16 or RELAY_BF16 */
+  int32_t tokens, channels;   /* channels a multiple of 8 */
+  int32_t experts, top_k;     /* 1 .. 1024; 1 .. min(experts, 64) */
+  int32_t score;              /* RELAY_SCORE_* */
+  int32_t normalize;          /* 1: the weights of a token's experts add up to `scale` */
+  float scale;
+  int64_t x_stride;
+} relay_route_desc;
+
+/* The router's product, scores and choice as one primitive function (paper Section 4.1).  chosen[t] = the top_k experts of token t with the largest score + bias, weights[t] = their scores (without bias) [/ their sum] * scale, where
+ *   l = w x,   score = softmax(l) over the experts, or 1 / (1 + exp(-l)) each
+ * The largest comes first, equal ones in the order of their numbers; a NaN counts as less than everything.  Products, sums and scores are 64-bit, so that a choice does not hang on
+ * the order of a sum; weights are rounded once, to fp32.  A sum of zero leaves weights of zero.
+ *   x [tokens][channels], 16-byte aligned with x_stride a multiple of 8; w [experts][channels], 16-byte aligned; bias fp32 [experts] or NULL
+ *   chosen int32, weights fp32 [tokens][top_k]
+ * Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED, _WORKSPACE (the workspace is required), _DEVICE. */
+relay_status relay_route_workspace_bytes(const relay_route_desc* d, size_t* bytes);
+relay_status relay_route(const relay_route_desc* d, const void* x, const void* w, const float* bias, int32_t* chosen, float* weights,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ---- the next token --------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype;              /* of the logits: RELAY_F16, RELAY_BF16 or RELAY_F32 */

@@ -48,6 +48,24 @@ def residual_norm(x, residual=None, gate=None, post=None, pre=None, branch_scale
     return v, dv, y, dy
 
 
+def route(x, w, top_k, score="softmax", bias=None, normalize=True, scale=1.0):
+    """chosen and weights [tokens, top_k]."""
+    l = x @ w.T
+    if score == "softmax":
+        s = np.exp(l - l.max(1, keepdims=True))
+        s /= s.sum(1, keepdims=True)
+    else:
+        with np.errstate(over="ignore"):
+            s = 1 / (1 + np.exp(-l))
+    by = s if bias is None else s + bias.astype(np.float64)
+    chosen = np.argsort(-by, axis=1, kind="stable")[:, :top_k]
+    weights = np.take_along_axis(s, chosen, 1)
+    if normalize:
+        total = weights.sum(1, keepdims=True)
+        weights = np.where(total == 0, 0.0, weights / np.where(total == 0, 1.0, total))
+    return chosen, weights * scale
+
+
 def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, uniform=0.0):
     """One row: the token, its probability among the kept, and how many are kept."""
     l = np.where(np.isnan(logits), -np.inf, logits)

@@ -122,6 +122,8 @@ SIGNATURES = {
     "relay_prepack_qdense_w4": [_P, _P, _P, _P, _P, _SZ, _P],
     "relay_qdense_w4": [_P, _P, _P, _P, _P, _P, _P],
     "relay_residual_norm": [_P] * 11,
+    "relay_route_workspace_bytes": [_P, C.POINTER(_SZ)],
+    "relay_route": [_P] * 7 + [_SZ, _P],
     "relay_sample_workspace_bytes": [_P, C.POINTER(_SZ)],
     "relay_sample": [_P] * 10 + [_SZ, _P],
     "relay_launch_list_create": [_P, C.POINTER(_P)],
@@ -833,6 +835,7 @@ def relay_qdense_w4(d: QDenseW4Desc, x, packed, bias, residual, y) -> None:
 
 # ------------------------------------------------ a decoder's step beside its attention layer
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 
 class ResidualNormDesc(C.Structure):
@@ -871,6 +874,8 @@ def _refuse_floats(name, t, count):
     global _FLOAT32
     import torch
     _FLOAT32 = torch.float32
+    if t is None:
+        raise RelayError(1, f"{name} is required")
     if t.dtype is not _FLOAT32 or t.numel() < count or not t.is_contiguous():
         raise RelayError(2, f"{name} must be float32, contiguous, of {count} elements, not {tuple(t.shape)} of {t.dtype}")
 
@@ -882,6 +887,37 @@ def relay_residual_norm(d: ResidualNormDesc, x, residual, gate, post_weight, pos
             _refuse_floats(name, t, n)
     _check(lib().relay_residual_norm(C.addressof(d), _ptr(x), _ptr(residual), _ptr(gate), _ptr(post_weight), _ptr(post_bias), _ptr(pre_weight),
                                      _ptr(pre_bias), _ptr(sum), _ptr(y), _stream()))
+
+
+class RouteDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "channels", "experts", "top_k", "score", "normalize")] + \
+        [("scale", C.c_float), ("x_stride", C.c_int64)]
+
+
+def route_desc(x, w, chosen, score=SCORE_SOFTMAX, normalize=True, scale=1.0) -> RouteDesc:
+    """Descriptor of relay_route from its tensors: x [tokens, channels] with contiguous rows, w [experts, channels], chosen [tokens, top_k]."""
+    if x.dim() != 2 or x.stride(1) != 1 or w.dim() != 2 or w.shape[1] != x.shape[1] or w.dtype is not x.dtype or not w.is_contiguous() or \
+            chosen.dim() != 2 or chosen.shape[0] != x.shape[0]:
+        raise RelayError(2, f"x {tuple(x.shape)} of {x.dtype}, w {tuple(w.shape)} of {w.dtype} and chosen {tuple(chosen.shape)} do not go together")
+    return RouteDesc(dtype_of(x), x.shape[0], x.shape[1], w.shape[0], chosen.shape[1], score, 1 if normalize else 0, scale, x.stride(0))
+
+
+def relay_route_workspace_bytes(d: RouteDesc) -> int:
+    b = _SZ()
+    _check(lib().relay_route_workspace_bytes(C.addressof(d), C.byref(b)))
+    return b.value
+
+
+def relay_route(d: RouteDesc, x, w, bias, chosen, weights, workspace) -> None:
+    n = d.tokens * d.top_k
+    if bias is not None and (bias.dtype is not _FLOAT32 or bias.numel() < d.experts or not bias.is_contiguous()):
+        _refuse_floats("bias", bias, d.experts)
+    if chosen is None or chosen.dtype is not _INT32 or chosen.numel() < n or not chosen.is_contiguous():
+        _refuse_index("chosen", chosen, n)
+    if weights is None or weights.dtype is not _FLOAT32 or weights.numel() < n or not weights.is_contiguous():
+        _refuse_floats("weights", weights, n)
+    _check(lib().relay_route(C.addressof(d), _ptr(x), _ptr(w), _ptr(bias), chosen.data_ptr(), weights.data_ptr(), _ptr(workspace),
+                             0 if workspace is None else workspace.nbytes, _stream()))
 
 
 class SampleDesc(C.Structure):

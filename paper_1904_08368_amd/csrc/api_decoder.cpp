@@ -17,6 +17,12 @@ size_t esize(int dtype) { return dtype == RELAY_F32 ? 4 : dtype == RELAY_F16 || 
 // a stride that keeps rows of `what` apart
 bool apart(int64_t stride, int rows, int64_t what) { return rows <= 1 ? stride >= 0 : stride >= what; }
 
+relay_status check_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (!workspace || bytes < need) return fail(RELAY_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? bytes : 0, need);
+  if (!aligned(workspace, 256)) return fail(RELAY_ERR_ALIGN, "workspace must be 256-byte aligned");
+  return RELAY_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -61,6 +67,50 @@ relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* 
   a.post_weight = post_weight; a.post_bias = post_bias; a.pre_weight = pre_weight; a.pre_bias = pre_bias;
   a.x_stride = d->x_stride; a.res_stride = d->residual_stride; a.gate_stride = d->gate_stride; a.sum_stride = d->sum_stride; a.y_stride = d->y_stride;
   return device_status(relay::launch_residual_norm(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "residual norm launch");
+}
+
+static relay_status route_args(const relay_route_desc* d, relay::RouteArgs* out) {
+  if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
+  if (d->dtype != RELAY_F16 && d->dtype != RELAY_BF16) return fail(RELAY_ERR_DTYPE, "the router takes F16 or BF16");
+  if (d->tokens < 0 || d->channels <= 0 || d->experts <= 0 || d->experts > relay::kRouteExperts)
+    return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d channels=%d experts=%d, experts in 1 .. %d)", d->tokens, d->channels, d->experts, relay::kRouteExperts);
+  if (d->top_k <= 0 || d->top_k > d->experts || d->top_k > relay::kRouteTopK)
+    return fail(RELAY_ERR_SHAPE, "top_k=%d must be in 1 .. min(experts, %d)", d->top_k, relay::kRouteTopK);
+  if (d->channels % 8) return fail(RELAY_ERR_ALIGN, "channels=%d must be a multiple of 8", d->channels);
+  if (d->score != RELAY_SCORE_SOFTMAX && d->score != RELAY_SCORE_SIGMOID) return fail(RELAY_ERR_UNSUPPORTED, "unknown score %d", d->score);
+  if (d->normalize != 0 && d->normalize != 1) return fail(RELAY_ERR_UNSUPPORTED, "normalize=%d (0 or 1)", d->normalize);
+  if (!std::isfinite(d->scale)) return fail(RELAY_ERR_SHAPE, "scale must be finite");
+  if (d->x_stride < 0) return fail(RELAY_ERR_SHAPE, "x_stride must not be negative");
+  if (d->x_stride % 8) return fail(RELAY_ERR_ALIGN, "x_stride must be a multiple of 8");
+  relay::RouteArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = d->tokens; a.channels = d->channels; a.experts = d->experts; a.top_k = d->top_k; a.score = d->score; a.normalize = d->normalize;
+  a.scale = d->scale; a.x_stride = d->x_stride;
+  *out = a;
+  return RELAY_OK;
+}
+
+relay_status relay_route_workspace_bytes(const relay_route_desc* d, size_t* bytes) {
+  if (!bytes) return fail(RELAY_ERR_NULL, "bytes is NULL");
+  relay::RouteArgs a;
+  if (relay_status st = route_args(d, &a)) return st;
+  *bytes = a.tokens ? relay::route_workspace_bytes(a) : 0;
+  return RELAY_OK;
+}
+
+relay_status relay_route(const relay_route_desc* d, const void* x, const void* w, const float* bias, int32_t* chosen, float* weights,
+                         void* workspace, size_t workspace_bytes, void* hip_stream) {
+  relay::RouteArgs a;
+  if (relay_status st = route_args(d, &a)) return st;
+  if (a.tokens == 0) return RELAY_OK;
+  if (!x || !w || !chosen || !weights) return fail(RELAY_ERR_NULL, "x, w, chosen and weights are required");
+  if (!aligned(x, 16) || !aligned(w, 16)) return fail(RELAY_ERR_ALIGN, "x and w must be 16-byte aligned");
+  if (!aligned(bias, 4) || !aligned(chosen, 4) || !aligned(weights, 4)) return fail(RELAY_ERR_ALIGN, "bias, chosen and weights must be aligned to their type");
+  if (static_cast<const void*>(chosen) == weights || chosen == x || weights == x || chosen == w || weights == w || (bias && (weights == bias || static_cast<const void*>(chosen) == bias)))
+    return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
+  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_bytes(a))) return st;
+  a.x = x; a.w = w; a.bias = bias; a.chosen = chosen; a.weights = weights; a.workspace = workspace;
+  return device_status(relay::launch_route(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "router launch");
 }
 
 static relay_status check_sample(const relay_sample_desc* d) {

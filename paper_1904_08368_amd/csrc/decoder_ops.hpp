@@ -28,6 +28,25 @@ struct NormArgs {
 constexpr size_t kNormRowBytes = 65536;   // what a workgroup's registers hold of a row
 hipError_t launch_residual_norm(const NormArgs& a, int dtype, hipStream_t st);
 
+enum : int { S_SOFTMAX = 0, S_SIGMOID = 1 };  // RELAY_SCORE_*
+
+struct RouteArgs {
+  int tokens, channels, experts, top_k, score, normalize;
+  float scale;
+  int64_t x_stride;
+  const void* x;
+  const void* w;
+  const float* bias;
+  int32_t* chosen;
+  float* weights;
+  void* workspace;
+  unsigned* counters;   // set by the launcher, as is
+  double* logits;       // [tokens][experts]
+};
+constexpr int kRouteExperts = 1024, kRouteTopK = 64;
+size_t route_workspace_bytes(const RouteArgs& a);
+hipError_t launch_route(const RouteArgs& a, int dtype, hipStream_t st);
+
 struct SampleArgs {
   int rows, vocab;
   int64_t logits_stride;

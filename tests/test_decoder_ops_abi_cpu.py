@@ -121,3 +121,50 @@ def test_sample_operands():
                       ("tokens", torch.zeros(2, dtype=torch.int32)), ("tokens", None), ("probs", torch.zeros(2))):
         with pytest.raises(B.RelayError):
             B.relay_sample(d, l, **{**good, name: bad})
+
+
+# -------------------------------------------------------------------------------- routing
+def _route(**kw):
+    return _with(B.RouteDesc(B.RELAY_F16, 5, 64, 8, 2, B.SCORE_SOFTMAX, 1, 1.0, 64), **kw)
+
+
+def _call_route(d, ws=at(9), ws_bytes=1 << 30, **kw):
+    names = ("x", "w", "bias", "chosen", "weights")
+    return _status("relay_route", d, *[kw.get(n, at(i)) for i, n in enumerate(names)], ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=B.RELAY_F32), 3), (dict(tokens=-1), 2), (dict(channels=0), 2), (dict(channels=60), 5), (dict(experts=0), 2), (dict(experts=1025), 2),
+    (dict(top_k=0), 2), (dict(top_k=9), 2), (dict(experts=100, top_k=65), 2), (dict(score=2), 4), (dict(normalize=2), 4), (dict(scale=INF), 2), (dict(scale=NAN), 2),
+    (dict(x_stride=-8), 2), (dict(x_stride=68), 5)])
+def test_route_refuses(kw, status):
+    b = C.c_size_t()
+    assert _call_route(_route(**kw)) == status
+    assert _status("relay_route_workspace_bytes", _route(**kw), C.byref(b)) == status
+
+
+def test_route_pointers():
+    b = C.c_size_t()
+    assert _call_route(None) == 1 and _status("relay_route_workspace_bytes", _route(), None) == 1
+    for name in ("x", "w", "chosen", "weights"):
+        assert _call_route(_route(), **{name: None}) == 1
+    for name, off in (("x", 8), ("w", 8), ("bias", 2), ("chosen", 2), ("weights", 2)):
+        assert _call_route(_route(), **{name: at(20) + off}) == 5
+    for name, other in (("chosen", 4), ("weights", 2), ("chosen", 0), ("weights", 1)):
+        assert _call_route(_route(), **{name: at(other)}) == 4
+    assert _status("relay_route_workspace_bytes", _route(), C.byref(b)) == 0 and b.value > 0
+    assert _call_route(_route(), ws=None) == 6 and _call_route(_route(), ws_bytes=b.value - 1) == 6 and _call_route(_route(), ws=at(9) + 128) == 5
+    assert _call_route(_route(tokens=0), ws=None, x=None, w=None, chosen=None, weights=None) == 0
+
+
+def test_route_operands():
+    x, w, chosen, weights = _f16(5, 64), _f16(8, 64), torch.zeros(5, 2, dtype=torch.int32), torch.zeros(5, 2)
+    d = B.route_desc(x, w, chosen)
+    assert (d.tokens, d.channels, d.experts, d.top_k, d.x_stride) == (5, 64, 8, 2, 64)
+    for bad in (lambda: B.route_desc(x, w.float(), chosen), lambda: B.route_desc(x, _f16(8, 72), chosen), lambda: B.route_desc(x, _f16(64, 8).t(), chosen),
+                lambda: B.route_desc(x, w, chosen[:4]), lambda: B.route_desc(_f16(64, 5).t(), w, chosen),
+                lambda: B.relay_route(d, x, w, torch.zeros(7), chosen, weights, None), lambda: B.relay_route(d, x, w, None, chosen.long(), weights, None),
+                lambda: B.relay_route(d, x, w, None, chosen, weights.half(), None), lambda: B.relay_route(d, x, w, None, chosen, weights[:4], None),
+                lambda: B.relay_route(d, x, w, None, chosen, None, None), lambda: B.relay_route(d, x, w, None, None, weights, None)):
+        with pytest.raises(B.RelayError):
+            bad()
