@@ -69,6 +69,36 @@ relay_status relay_route_workspace_bytes(const relay_route_desc* d, size_t* byte
 relay_status relay_route(const relay_route_desc* d, const void* x, const void* w, const float* bias, int32_t* chosen, float* weights,
                          void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- the experts ------------------------------------------------------------------------------------------------ */
+enum { RELAY_ACT_SILU = 0, RELAY_ACT_GELU = 1 };   /* v / (1 + exp(-v));  v (1 + erf(v / sqrt 2)) / 2 */
+
+typedef struct {
+  int32_t dtype;              /* of x, y, the scales and the residual: RELAY_F16 or RELAY_BF16 */
+  int32_t tokens, top_k;      /* top_k 1 .. 64 */
+  int32_t channels, inter;    /* multiples of 16 */
+  int32_t experts;            /* 1 .. 1024 */
+  int32_t group, has_zeros;   /* of the 4-bit weights, as of relay_qdense_w4_desc */
+  int32_t act;                /* RELAY_ACT_* */
+  uint32_t flags;             /* RELAY_HAS_RESIDUAL */
+  int64_t x_stride, y_stride; /* of the rows of x; of y and of the residual */
+} relay_experts_w4_desc;
+
+/* y[t] = sum_s weights[t][s] * down_e (act(gate_e x[t]) * up_e x[t])  [+ residual[t]],   e = chosen[t][s]
+ * for few tokens, where the chosen experts' codes are most of what there is to read: each is read once for all the tokens that chose it.
+ * weights * act * up is rounded to the tensors' type for the second product (an operand of the matrix cores); sums are fp32, in a fixed order.
+ * Three launches: what is elementwise goes into the products' ends (paper Section 4.1), scales behind the
+ * quantized operands (Section 4.2).
+ * gate_up and down are packed by relay_prepack_qdense_w4 with the experts' units one behind the other:
+ *   gate_up: n = experts * 2 * inter, k = channels, an expert's gates ahead of its other units;   down: n = experts * channels, k = inter
+ * An entry of chosen outside 0 .. experts-1 adds nothing (a padding token has all of them -1 and gets its residual, or zeros); an
+ * expert named twice by a token counts twice.
+ *   x [tokens][channels], 16-byte aligned with x_stride a multiple of 8; y, residual [tokens][channels] of any alignment of the type; chosen int32,
+ *   weights fp32 [tokens][top_k].  y may be the residual; it must not overlap x.
+ * Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (act, flags, aliasing), _WORKSPACE (the workspace is required), _DEVICE. */
+relay_status relay_experts_w4_workspace_bytes(const relay_experts_w4_desc* d, size_t* bytes);
+relay_status relay_experts_w4(const relay_experts_w4_desc* d, const void* x, const int32_t* chosen, const float* weights, const void* gate_up,
+                              const void* down, const void* residual, void* y, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ---- the next token --------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t dtype;              /* of the logits: RELAY_F16, RELAY_BF16 or RELAY_F32 */

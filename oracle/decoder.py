@@ -9,6 +9,8 @@ import math
 
 import numpy as np
 
+from . import attention
+
 E32 = 2.0 ** -24   # half a step of fp32, relative
 DEPTH = 64         # additions that a term of a row's sum passes through at most: 32 of a thread, 6 of a wave, 16 of waves
 
@@ -64,6 +66,40 @@ def route(x, w, top_k, score="softmax", bias=None, normalize=True, scale=1.0):
         total = weights.sum(1, keepdims=True)
         weights = np.where(total == 0, 0.0, weights / np.where(total == 0, 1.0, total))
     return chosen, weights * scale
+
+
+def experts(x, chosen, weights, gate_up, down, inter, group, act="silu", residual=None, u=2.0 ** -11, tiny=2.0 ** -24):
+    """gate_up, down: (codes, scales, zeros) of all experts' units one behind the other; u, tiny: half a step and the least step of the type that h is
+    rounded to.  Returns y [tokens, channels] before its rounding and a bound of its error: of the sums of 32 bits (oracle.attention.dense_w4), through the activation
+    (whose slope is 1.13 at most, its own functions off by 8 half-steps), the product and its rounding, through the second product."""
+    tokens, channels = x.shape
+    part = lambda w, first, n: tuple(None if a is None else a[first:first + n] for a in w)
+    y, err = np.zeros((tokens, channels)), np.zeros((tokens, channels))
+    size = np.zeros((tokens, channels))
+    for e in sorted({int(c) for c in chosen.ravel() if 0 <= c < len(gate_up[0]) // (2 * inter)}):
+        tok, slot = np.nonzero(chosen == e)
+        (g, dg), (v, dv) = (attention.dense_w4(x[tok], *part(gate_up, (2 * e + i) * inter, inter), group) for i in (0, 1))
+        with np.errstate(over="ignore"):
+            a = g / (1 + np.exp(-g)) if act == "silu" else 0.5 * g * np.vectorize(math.erfc)(-g * math.sqrt(0.5))
+        da = 1.13 * dg + 8 * E32 * (np.abs(a) + dg)
+        w = weights[tok, slot][:, None]
+        h = w * a * v
+        dh = np.abs(w) * ((np.abs(a) + da) * (np.abs(v) + dv) - np.abs(a * v))
+        dh = dh + 3 * E32 * (np.abs(h) + dh)
+        dh = dh + u * (np.abs(h) + dh) + tiny
+        wd = part(down, e * channels, channels)
+        out, bound = attention.dense_w4(h, *wd, group)
+        codes = np.empty((channels, inter))
+        codes[:, 0::2], codes[:, 1::2] = wd[0] & 15, wd[0] >> 4
+        which = np.arange(inter) // group
+        mag = np.abs((codes - (8.0 if wd[2] is None else wd[2][:, which].astype(np.float64))) * wd[1][:, which])
+        moved = dh @ mag.T
+        np.add.at(y, tok, out)
+        np.add.at(err, tok, 1.02 * bound + moved)
+        np.add.at(size, tok, np.abs(out) + bound + moved)
+    if residual is not None:
+        y, size = y + residual, size + np.abs(residual)
+    return y, err + (chosen.shape[1] + 2) * E32 * size
 
 
 def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, uniform=0.0):

@@ -124,6 +124,8 @@ SIGNATURES = {
     "relay_residual_norm": [_P] * 11,
     "relay_route_workspace_bytes": [_P, C.POINTER(_SZ)],
     "relay_route": [_P] * 7 + [_SZ, _P],
+    "relay_experts_w4_workspace_bytes": [_P, C.POINTER(_SZ)],
+    "relay_experts_w4": [_P] * 9 + [_SZ, _P],
     "relay_sample_workspace_bytes": [_P, C.POINTER(_SZ)],
     "relay_sample": [_P] * 10 + [_SZ, _P],
     "relay_launch_list_create": [_P, C.POINTER(_P)],
@@ -836,6 +838,7 @@ def relay_qdense_w4(d: QDenseW4Desc, x, packed, bias, residual, y) -> None:
 # ------------------------------------------------ a decoder's step beside its attention layer
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+ACT_SILU, ACT_GELU = 0, 1
 
 
 class ResidualNormDesc(C.Structure):
@@ -918,6 +921,46 @@ def relay_route(d: RouteDesc, x, w, bias, chosen, weights, workspace) -> None:
         _refuse_floats("weights", weights, n)
     _check(lib().relay_route(C.addressof(d), _ptr(x), _ptr(w), _ptr(bias), chosen.data_ptr(), weights.data_ptr(), _ptr(workspace),
                              0 if workspace is None else workspace.nbytes, _stream()))
+
+
+class ExpertsW4Desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "top_k", "channels", "inter", "experts", "group", "has_zeros", "act")] + \
+        [("flags", C.c_uint32)] + [(n, C.c_int64) for n in ("x_stride", "y_stride")]
+
+    @functools.cached_property
+    def packed_bytes(self) -> Tuple[int, int]:
+        """What relay_experts_w4 reads of gate_up and of down (asked for once)."""
+        return tuple(relay_qdense_w4_packed_bytes(QDenseW4Desc(self.dtype, 0, n, k, self.group, self.has_zeros, 0, k, n))
+                     for n, k in ((2 * self.experts * self.inter, self.channels), (self.experts * self.channels, self.inter)))
+
+
+def experts_w4_desc(x, chosen, y, experts: int, inter: int, group: int, zeros=False, act=ACT_SILU, residual=None) -> ExpertsW4Desc:
+    """Descriptor of relay_experts_w4 from its tensors: x, y [tokens, channels] with contiguous rows; residual with y's strides; chosen [tokens, top_k]."""
+    if x.dim() != 2 or x.shape != y.shape or x.dtype is not y.dtype or x.stride(1) != 1 or y.stride(1) != 1 or chosen.dim() != 2 or chosen.shape[0] != x.shape[0]:
+        raise RelayError(2, f"x {tuple(x.shape)} of {x.dtype}, y {tuple(y.shape)} of {y.dtype} and chosen {tuple(chosen.shape)} do not go together")
+    if residual is not None and (residual.shape != y.shape or residual.stride() != y.stride() or residual.dtype is not y.dtype):
+        raise RelayError(2, "residual must have the type, shape and strides of y")
+    return ExpertsW4Desc(dtype_of(x), x.shape[0], chosen.shape[1], x.shape[1], inter, experts, group, 1 if zeros else 0, act,
+                         flags_of(None, None, residual), x.stride(0), y.stride(0))
+
+
+def relay_experts_w4_workspace_bytes(d: ExpertsW4Desc) -> int:
+    b = _SZ()
+    _check(lib().relay_experts_w4_workspace_bytes(C.addressof(d), C.byref(b)))
+    return b.value
+
+
+def relay_experts_w4(d: ExpertsW4Desc, x, chosen, weights, gate_up, down, residual, y, workspace) -> None:
+    n = d.tokens * d.top_k
+    if chosen is None or chosen.dtype is not _INT32 or chosen.numel() < n or not chosen.is_contiguous():
+        _refuse_index("chosen", chosen, n)
+    if weights is None or weights.dtype is not _FLOAT32 or weights.numel() < n or not weights.is_contiguous():
+        _refuse_floats("weights", weights, n)
+    for name, t, need in (("gate_up", gate_up, d.packed_bytes[0]), ("down", down, d.packed_bytes[1])):
+        if t is not None and t.nbytes < need:
+            raise RelayError(6, f"{name}: packed weights of {t.nbytes} bytes, {need} needed")
+    _check(lib().relay_experts_w4(C.addressof(d), _ptr(x), chosen.data_ptr(), weights.data_ptr(), _ptr(gate_up), _ptr(down), _ptr(residual), _ptr(y),
+                                  _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
 
 
 class SampleDesc(C.Structure):

@@ -113,6 +113,52 @@ relay_status relay_route(const relay_route_desc* d, const void* x, const void* w
   return device_status(relay::launch_route(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "router launch");
 }
 
+static relay_status experts_args(const relay_experts_w4_desc* d, relay::ExpertsArgs* out) {
+  if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
+  if (d->dtype != RELAY_F16 && d->dtype != RELAY_BF16) return fail(RELAY_ERR_DTYPE, "4-bit experts take F16 or BF16");
+  if (d->tokens < 0 || d->top_k <= 0 || d->top_k > relay::kRouteTopK || d->channels <= 0 || d->inter <= 0 || d->experts <= 0 || d->experts > relay::kRouteExperts)
+    return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d top_k=%d channels=%d inter=%d experts=%d)", d->tokens, d->top_k, d->channels, d->inter, d->experts);
+  if (d->channels % 16 || d->inter % 16) return fail(RELAY_ERR_ALIGN, "channels=%d and inter=%d must be multiples of 16", d->channels, d->inter);
+  if (2L * d->experts * d->inter > 0x7ffffff0L || (long)d->experts * d->channels > 0x7ffffff0L || d->channels > 0x7fffff00 / 16)
+    return fail(RELAY_ERR_SHAPE, "experts=%d channels=%d inter=%d too large", d->experts, d->channels, d->inter);
+  if (d->group <= 0 || d->group % 32) return fail(RELAY_ERR_SHAPE, "group=%d must be a positive multiple of 32", d->group);
+  if (d->has_zeros != 0 && d->has_zeros != 1) return fail(RELAY_ERR_UNSUPPORTED, "has_zeros=%d (0 or 1)", d->has_zeros);
+  if (d->act != RELAY_ACT_SILU && d->act != RELAY_ACT_GELU) return fail(RELAY_ERR_UNSUPPORTED, "unknown activation %d", d->act);
+  if (d->flags & ~(uint32_t)RELAY_HAS_RESIDUAL) return fail(RELAY_ERR_UNSUPPORTED, "unknown flag bits 0x%x", d->flags);
+  if (d->x_stride < 0 || !apart(d->y_stride, d->tokens, d->channels)) return fail(RELAY_ERR_SHAPE, "x_stride must not be negative, y_stride not below channels");
+  if (d->x_stride % 8) return fail(RELAY_ERR_ALIGN, "x_stride must be a multiple of 8");
+  relay::ExpertsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = d->tokens; a.top_k = d->top_k; a.channels = d->channels; a.inter = d->inter; a.experts = d->experts; a.group = d->group;
+  a.zeros = d->has_zeros; a.act = d->act; a.x_stride = d->x_stride; a.y_stride = d->y_stride;
+  *out = a;
+  return RELAY_OK;
+}
+
+relay_status relay_experts_w4_workspace_bytes(const relay_experts_w4_desc* d, size_t* bytes) {
+  if (!bytes) return fail(RELAY_ERR_NULL, "bytes is NULL");
+  relay::ExpertsArgs a;
+  if (relay_status st = experts_args(d, &a)) return st;
+  *bytes = a.tokens ? relay::experts_workspace_bytes(a) : 0;
+  return RELAY_OK;
+}
+
+relay_status relay_experts_w4(const relay_experts_w4_desc* d, const void* x, const int32_t* chosen, const float* weights, const void* gate_up,
+                              const void* down, const void* residual, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  relay::ExpertsArgs a;
+  if (relay_status st = experts_args(d, &a)) return st;
+  if (a.tokens == 0) return RELAY_OK;
+  if (!x || !chosen || !weights || !gate_up || !down || !y) return fail(RELAY_ERR_NULL, "x, chosen, weights, gate_up, down and y are required");
+  if (!residual != !(d->flags & RELAY_HAS_RESIDUAL)) return fail(RELAY_ERR_NULL, "residual must be given exactly if its flag is set");
+  if (!aligned(x, 16) || !aligned(gate_up, 16) || !aligned(down, 16)) return fail(RELAY_ERR_ALIGN, "x, gate_up and down must be 16-byte aligned");
+  if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(chosen, 4) || !aligned(weights, 4))
+    return fail(RELAY_ERR_ALIGN, "y, residual, chosen and weights must be aligned to their type");
+  if (y == x || y == gate_up || y == down || y == chosen || y == weights || y == workspace) return fail(RELAY_ERR_UNSUPPORTED, "output must not alias an input");
+  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::experts_workspace_bytes(a))) return st;
+  a.x = x; a.chosen = chosen; a.weights = weights; a.gate_up = gate_up; a.down = down; a.res = residual; a.y = y; a.workspace = workspace;
+  return device_status(relay::launch_experts(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "experts launch");
+}
+
 static relay_status check_sample(const relay_sample_desc* d) {
   if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
   if (!esize(d->dtype)) return fail(RELAY_ERR_DTYPE, "logits are F16, BF16 or F32");

@@ -47,6 +47,30 @@ constexpr int kRouteExperts = 1024, kRouteTopK = 64;
 size_t route_workspace_bytes(const RouteArgs& a);
 hipError_t launch_route(const RouteArgs& a, int dtype, hipStream_t st);
 
+enum : int { A_SILU = 0, A_GELU = 1 };  // RELAY_ACT_*
+
+struct ExpertsArgs {
+  int tokens, top_k, channels, inter, experts, group, zeros, act;
+  int64_t x_stride, y_stride;
+  const void* x;
+  const int32_t* chosen;
+  const float* weights;
+  const void* gate_up;
+  const void* down;
+  const void* res;
+  void* y;
+  void* workspace;
+  // set by the launcher, as is: pairs of a token and an expert; whether a launch has a workgroup to a pair (or to an expert)
+  int pairs, by_pair;
+  FastDiv fd_top_k;
+  void* h;        // [pairs][inter]
+  float* parts;   // [pairs][channels]
+  // (a group as long as the row is the row's chunks of 128, whole, as for the dense layers)
+  __host__ __device__ int group_of(int k) const { return group < k ? group : (k + 127) / 128 * 128; }
+};
+size_t experts_workspace_bytes(const ExpertsArgs& a);
+hipError_t launch_experts(const ExpertsArgs& a, int dtype, hipStream_t st);
+
 struct SampleArgs {
   int rows, vocab;
   int64_t logits_stride;

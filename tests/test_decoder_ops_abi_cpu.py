@@ -168,3 +168,56 @@ def test_route_operands():
                 lambda: B.relay_route(d, x, w, None, chosen, None, None), lambda: B.relay_route(d, x, w, None, None, weights, None)):
         with pytest.raises(B.RelayError):
             bad()
+
+
+# -------------------------------------------------------------------------------- experts
+def _experts(**kw):
+    return _with(B.ExpertsW4Desc(B.RELAY_BF16, 5, 2, 64, 32, 8, 32, 0, B.ACT_SILU, 0, 64, 64), **kw)
+
+
+def _call_experts(d, ws=at(9), ws_bytes=1 << 30, **kw):
+    names = ("x", "chosen", "weights", "gate_up", "down", "residual", "y")
+    return _status("relay_experts_w4", d, *[kw.get(n, None if n == "residual" else at(i)) for i, n in enumerate(names)], ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=B.RELAY_F32), 3), (dict(tokens=-1), 2), (dict(top_k=0), 2), (dict(top_k=65), 2), (dict(channels=0), 2), (dict(channels=72), 5), (dict(inter=0), 2),
+    (dict(inter=40), 5), (dict(experts=0), 2), (dict(experts=1025), 2), (dict(experts=1000, inter=1 << 21), 2), (dict(experts=1000, channels=1 << 22, y_stride=1 << 22), 2),
+    (dict(group=0), 2), (dict(group=48), 2), (dict(has_zeros=2), 4), (dict(act=2), 4), (dict(flags=B.RELU), 4), (dict(flags=64), 4), (dict(x_stride=-8), 2),
+    (dict(x_stride=68), 5), (dict(y_stride=63), 2)])
+def test_experts_refuse(kw, status):
+    b = C.c_size_t()
+    assert _call_experts(_experts(**kw)) == status
+    assert _status("relay_experts_w4_workspace_bytes", _experts(**kw), C.byref(b)) == status
+
+
+def test_experts_pointers():
+    b = C.c_size_t()
+    assert _call_experts(None) == 1 and _status("relay_experts_w4_workspace_bytes", _experts(), None) == 1
+    for name in ("x", "chosen", "weights", "gate_up", "down", "y"):
+        assert _call_experts(_experts(), **{name: None}) == 1
+    assert _call_experts(_experts(), residual=at(5)) == 1 and _call_experts(_experts(flags=B.HAS_RESIDUAL)) == 1
+    for name, off in (("x", 8), ("chosen", 2), ("weights", 1), ("gate_up", 8), ("down", 4), ("y", 1)):
+        assert _call_experts(_experts(), **{name: at(20) + off}) == 5
+    assert _call_experts(_experts(flags=B.HAS_RESIDUAL), residual=at(5) + 1) == 5
+    for other in (0, 1, 2, 3, 4, 9):
+        assert _call_experts(_experts(), y=at(other)) == 4
+    assert _status("relay_experts_w4_workspace_bytes", _experts(), C.byref(b)) == 0 and b.value > 0
+    assert _call_experts(_experts(), ws=None) == 6 and _call_experts(_experts(), ws_bytes=b.value - 1) == 6 and _call_experts(_experts(), ws=at(9) + 128) == 5
+    assert _call_experts(_experts(tokens=0), ws=None, x=None, chosen=None, weights=None, gate_up=None, down=None, y=None) == 0
+
+
+def test_experts_operands():
+    x, y, chosen, weights = _f16(5, 64), _f16(5, 64), torch.zeros(5, 2, dtype=torch.int32), torch.zeros(5, 2)
+    d = B.experts_w4_desc(x, chosen, y, 8, 32, 32)
+    assert (d.tokens, d.top_k, d.channels, d.inter, d.experts, d.flags) == (5, 2, 64, 32, 8, 0)
+    assert d.packed_bytes == (32 * 1024 + 32 * 2 * 32, 32 * 1024 + 32 * 32)
+    up, down = (torch.zeros(n, dtype=torch.uint8) for n in d.packed_bytes)
+    call = lambda **kw: B.relay_experts_w4(*[{**dict(d=d, x=x, chosen=chosen, weights=weights, gate_up=up, down=down, residual=None, y=y, workspace=None), **kw}[n] for n in
+                                             ("d", "x", "chosen", "weights", "gate_up", "down", "residual", "y", "workspace")])
+    for bad in (lambda: B.experts_w4_desc(x, chosen, y.bfloat16(), 8, 32, 32), lambda: B.experts_w4_desc(x, chosen, _f16(5, 80), 8, 32, 32),
+                lambda: B.experts_w4_desc(x, chosen[:4], y, 8, 32, 32), lambda: B.experts_w4_desc(x, chosen, y, 8, 32, 32, residual=_f16(5, 80)[:, :64]),
+                lambda: B.experts_w4_desc(_f16(64, 5).t(), chosen, y, 8, 32, 32), lambda: call(chosen=chosen.long()), lambda: call(chosen=None),
+                lambda: call(weights=weights.half()), lambda: call(weights=weights[:4]), lambda: call(gate_up=up[1:]), lambda: call(down=down[:100])):
+        with pytest.raises(B.RelayError):
+            bad()
