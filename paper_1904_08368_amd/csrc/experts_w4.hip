@@ -1,8 +1,9 @@
 // The experts of a mixture with 4-bit weights for a few tokens:  h = weight act(gate x) (up x),  y = sum over a token's experts of down h.
 //
 // A pair is a token and one of the experts it has chosen; pairs of one expert share its codes, which are most of what there is to read.  The first
-// launch makes h of every pair, a workgroup to 16 units of an expert's gates and the 16 beside them; the second makes 16 channels of y, walking the units of
-// all experts that were chosen, keeps a pair's part of them in LDS and adds a token's parts up in the order of its choices.  The experts' weights go into h: the second product then needs none.
+// launch makes h of every pair; the second y, of few pairs directly (a workgroup adds up what the experts make of 16 channels), of more through a pair's parts in memory, which a third adds
+// up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
+// reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 117 and 70 (4.6 and 3.9 TB/s).
 // Codes become operands as in the dense kernels (16 + code, the sums of x taking the zero points out).
 #include "decoder_ops.hpp"
 #include "w4_common.hpp"
@@ -10,76 +11,81 @@
 namespace relay {
 namespace {
 
-// The pairs that name expert e, of those from `from` on the first `most`, into rows; returns how many there are in all.  W waves, each a stretch of the pairs; two barriers.
-template <int W>
-__device__ int pairs_of(const int32_t* chosen, int pairs, int e, int from, int most, int* rows, int* counts) {
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int stretch = ((pairs + W - 1) / W + 63) / 64 * 64, lo = wave * stretch, hi = min(lo + stretch, pairs);
-  int n = 0;
-  for (int p = lo; p < hi; p += 64) n += __builtin_popcountll(__ballot(p + lane < hi && chosen[min(p + lane, hi - 1)] == e));
-  if (lane == 0) counts[wave] = n;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int u = 0; u < W; ++u) {
-    const int c = counts[u];
-    if (u < wave) before += c;
-    all += c;
+// The pairs that name expert e, of those from `from` on the first `most`, into this wave's rows; how many there are in all, and which is the first.
+struct Found { int all, first; };
+__device__ __forceinline__ Found pairs_of(const int32_t* chosen, int pairs, int e, int from, int most, int* rows, int lane) {
+  Found f{0, pairs};
+  for (int p = 0; p < pairs; p += 64) {
+    const bool mine = p + lane < pairs && chosen[min(p + lane, pairs - 1)] == e;
+    const unsigned long long set = __ballot(mine);
+    if (!set) continue;
+    if (!f.all) f.first = p + __builtin_ctzll(set);
+    const int at = f.all + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u)) - from;
+    if (mine && at >= 0 && at < most) rows[at] = p + lane;
+    f.all += __builtin_popcountll(set);
   }
-  if (n)
-    for (int p = lo; p < hi; p += 64) {
-      const bool mine = p + lane < hi && chosen[min(p + lane, hi - 1)] == e;
-      const unsigned long long set = __ballot(mine);
-      const int at = before + __builtin_popcountll(set & ((1ull << lane) - 1)) - from;
-      if (mine && at >= 0 && at < most) rows[at] = p + lane;
-      before += __builtin_popcountll(set);
-    }
-  __syncthreads();
-  return all;
+  return f;
 }
 
-// What a wave holds of a chunk of 128 of the reduction: codes of NT tiles of 16 units, their scales and zero points, XL loads of four rows of x each.
+// What a wave holds of a chunk of 128 of the reduction: codes of NT tiles of 16 units; XL loads of x, four rows each; scales and zero points, which come in whole 16-byte
+// pieces and go through LDS with x (a load of a wave takes the memory pipe 16 clocks whatever its lanes ask for).
 // FL: steps of 32 between two applications of the scales, 4 where groups are whole chunks, 2 or 1 where they are not.
+// All loads are made, of something that is there: which of them return when is then known ahead, and a wait is for those of its chunk alone.
 template <typename T, int NT, int XL, int FL>
 struct Chunk {
   typedef T four __attribute__((ext_vector_type(4)));
-  uintx4 codes[NT], x[XL];
-  four scale[4 / FL][NT];
-  unsigned zero[4 / FL][NT];
-  // (the caller has checked that the chunk is there; rows that are not: a NULL)
-  __device__ __forceinline__ void load(const unsigned char* packed, const W4Layout& l, const FastDiv& per_group, bool zeros, const long (&tile)[NT], const T* const (&row)[XL], int chunk, int k,
-                                       int lane) {
-    const int g = lane >> 4, col = lane & 15;
+  static constexpr int PG = 4 / FL, PIECES = XL * 64 + NT * PG * 3;   // groups of a chunk at most; 16-byte pieces of LDS
+  uintx4 codes[NT], x[XL], params;
+  // One place of a stack of units.
+  struct Where {
+    const uintx4* codes[NT];   // of the tiles' first chunk (the same for all lanes)
+    const uintx4* params;      // this lane's piece of the scales (of the zero points) of the tiles' first group
+    int step, half;            // pieces from group to group; of scales
+    const T* row[XL];          // this lane's rows, at its piece of a chunk
+    __device__ __forceinline__ void set(const unsigned char* packed, const W4Layout& l, bool zeros, const long (&tile)[NT], int lane) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) codes[t] = reinterpret_cast<const uintx4*>(packed)[((size_t)tile[t] * l.chunks + chunk) * 64 + lane];
+      for (int t = 0; t < NT; ++t) codes[t] = reinterpret_cast<const uintx4*>(packed) + (size_t)tile[t] * l.chunks * 64;
+      // lanes: [tile][group] scales of two pieces, then [tile][group] zero points of one
+      const int which = min(lane, NT * PG * 3 - 1), z = which - NT * PG * 2;
+      long at = tile[0];
 #pragma unroll
-    for (int f = 0; f < 4 / FL; ++f) {
-      const int at = min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const size_t unit = ((size_t)tile[t] * l.groups + at) * 16 + 4 * g;
-        scale[f][t] = *reinterpret_cast<const four*>(packed + l.scales_at + unit * 2);
-        zero[f][t] = zeros ? *reinterpret_cast<const unsigned*>(packed + l.zeros_at + unit) : 0x18181818u;
-      }
+      for (int t = 1; t < NT; ++t)
+        if ((z < 0 ? which / (2 * PG) : z / PG) == t) at = tile[t];
+      const bool zp = z >= 0 && zeros;
+      step = zp ? 1 : 2;
+      half = z < 0 ? (which & 1) : 0;
+      params = reinterpret_cast<const uintx4*>(packed + (zp ? l.zeros_at : l.scales_at)) + (size_t)at * l.groups * step + half;
+      group = z < 0 ? which % (2 * PG) / 2 : z % PG;
     }
+    int group;                 // this lane's of a chunk's groups
+  };
+  // chunk `chunk` of the tiles `ahead` behind the first
+  __device__ __forceinline__ void load_codes(const Where& w, const W4Layout& l, const FastDiv& per_group, int ahead, int chunk, int lane) {
 #pragma unroll
-    for (int i = 0; i < XL; ++i) {
-      x[i] = (uintx4){0, 0, 0, 0};
-      if (row[i] && chunk * 128 + col * 8 < k) x[i] = *reinterpret_cast<const uintx4*>(row[i] + chunk * 128 + col * 8);
-    }
+    for (int t = 0; t < NT; ++t) codes[t] = (w.codes[t] + ((size_t)ahead * l.chunks + chunk) * 64)[(unsigned)lane];
+    params = w.params[((size_t)ahead * l.groups + min((int)fast_div((unsigned)(chunk * 4), per_group) + w.group, l.groups - 1)) * w.step];
   }
-  // sums += the chunk's part; mine: LDS of this wave for XL times four rows of 16 pieces
+  __device__ __forceinline__ void load_x(const Where& w, int chunk, int k, int lane) {
+    const int at = chunk * 128 + (lane & 15) * 8 < k ? chunk * 128 : 0;
+#pragma unroll
+    for (int i = 0; i < XL; ++i) x[i] = *reinterpret_cast<const uintx4*>(w.row[i] + at);
+  }
+  // sums += the chunk's part; mine: PIECES of LDS of this wave
   template <int RT>
-  __device__ __forceinline__ void add(floatx4 (&sum)[NT][RT], uintx4* mine, const Widen<T>& widen, int lane) const {
+  __device__ __forceinline__ void add(floatx4 (&sum)[NT][RT], uintx4* mine, const W4Layout& l, const FastDiv& per_group, bool zeros, const Widen<T>& widen, int chunk, int k, int lane) const {
     typedef W4Type<T> C;
     typedef typename C::vec vec;
     const int g = lane >> 4, col = lane & 15;
     const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
     const floatx4 none = {0, 0, 0, 0};
+    const bool there = chunk * 128 + col * 8 < k;   // (what lies past k: zeros)
 #pragma unroll
-    for (int i = 0; i < XL; ++i) mine[(4 * i + g) * 16 + (col ^ ((4 * i + g) & 15))] = x[i];
+    for (int i = 0; i < XL; ++i) mine[(4 * i + g) * 16 + (col ^ ((4 * i + g) & 15))] = there ? x[i] : (uintx4){0, 0, 0, 0};
+    if (lane < NT * PG * 3) mine[XL * 64 + lane] = params;
+    const four* const scales = reinterpret_cast<const four*>(mine + XL * 64);
+    const unsigned* const zps = reinterpret_cast<const unsigned*>(mine + XL * 64 + NT * PG * 2);
 #pragma unroll
-    for (int f = 0; f < 4 / FL; ++f) {
+    for (int f = 0; f < PG; ++f) {
       floatx4 acc[NT][RT], xs[RT];
 #pragma unroll
       for (int s = f * FL; s < (f + 1) * FL; ++s) {
@@ -87,7 +93,7 @@ struct Chunk {
         vec xb[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-          const int at = XL == 1 ? col & 3 : r * 16 + col;   // (four rows: the columns behind repeat them)
+          const int at = XL < 4 ? col & (4 * XL - 1) : r * 16 + col;   // (fewer rows than columns: those behind repeat them)
           xb[r] = __builtin_bit_cast(vec, mine[at * 16 + ((4 * s + g) ^ (at & 15))]);
           xs[r] = C::mfma(ones, xb[r], fresh ? none : xs[r]);
         }
@@ -98,14 +104,19 @@ struct Chunk {
           for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
         }
       }
+      // (the group of step f * FL, counted from the chunk's first)
+      const int gr = PG == 1 ? 0 : min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t) {
+        const four sc = scales[(t * PG + gr) * 4 + g];
+        const unsigned zp = zeros ? zps[(t * PG + gr) * 4 + g] : 0x18181818u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float z = -(float)((zero[f][t] >> (8 * i)) & 255u), k = (float)scale[f][t][i];
+          const float z = -(float)((zp >> (8 * i)) & 255u), kf = (float)sc[i];
 #pragma unroll
-          for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(k, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
+          for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(kf, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
         }
+      }
     }
   }
 };
@@ -114,120 +125,228 @@ __device__ __forceinline__ float activated(int act, float v) {
   return act == A_SILU ? v / (1.f + expf(-v)) : 0.5f * v * erfcf(v * -0.70710678118654752440f);   // (1 + erf(v) is erfc(-v), without the difference)
 }
 
-// A workgroup: TILES tiles of 16 units of an expert's products, its waves share the reduction out; blocks of up to XL * 4 of the expert's pairs.
-//   UP: h of the pairs, from as many tiles of gates as of the other units.   not UP: a pair's part of y, in fp32.
-template <typename T, bool UP, int TILES, int XL, int W, int FL>
-__global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group) {
-  constexpr int NT = UP ? 2 * TILES : TILES, RT = XL == 1 ? 1 : XL / 4, ROWS = XL * 4, XPIECES = ROWS * 16, SUMS = NT * RT * 64;
-  __shared__ __attribute__((aligned(16))) uintx4 lds[W][XPIECES > SUMS ? XPIECES : SUMS];
-  __shared__ int rows[ROWS], counts[W];
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4;
-  int e = (int)blockIdx.y;
-  if (a.by_pair) {   // the first pair of an expert stands for it
-    const int p = e;
-    e = a.chosen[p];
-    bool first = true;
-    for (int q = lane; q < p; q += 64) first &= a.chosen[q] != e;
-    if (!__all(first) || (unsigned)e >= (unsigned)a.experts) return;
+// sums += chunks first .. last - 1 of the tiles `ahead` behind the first, D of them on their way: c holds the first D.
+template <int D, typename T, int NT, int XL, int FL, int RT>
+__device__ __forceinline__ void walk(floatx4 (&sum)[NT][RT], Chunk<T, NT, XL, FL> (&c)[D], const typename Chunk<T, NT, XL, FL>::Where& w, const W4Layout& l, const FastDiv& per_group, bool zeros,
+                                     int ahead, int first, int last, int k, uintx4* mine, const Widen<T>& widen, int lane) {
+  int chunk = first;
+  for (; chunk + D < last; chunk += D) {
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      c[i].template add<RT>(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
+      c[i].load_codes(w, l, per_group, ahead, min(chunk + i + D, last - 1), lane);
+      c[i].load_x(w, min(chunk + i + D, last - 1), k, lane);
+      __builtin_amdgcn_sched_barrier(0);   // (two chunks' sums side by side take twice the registers)
+    }
   }
-  const int k = UP ? a.channels : a.inter, units = (UP ? a.inter : a.channels) / 16;
-  const unsigned char* const packed = static_cast<const unsigned char*>(UP ? a.gate_up : a.down);
-  long tile[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const long in = min((int)blockIdx.x * TILES + t % TILES, units - 1);   // (a tile past the last is computed again and not stored)
-    tile[t] = UP ? (long)e * 2 * units + (t / TILES) * units + in : (long)e * units + in;
-  }
-  const int first = l.chunks * wave / W, last = l.chunks * (wave + 1) / W;
-  const Widen<T> widen;
-  for (int from = (int)blockIdx.z * ROWS, all = 0x7fffffff; from < all; from += (int)gridDim.z * ROWS) {
-    all = pairs_of<W>(a.chosen, a.pairs, e, from, ROWS, rows, counts);
-    if (from >= all) return;   // (the same for all threads)
-    const int have = min(ROWS, all - from);
-    const T* row[XL];
-#pragma unroll
-    for (int i = 0; i < XL; ++i) {
-      row[i] = nullptr;
-      if (4 * i + g < have) {
-        const int p = rows[4 * i + g];
-        row[i] = UP ? static_cast<const T*>(a.x) + (long)fast_div((unsigned)p, a.fd_top_k) * a.x_stride : static_cast<const T*>(a.h) + (long)p * a.inter;
-      }
-    }
-    floatx4 sum[NT][RT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < RT; ++r) sum[t][r] = (floatx4){0, 0, 0, 0};
-    Chunk<T, NT, XL, FL> c;
-    if (first < last) c.load(packed, l, per_group, a.zeros, tile, row, first, k, lane);
-    for (int chunk = first; chunk < last; ++chunk) {
-      const Chunk<T, NT, XL, FL> now = c;
-      if (chunk + 1 < last) c.load(packed, l, per_group, a.zeros, tile, row, chunk + 1, k, lane);
-      now.template add<RT>(sum, lds[wave], widen, lane);
-    }
-    floatx4* const part = reinterpret_cast<floatx4*>(lds[wave]);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < RT; ++r) part[(t * RT + r) * 64 + lane] = sum[t][r];
-    __syncthreads();
-    for (int i = (int)threadIdx.x; i < TILES * RT * 64; i += W * 64) {
-      const int t = i / (RT * 64), at = i / 64 % RT * 16 + (i & 15), u0 = ((int)blockIdx.x * TILES + t) * 16 + 4 * (i >> 4 & 3);
-      if (at >= have || u0 >= units * 16) continue;
-      const int p = rows[at];
-      floatx4 v[UP ? 2 : 1];
-#pragma unroll
-      for (int w = 0; w < (UP ? 2 : 1); ++w) {
-        v[w] = (floatx4){0, 0, 0, 0};
-#pragma unroll
-        for (int u = 0; u < W; ++u) v[w] += reinterpret_cast<const floatx4*>(lds[u])[i + w * TILES * RT * 64];
-        if (__builtin_expect(!is_finite(v[w]), 0)) {
-          const T* const x = UP ? static_cast<const T*>(a.x) + (long)fast_div((unsigned)p, a.fd_top_k) * a.x_stride : static_cast<const T*>(a.h) + (long)p * a.inter;
-#pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
-            const float again = sum_by_weights<T>(packed, l, k, a.group_of(k), a.zeros, x, (UP ? e * 2 * a.inter + w * a.inter : e * a.channels) + u0 + j);
-#pragma unroll
-            for (int f = 0; f < 4; ++f) v[w][f] = j == f ? again : v[w][f];
-          }
-        }
-      }
-      if constexpr (UP) {
-        typedef T four __attribute__((ext_vector_type(4)));
-        four h;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = (T)(a.weights[p] * activated(a.act, v[0][j]) * v[UP][j]);
-        *reinterpret_cast<four*>(static_cast<T*>(a.h) + (long)p * a.inter + u0) = h;
-      } else {
-        *reinterpret_cast<floatx4*>(a.parts + (long)p * a.channels + u0) = v[0];
-      }
-    }
-    __syncthreads();
+  for (int i = 0; i < D; ++i) {
+    if (chunk + i < last) c[i].template add<RT>(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// y of a token: its pairs' parts in their order, and the residual.  A thread makes four channels.
+// A wave: n times two tiles of 16 units of an expert (UP: of its gates and the ones beside them, for h; not UP: for a pair's part of y, in fp32) for blocks of up to
+// XL * 4 of the expert's pairs.  KS > 1: that many waves share the reduction of the same two tiles out (n = 1).  Waves know nothing of each other otherwise.
+template <typename T, bool UP, int XL, int KS, int D, int W, int FL>
+__global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group, const int n) {
+  typedef Chunk<T, 2, XL, FL> Held;
+  constexpr int RT = XL <= 4 ? 1 : XL / 4, ROWS = XL * 4, SUMS = 2 * RT * 64, LDS = Held::PIECES > SUMS ? Held::PIECES : SUMS, PER = UP ? 1 : 2;
+  __shared__ __attribute__((aligned(16))) uintx4 lds[W][LDS];
+  __shared__ int rows_of[W][ROWS];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4;
+  const int e = a.by_pair ? a.chosen[blockIdx.y] : (int)blockIdx.y;
+  if ((unsigned)e >= (unsigned)a.experts) return;
+  const int k = UP ? a.channels : a.inter, units = (UP ? a.inter : a.channels) / 16;
+  const unsigned char* const packed = static_cast<const unsigned char*>(UP ? a.gate_up : a.down);
+  const int tile0 = ((int)blockIdx.x * (W / KS) + wave / KS) * PER * n;   // the first of this wave's outputs
+  if (KS == 1 && tile0 >= units) return;
+  // (a tile past the last: the last again, not stored)
+  const long base = UP ? (long)e * 2 * units : (long)e * units;
+  const int part = wave % KS, first = l.chunks * part / KS, last = l.chunks * (part + 1) / KS, many = KS > 1 ? 1 : min(n, (units - tile0 + PER - 1) / PER);
+  const Widen<T> widen;
+  uintx4* const mine = lds[wave];
+  int* const rows = rows_of[wave];
+  auto x_of = [&](int p) { return UP ? static_cast<const T*>(a.x) + (long)fast_div((unsigned)p, a.fd_top_k) * a.x_stride : static_cast<const T*>(a.h) + (long)p * a.inter; };
+  typename Held::Where where;
+  Held c[D];
+  auto at_tile = [&](int i) {
+    const int t = min(tile0 + i * PER, units - 1);
+    const long tile[2] = {base + t, base + (UP ? t + units : min(t + 1, units - 1))};
+    where.set(packed, l, a.zeros, tile, lane);
+#pragma unroll
+    for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, 0, max(min(first + j, last - 1), 0), lane);
+  };
+  auto load_x = [&]() {
+#pragma unroll
+    for (int j = 0; j < D; ++j) c[j].load_x(where, max(min(first + j, last - 1), 0), k, lane);
+  };
+  for (int from = (int)blockIdx.z * ROWS;; from += (int)gridDim.z * ROWS) {
+    at_tile(0);   // (on its way while the rows are looked up)
+    const Found found = pairs_of(a.chosen, a.pairs, e, from, ROWS, rows, lane);
+    if (from >= found.all || (a.by_pair && found.first != (int)blockIdx.y)) return;   // (an expert's first pair stands for it; the same for all waves)
+    const int have = min(ROWS, found.all - from);
+#pragma unroll
+    for (int i = 0; i < XL; ++i) where.row[i] = x_of(rows[min(4 * i + g, have - 1)]) + (lane & 15) * 8;   // (rows that are not there repeat the last one)
+    load_x();
+    for (int i = 0; i < many; ++i) {
+      floatx4 sum[2][RT];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sum[t][r] = (floatx4){0, 0, 0, 0};
+      if (first < last) walk<D, T, 2, XL, FL, RT>(sum, c, where, l, per_group, a.zeros, 0, first, last, k, mine, widen, lane);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) reinterpret_cast<floatx4*>(mine)[(t * RT + r) * 64 + lane] = sum[t][r];
+      if (i + 1 < many) {
+        at_tile(i + 1);
+        load_x();
+      }
+      if (KS > 1) __syncthreads();
+      // four units of a pair: to a lane in turn of the KS waves
+#pragma unroll 1
+      for (int j = KS > 1 ? (wave % KS) * 64 + lane : lane; j < PER * RT * 64; j += KS * 64) {
+        const int t = j / (RT * 64), at = j / 64 % RT * 16 + (j & 15), tl = tile0 + i * PER + t;
+        if (at >= have || tl >= units) continue;
+        floatx4 v[UP ? 2 : 1];
+        const int p = rows[at], u0 = tl * 16 + 4 * (j >> 4 & 3);
+#pragma unroll
+        for (int w = 0; w < (UP ? 2 : 1); ++w) {
+          v[w] = (floatx4){0, 0, 0, 0};
+#pragma unroll
+          for (int u = 0; u < KS; ++u) v[w] += reinterpret_cast<const floatx4*>(lds[wave / KS * KS + u])[j + w * RT * 64];
+          if (__builtin_expect(!is_finite(v[w]), 0))
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const float again = sum_by_weights<T>(packed, l, k, a.group_of(k), a.zeros, x_of(p), (UP ? (2 * e + w) * a.inter : e * a.channels) + u0 + q);
+#pragma unroll
+              for (int f = 0; f < 4; ++f) v[w][f] = q == f ? again : v[w][f];
+            }
+        }
+        if constexpr (UP) {
+          typedef T four __attribute__((ext_vector_type(4)));
+          four h;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) h[q] = (T)(a.weights[p] * activated(a.act, v[0][q]) * v[1][q]);
+          *reinterpret_cast<four*>(static_cast<T*>(a.h) + (long)p * a.inter + u0) = h;
+        } else {
+          *reinterpret_cast<floatx4*>(a.parts + (long)p * a.channels + u0) = v[0];
+        }
+      }
+      if (KS > 1) __syncthreads();
+    }
+    if (from + (int)gridDim.z * ROWS >= found.all) return;
+  }
+}
+
+// y of up to kJoined pairs at once: a workgroup makes 16 channels of all tokens.  Its waves take the chosen experts in turn (several share one's reduction where there are fewer experts than waves), leave
+// each pair's part in LDS, and add a token's up in the order of its choices.
+constexpr int kJoined = 64, kJoinWaves = 8;
+template <typename T, int XL, int FL>
+__global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group) {
+  typedef Chunk<T, 1, XL, FL> Held;
+  constexpr int D = 2, W = kJoinWaves, ROWS = XL * 4;
+  __shared__ __attribute__((aligned(16))) uintx4 lds[W][Held::PIECES];
+  __shared__ __attribute__((aligned(16))) floatx4 parts[W * kJoined][4];   // [share of the reduction][pair]
+  __shared__ int rows_of[W][kJoined];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, tile = (int)blockIdx.x;
+  const unsigned char* const packed = static_cast<const unsigned char*>(a.down);
+  const T* const h = static_cast<const T*>(a.h);
+  const int named = lane < a.pairs ? a.chosen[lane] : -1;
+  const unsigned long long valid = __ballot((unsigned)named < (unsigned)a.experts);
+  int many = 0;
+  for (unsigned long long left = valid; left; ++many) left &= ~__ballot(named == __builtin_amdgcn_readlane(named, __builtin_ctzll(left)));
+  const int shares = many >= W ? 1 : many >= W / 2 ? 2 : many >= W / 4 ? 4 : W;
+  const Widen<T> widen;
+  uintx4* const mine = lds[wave];
+  int* const rows = rows_of[wave];
+  unsigned long long left = valid;
+  for (int unit = 0; left; ++unit) {
+    const int e = __builtin_amdgcn_readlane(named, __builtin_ctzll(left));
+    const unsigned long long set = __ballot(named == e);
+    left &= ~set;
+    const int turn = (wave - unit * shares % W + W) % W;   // this wave's share of the unit, if it has one
+    if (turn >= shares) continue;
+    const int have = __builtin_popcountll(set), first = l.chunks * turn / shares, last = l.chunks * (turn + 1) / shares;
+    if (set >> lane & 1) rows[(int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u))] = lane;
+    typename Held::Where where;
+    const long at[1] = {(long)e * (a.channels / 16) + tile};
+    where.set(packed, l, a.zeros, at, lane);
+    for (int from = 0; from < have; from += ROWS) {
+      floatx4 sum[1][1] = {{{0, 0, 0, 0}}};
+#pragma unroll
+      for (int i = 0; i < XL; ++i) where.row[i] = h + (long)rows[min(from + 4 * i + g, have - 1)] * a.inter + (lane & 15) * 8;   // (rows that are not there repeat the last one)
+      if (first < last) {
+        Held c[D];
+#pragma unroll
+        for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, 0, min(first + j, last - 1), lane);
+#pragma unroll
+        for (int j = 0; j < D; ++j) c[j].load_x(where, min(first + j, last - 1), a.inter, lane);
+        walk<D, T, 1, XL, FL, 1>(sum, c, where, l, per_group, a.zeros, 0, first, last, a.inter, mine, widen, lane);
+      }
+      const int row = from + (lane & 15);
+      if ((lane & 15) < ROWS && row < have) parts[turn * kJoined + rows[row]][g] = sum[0][0];
+    }
+  }
+  __syncthreads();
+  for (int i = (int)threadIdx.x; i < a.tokens * 16; i += W * 64) {
+    const int t = i >> 4, j = i & 15;
+    float v = 0.f;
+    for (int p = t * a.top_k; p < (t + 1) * a.top_k; ++p) {
+      if (!(valid >> p & 1)) continue;
+      float part = 0.f;
+      for (int u = 0; u < shares; ++u) part += reinterpret_cast<const float*>(parts[u * kJoined + p])[j];
+      if (__builtin_expect(!is_finite(part), 0))
+        part = sum_by_weights<T>(packed, l, a.inter, a.group_of(a.inter), a.zeros, h + (long)p * a.inter, a.chosen[p] * a.channels + tile * 16 + j);
+      v += part;
+    }
+    const long at = (long)t * a.y_stride + tile * 16 + j;
+    if (a.res) v += (float)static_cast<const T*>(a.res)[at];
+    static_cast<T*>(a.y)[at] = (T)v;
+  }
+}
+
+// y of more pairs: a token's parts from memory, eight at a time, and the residual.  A thread makes four channels.
 template <typename T>
 __global__ __launch_bounds__(256) void experts_add_kernel(const ExpertsArgs a) {
   const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, t = (int)blockIdx.y;
   if (c >= a.channels) return;
   floatx4 v = {0, 0, 0, 0};
-  for (int s = 0; s < a.top_k; ++s) {
-    const int p = t * a.top_k + s;
-    if ((unsigned)a.chosen[p] < (unsigned)a.experts) v += *reinterpret_cast<const floatx4*>(a.parts + (long)p * a.channels + c);
+  for (int s0 = 0; s0 < a.top_k; s0 += 8) {
+    floatx4 part[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) part[s] = *reinterpret_cast<const floatx4*>(a.parts + (long)(t * a.top_k + min(s0 + s, a.top_k - 1)) * a.channels + c);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)   // (a pair that names no expert has no part: what stands in its place is not used)
+      if (s0 + s < a.top_k && (unsigned)a.chosen[t * a.top_k + s0 + s] < (unsigned)a.experts) v += part[s];
   }
   const long at = (long)t * a.y_stride + c;
 #pragma unroll
   for (int j = 0; j < 4; ++j) static_cast<T*>(a.y)[at + j] = (T)(a.res ? v[j] + (float)static_cast<const T*>(a.res)[at + j] : v[j]);
 }
 
-template <typename T, bool UP, int TILES, int XL, int W>
-hipError_t launch_rows(const ExpertsArgs& a, const W4Layout& l, int blocks, hipStream_t st) {
-  const int units = (UP ? a.inter : a.channels) / 16, per_group = a.group_of(UP ? a.channels : a.inter) / 32;
+template <typename T, bool UP, int XL, int KS>
+hipError_t launch_rows(const ExpertsArgs& a, const W4Layout& l, int n, hipStream_t st) {
+  constexpr int W = 4, D = 2;
+  const int units = (UP ? a.inter : a.channels) / 16, tiles = W / KS * (UP ? n : 2 * n), per_group = a.group_of(UP ? a.channels : a.inter) / 32;
   const FastDiv fd = make_fastdiv((uint32_t)per_group);
-  const dim3 grid((unsigned)((units + TILES - 1) / TILES), (unsigned)(a.by_pair ? a.pairs : a.experts), (unsigned)blocks), block(W * 64);
-  if (per_group % 4 == 0) hipLaunchKernelGGL((experts_rows_kernel<T, UP, TILES, XL, W, 4>), grid, block, 0, st, a, l, fd);
-  else if (per_group % 2 == 0) hipLaunchKernelGGL((experts_rows_kernel<T, UP, TILES, XL, W, 2>), grid, block, 0, st, a, l, fd);
-  else hipLaunchKernelGGL((experts_rows_kernel<T, UP, TILES, XL, W, 1>), grid, block, 0, st, a, l, fd);
+  const dim3 grid((unsigned)((units + tiles - 1) / tiles), (unsigned)(a.by_pair ? a.pairs : a.experts)), block(W * 64);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((experts_rows_kernel<T, UP, XL, KS, D, W, 4>), grid, block, 0, st, a, l, fd, n);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((experts_rows_kernel<T, UP, XL, KS, D, W, 2>), grid, block, 0, st, a, l, fd, n);
+  else hipLaunchKernelGGL((experts_rows_kernel<T, UP, XL, KS, D, W, 1>), grid, block, 0, st, a, l, fd, n);
+  return hipGetLastError();
+}
+
+template <typename T, int XL>
+hipError_t launch_join(const ExpertsArgs& a, const W4Layout& l, hipStream_t st) {
+  const int per_group = a.group_of(a.inter) / 32;
+  const FastDiv fd = make_fastdiv((uint32_t)per_group);
+  const dim3 grid((unsigned)(a.channels / 16)), block(kJoinWaves * 64);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((experts_join_kernel<T, XL, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((experts_join_kernel<T, XL, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((experts_join_kernel<T, XL, 1>), grid, block, 0, st, a, l, fd);
   return hipGetLastError();
 }
 
@@ -235,10 +354,19 @@ template <typename T>
 hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
   const W4Layout up = w4_layout(a.experts * 2 * a.inter, a.channels, a.group_of(a.channels), a.zeros != 0);
   const W4Layout down = w4_layout(a.experts * a.channels, a.inter, a.group_of(a.inter), a.zeros != 0);
-  const int blocks = a.tokens <= 16 ? 1 : (a.tokens + 15) / 16 < 4 ? (a.tokens + 15) / 16 : 4;
-  hipError_t e = a.pairs <= 4 ? launch_rows<T, true, 1, 1, 8>(a, up, 1, st) : launch_rows<T, true, 1, 4, 8>(a, up, blocks, st);
+  const long active = a.pairs < a.experts ? a.pairs : a.experts, up_waves = active * (a.inter / 16), down_waves = active * (a.channels / 32);
+  const bool few = 4L * a.pairs <= a.experts, some = a.pairs <= 4L * a.experts;   // rows of an expert: one, seldom two; four on the mean
+  hipError_t e;
+  if (few || some) {
+    if (few) e = up_waves >= 2048 ? launch_rows<T, true, 1, 2>(a, up, 1, st) : launch_rows<T, true, 1, 4>(a, up, 1, st);
+    else e = up_waves >= 4096 ? launch_rows<T, true, 2, 1>(a, up, 1, st) : up_waves >= 2048 ? launch_rows<T, true, 2, 2>(a, up, 1, st) : launch_rows<T, true, 2, 4>(a, up, 1, st);
+  } else {
+    e = launch_rows<T, true, 4, 2>(a, up, 1, st);
+  }
   if (e != hipSuccess) return e;
-  e = a.pairs <= 4 ? launch_rows<T, false, 2, 1, 8>(a, down, 1, st) : launch_rows<T, false, 2, 4, 8>(a, down, blocks, st);
+  if (a.pairs <= kJoined) return few ? launch_join<T, 1>(a, down, st) : some ? launch_join<T, 2>(a, down, st) : launch_join<T, 4>(a, down, st);
+  if (some) e = down_waves >= 4096 ? launch_rows<T, false, 2, 1>(a, down, down_waves >= 8192 ? 2 : 1, st) : launch_rows<T, false, 2, 2>(a, down, 1, st);
+  else e = launch_rows<T, false, 4, 2>(a, down, 1, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((experts_add_kernel<T>), dim3((unsigned)((a.channels + 1023) / 1024), (unsigned)a.tokens), dim3(256), 0, st, a);
   return hipGetLastError();
