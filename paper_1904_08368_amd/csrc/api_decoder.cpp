@@ -159,36 +159,44 @@ relay_status relay_experts_w4(const relay_experts_w4_desc* d, const void* x, con
   return device_status(relay::launch_experts(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "experts launch");
 }
 
-static relay_status check_sample(const relay_sample_desc* d) {
+static relay_status sample_args(const relay_sample_desc* d, relay::SampleArgs* out) {
   if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
   if (!esize(d->dtype)) return fail(RELAY_ERR_DTYPE, "logits are F16, BF16 or F32");
   if (d->rows < 0 || d->vocab <= 0 || d->vocab > relay::kVocab)
     return fail(RELAY_ERR_SHAPE, "bad extent (rows=%d vocab=%d, vocab in 1 .. %d)", d->rows, d->vocab, relay::kVocab);
   if (d->logits_stride < 0) return fail(RELAY_ERR_SHAPE, "logits_stride must not be negative");
+  relay::SampleArgs a;
+  memset(&a, 0, sizeof(a));
+  a.rows = d->rows; a.vocab = d->vocab; a.logits_stride = d->logits_stride;
+  *out = a;
   return RELAY_OK;
 }
 
 relay_status relay_sample_workspace_bytes(const relay_sample_desc* d, size_t* bytes) {
   if (!bytes) return fail(RELAY_ERR_NULL, "bytes is NULL");
-  if (relay_status st = check_sample(d)) return st;
-  *bytes = 0;
+  relay::SampleArgs a;
+  if (relay_status st = sample_args(d, &a)) return st;
+  *bytes = a.rows ? relay::sample_workspace_bytes(a) : 0;
   return RELAY_OK;
 }
 
 relay_status relay_sample(const relay_sample_desc* d, const void* logits, const float* temperature, const int32_t* top_k, const float* top_p,
                           const float* min_p, const float* uniform, int32_t* tokens, float* probs, void* workspace, size_t workspace_bytes,
                           void* hip_stream) {
-  if (relay_status st = check_sample(d)) return st;
-  if (d->rows == 0) return RELAY_OK;
+  relay::SampleArgs a;
+  if (relay_status st = sample_args(d, &a)) return st;
+  if (a.rows == 0) return RELAY_OK;
   if (!logits || !tokens) return fail(RELAY_ERR_NULL, "logits and tokens are required");
   if (!aligned(logits, esize(d->dtype)) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
       !aligned(uniform, 4) || !aligned(tokens, 4) || !aligned(probs, 4))
     return fail(RELAY_ERR_ALIGN, "tensors must be aligned to their type");
   if (static_cast<const void*>(tokens) == probs || static_cast<const void*>(tokens) == logits || probs == logits)
     return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
-  relay::SampleArgs a;
-  memset(&a, 0, sizeof(a));
-  a.rows = d->rows; a.vocab = d->vocab; a.logits_stride = d->logits_stride;
+  if (workspace) {
+    const size_t need = relay::sample_workspace_bytes(a);
+    if (relay_status st = check_workspace(workspace, workspace_bytes, need)) return st;
+    a.workspace = need ? workspace : nullptr;
+  }
   a.logits = logits; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.uniform = uniform;
   a.tokens = tokens; a.probs = probs;
   return device_status(relay::launch_sample(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "sampling launch");

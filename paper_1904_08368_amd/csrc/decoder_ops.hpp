@@ -82,9 +82,11 @@ struct SampleArgs {
   const float* uniform;
   int32_t* tokens;
   float* probs;
+  void* workspace;  // NULL: a workgroup to a row
   int scale_bits;   // set by the launcher
 };
 constexpr int kVocab = 1 << 20;
+size_t sample_workspace_bytes(const SampleArgs& a);
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
 
 }  // namespace relay

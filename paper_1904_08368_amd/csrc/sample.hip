@@ -2,9 +2,11 @@
 // running sum of w passes u times the sum over the kept.
 //
 // What is asked of the order is always a place in it: the k-th token, the one that reaches a mass.  So nothing is sorted but the few tokens
-// around such a place.  Tokens are told apart by bins of equal width of their distance from the maximum, counted or added up in LDS; the bin of a place is found by
-// a scan, and its tokens are gathered and sorted.  Masses are integers, multiples of 2^-S of the largest weight: sums of them have no order, and the borders between tokens are where 64 bits put them.
-// A row is read three times at most in what settings commonly leave (maximum; counts or masses; gathering), from the caches after the first.
+// around such places.  Tokens are told apart by bins of equal width of their distance from the maximum, counted or added up in LDS.  A place lies in one bin; the mass that the places behind
+// it start from is known up to that bin's, which leaves them few bins.  All these bins' tokens are gathered and sorted, and give the places exactly.
+// Masses are integers, multiples of 2^-S of the largest weight: sums of them have no order, and the borders between tokens are where 64 bits put them.
+// So a row is read three times: maximum; counts or masses; gathering.  One workgroup reads it where there are many rows, from the caches after the first time.  Of few rows each is shared out over
+// workgroups, a launch to each reading.
 #include <float.h>
 
 #include "decoder_ops.hpp"
@@ -12,7 +14,9 @@
 namespace relay {
 namespace {
 
-constexpr int NT = 1024, WAVES = NT / 64, BINS = 2 * NT, CAP = 2048;   // threads to a row; bins of a histogram; tokens that a list holds
+constexpr int BINS = 2048, CAP = 2048;   // of a histogram; tokens that a list holds
+constexpr int NT = 512, WAVES = NT / 64; // threads of a workgroup (of 1024 each would have too few registers)
+constexpr int PARTS = 64;                // workgroups that share a row at most
 typedef unsigned long long u64;
 
 template <typename T> struct Piece { typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
@@ -27,48 +31,27 @@ __device__ __forceinline__ float value_of(unsigned key) {
 }
 
 struct Lds {
-  u64 mass[BINS];      // of a bin, then of all bins up to it
+  u64 mass[BINS];        // of a bin, then of all bins up to it
   unsigned count[BINS];
+  unsigned place[BINS];  // of a bin's tokens in the list
+  unsigned char gathered[BINS];
   union {
     struct {
-      u64 list[CAP];   // (descending value, ascending number) as one ascending number
-      u64 run[CAP];    // masses of the list up to a place
+      u64 list[CAP];     // (descending value, ascending number) as one ascending number
+      u64 run[CAP];      // masses of all tokens up to a place of the list
     };
     struct {
       u64 mass2[BINS];   // as above, of the digits of a crowded bin's keys (while there is no list)
       unsigned count2[BINS];
     };
   };
-  double exp2s[256];   // 2^(i / 256)
+  double exp2s[256];     // 2^(i / 256)
   u64 wave64[WAVES];
   unsigned wave32[WAVES];
   float wavef[2][WAVES];
   int found;
   unsigned listed;
 };
-
-// Sums up to and with this thread's over the block's threads; the total.  (Two barriers: the cells are free again behind them.)
-template <typename V>
-__device__ __forceinline__ V block_scan(V v, V* cells, V* total) {
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const V o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  if (lane == 63) cells[wave] = v;
-  __syncthreads();
-  V before = 0, all = 0;
-#pragma unroll
-  for (int u = 0; u < WAVES; ++u) {
-    const V c = cells[u];
-    if (u < wave) before += c;
-    all += c;
-  }
-  __syncthreads();
-  *total = all;
-  return v + before;
-}
 
 // floor(f x) and ceil(f x), 0 <= f < 1 (of f below 2^-40 the bits past the 64th are dropped)
 __device__ __forceinline__ u64 part_of(float f, u64 x) { return __umul64hi(x, (u64)((double)f * 18446744073709551616.0)); }
@@ -77,128 +60,367 @@ __device__ __forceinline__ u64 part_up(float f, u64 x) {
   return __umul64hi(x, m) + (x * m != 0);
 }
 
+// A row's settings; those that are off as such.
+struct Settings {
+  float temperature, top_p, min_p, u;
+  int top_k;
+  bool cut_p, cut_min, greedy;
+  double z_min;
+  __device__ Settings(const SampleArgs& a, int r) {
+    temperature = a.temperature ? a.temperature[r] : 1.f;
+    top_p = a.top_p ? a.top_p[r] : 1.f;
+    min_p = a.min_p ? a.min_p[r] : 0.f;
+    u = a.uniform ? a.uniform[r] : 0.f;
+    top_k = a.top_k ? a.top_k[r] : 0;
+    if (!(temperature == temperature)) temperature = 1.f;
+    if (top_k <= 0 || top_k >= a.vocab) top_k = 0;
+    cut_p = top_p < 1.f;
+    cut_min = min_p > 0.f;
+    u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);   // (a NaN: 0)
+    greedy = !a.uniform || temperature <= 0.f || top_k == 1 || top_p <= 0.f;
+    z_min = cut_min ? log2((double)fminf(min_p, 1.f)) : 0.0;
+  }
+  // what the second reading adds up: nothing, where the third finds all that min-p keeps by itself; otherwise bins' tokens, and their masses
+  __device__ bool by_value() const { return !top_k && !cut_p && cut_min; }
+  __device__ bool masses() const { return !top_k || top_k > CAP / 2; }   // (of a few tokens the list tells)
+};
+
+struct Top { float best, low; int at; };   // the maximum, the lowest number, the first token that has the maximum
+__device__ __forceinline__ void merge(Top& t, float best, float low, int at) {
+  if (best > t.best || (best == t.best && at < t.at)) t.best = best, t.at = at;
+  t.low = fminf(t.low, low);
+}
+
 template <typename T>
 struct Row {
   Lds& s;
   const T* logits;
   int n, scale_bits;   // tokens; S
+  int piece0, piece1;  // the 16-byte pieces that this workgroup reads,
+  bool tail;           // ... and whether what is left behind the last whole one
+  int tid;
   float top;           // the maximum
   double per_unit;     // log2(e) / T
   float half_top, half_range, to_bin;   // distances are halved, so that none overflows
-  int tid;
+  struct Bins { int first, last; };
+  Bins of_k, of_p, of_min, of_u;        // what is gathered: the bins where top-k, top-p and min-p cut, and where the token is
 
-  // a logit as it counts: NaN as -infinity, +infinity as the largest number
-  static __device__ __forceinline__ float clean(T v) { return fminf(fmaxf((float)v, -__builtin_inff()), FLT_MAX); }
-
-  // f(logit, number) of every token; tokens of a thread in ascending order
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    constexpr int V = 16 / sizeof(T), U = 2;
-    typedef typename Piece<T>::vec vec;
+  __device__ Row(Lds& lds, const SampleArgs& a, int r) : s(lds), logits(static_cast<const T*>(a.logits) + (size_t)r * a.logits_stride), n(a.vocab), scale_bits(a.scale_bits),
+      piece0(0), piece1(a.vocab / V), tail(true), tid((int)threadIdx.x), of_k{BINS, BINS}, of_p{BINS, BINS}, of_min{BINS, BINS}, of_u{BINS, BINS} {}
+  __device__ void share(int g, int parts) {
     const int pieces = n / V;
-    for (int p0 = tid; p0 < pieces; p0 += U * NT) {
-      vec v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (p0 + u * NT < pieces) v[u] = *reinterpret_cast<const vec*>(logits + (size_t)(p0 + u * NT) * V);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (p0 + u * NT < pieces)
-#pragma unroll
-          for (int e = 0; e < V; ++e) f(clean(v[u][e]), (p0 + u * NT) * V + e);
-    }
-    const int rest = pieces * V + tid;
-    if (rest < n) f(clean(logits[rest]), rest);
+    piece0 = (int)((long)pieces * g / parts);
+    piece1 = (int)((long)pieces * (g + 1) / parts);
+    tail = g == parts - 1;
   }
 
+  static constexpr int V = 16 / sizeof(T);
+  typedef typename Piece<T>::vec vec;
+
+  // f(logit, number) of every token, those of a thread in ascending order; 2 U pieces on their way.  (A NaN is as far from the maximum as nothing else, and has no weight;
+  // +infinity counts as the largest number.)
+  template <int U>
+  __device__ __forceinline__ void load(vec (&v)[U], int p) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p + u * NT < piece1) v[u] = *reinterpret_cast<const vec*>(logits + (size_t)(p + u * NT) * V);
+  }
+  template <int U, typename F>
+  __device__ __forceinline__ void each(F f) const {
+    vec now[U];
+    load(now, piece0 + tid);
+    each(f, now);
+  }
+  // ... the first U of this thread being there
+  template <int U, typename F>
+  __device__ __forceinline__ void each(F f, vec (&now)[U]) const {
+    pieces([&](const vec& v, int i) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) f((float)v[e], i + e);
+    }, [&](float l, int i) { f(l, i); }, now);
+  }
+  // f(piece, number of its first token) of every piece, one(logit, number) of what is left behind the last whole one
+  template <int U, typename F, typename G>
+  __device__ __forceinline__ void pieces(F f, G one, vec (&now)[U]) const {
+    vec next[U];
+    for (int p = piece0 + tid; p < piece1; p += U * NT) {
+      load(next, p + U * NT);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u * NT < piece1) f(now[u], (p + u * NT) * V);
+        now[u] = next[u];
+      }
+    }
+    const int rest = n / V * V + tid;
+    if (tail && rest < n) one((float)logits[rest], rest);
+  }
+
+  // Sums up to and with this lane's over the wave: within rows of 16 lanes, then the rows' last lanes to the rows behind.
+  template <int CTRL, int ROWS>
+  static __device__ __forceinline__ unsigned moved(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false); }
+  template <int CTRL, int ROWS>
+  static __device__ __forceinline__ u64 moved(u64 v) { return (u64)moved<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | moved<CTRL, ROWS>((unsigned)v); }
+  template <typename N>
+  static __device__ __forceinline__ N wave_scan(N v) {
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
+    return v;
+  }
+  // The same over the block's threads; the total.  (Two barriers: the cells are free again behind them.)
+  template <typename N>
+  __device__ __forceinline__ N scan(N v, N* cells, N* total) const {
+    const int lane = tid & 63, wave = tid >> 6;
+    v = wave_scan(v);
+    if (lane == 63) cells[wave] = v;
+    __syncthreads();
+    N before = 0, all = 0;
+#pragma unroll
+    for (int u = 0; u < WAVES; ++u) {
+      const N c = cells[u];
+      if (u < wave) before += c;
+      all += c;
+    }
+    __syncthreads();
+    *total = all;
+    return v + before;
+  }
+  // `size` numbers become their running sums, SIZE / NT neighbours to a thread
+  template <int SIZE, typename N>
+  __device__ __forceinline__ void running(N* v, N* cells, N* total) const {
+    constexpr int PER = SIZE / NT;
+    N mine[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      mine[i] = v[tid * PER + i];
+      sum += mine[i];
+    }
+    N at = scan<N>(sum, cells, total) - sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      at += mine[i];
+      v[tid * PER + i] = at;
+    }
+    __syncthreads();
+  }
+  // the first of `size` running sums that reaches (OVER: passes) a goal, or the last; each wave looks for itself, a range of 64th parts at a time
+  template <bool OVER, typename N>
+  __device__ __forceinline__ int first_of(const N* sums, int size, N goal) const {
+    int lo = 0;   // all ahead of this lie below the goal
+    for (int step = size; step > 1;) {
+      const int len = min(step, size - lo);
+      step = (len + 63) / 64;
+      const int at = min(lo + ((tid & 63) + 1) * step, size) - 1;
+      const unsigned long long there = __ballot(OVER ? sums[at] > goal : sums[at] >= goal);
+      lo = min(lo + (there ? __builtin_ctzll(there) : 63) * step, size - 1);
+    }
+    return lo;
+  }
+
+  // ---- the maximum
+  // The first token that has it where that is what is asked for; else the lowest number, which keeps the bins narrow.  -infinity among the logits hides it, unless the temperature is high and the bins
+  // were wide without it.
+  __device__ __forceinline__ Top extremes(const Settings& s0) const {
+    Top t{-__builtin_inff(), __builtin_inff(), n};
+    if (s0.greedy) {
+      each<2>([&](float l, int i) { if (l > t.best) t.best = l, t.at = i; });
+    } else if (s0.temperature > 4.f) {
+      each<2>([&](float l, int) {
+        t.best = fmaxf(t.best, l);
+        t.low = l >= -FLT_MAX ? fminf(t.low, l) : t.low;
+      });
+    } else {
+      each<4>([&](float l, int) {
+        t.best = fmaxf(t.best, l);
+        t.low = fminf(t.low, l);
+      });
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const float best = __shfl_xor(t.best, d), low = __shfl_xor(t.low, d);
+      merge(t, best, low, __shfl_xor(t.at, d));
+    }
+    if ((tid & 63) == 0) s.wavef[0][tid >> 6] = t.best, s.wavef[1][tid >> 6] = t.low, s.wave32[tid >> 6] = (unsigned)t.at;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) merge(t, s.wavef[0][w], s.wavef[1][w], (int)s.wave32[w]);
+    __syncthreads();
+    return t;
+  }
+  __device__ __forceinline__ void set(const Top& t, float temperature) {
+    top = fminf(t.best, FLT_MAX);
+    per_unit = 1.4426950408889634074 / (double)temperature;
+    half_top = 0.5f * top;
+    const double reach = 0.5 * (scale_bits + 1.0) / per_unit;   // where weights of half a unit lie
+    half_range = (float)fmin(reach, (double)fminf(0.5f * top - 0.5f * fmaxf(t.low, -FLT_MAX), FLT_MAX));
+    to_bin = (float)BINS / half_range;
+    if (!(to_bin < 1e30f)) to_bin = 0.f;
+    for (int i = tid; i < 256; i += NT) s.exp2s[i] = exp2(i / 256.0);
+    __syncthreads();
+  }
+
+  // ---- weights
   __device__ __forceinline__ float distance(float l) const { return fmaf(-0.5f, l, half_top); }
-  __device__ __forceinline__ bool counts(float d) const { return d <= half_range; }   // (beyond: a weight of zero)
-  __device__ __forceinline__ int bin(float d) const { return min((int)(d * to_bin), BINS - 1); }
-  __device__ __forceinline__ double exponent(float l) const { return ((double)l - (double)top) * per_unit; }
+  __device__ __forceinline__ bool weighs(float d) const { return d <= half_range; }   // (beyond: a weight of zero)
+  __device__ __forceinline__ int bin(float d) const { return max(min((int)(d * to_bin), BINS - 1), 0); }
+  __device__ __forceinline__ double exponent(float l) const { return ((double)fminf(l, top) - (double)top) * per_unit; }
   // 2^z: z = i / 256 + r, a table and the series of 2^r to the fourth power (|r| <= 2^-9: off by 2^-54)
-  __device__ __forceinline__ double pow2(double z) const {
+  __device__ __forceinline__ double pow2(double z, int up = 0) const {   // (2^(z + up))
     const double magic = 6755399441055744.0;   // 1.5 2^52: what is added to it is rounded to a whole number
     const double t = fma(z, 256.0, magic);
     const int i = (int)(unsigned)__builtin_bit_cast(u64, t);
     const double r = fma(t - magic, -1.0 / 256, z);
     const double p = fma(fma(fma(fma(9.6181291076284771619791e-3, r, 5.5504108664821579953143e-2), r, 0.24022650695910071233355), r, 0.69314718055994530941723), r, 1.0);
-    return ldexp(p * s.exp2s[i & 255], i >> 8);
+    return ldexp(p * s.exp2s[i & 255], (i >> 8) + up);
   }
   // as a multiple of 2^-S, rounded
   __device__ __forceinline__ u64 weight(float l) const {
-    const double w = ldexp(pow2(exponent(l)), scale_bits) + 4503599627370496.0;   // (at most 2^51; 2^52 + w has w as its lowest bits)
+    const double w = pow2(exponent(l), scale_bits) + 4503599627370496.0;   // (at most 2^51; 2^52 + w has w as its lowest bits)
     return __builtin_bit_cast(u64, w) & 0x000fffffffffffffull;
   }
 
-  // Bins' counts into s.count and, if asked for, masses into s.mass, each then with those of all bins ahead of it; the totals.
-  __device__ __forceinline__ void histogram(bool masses, unsigned* total_count, u64* total_mass) {
+  // ---- bins
+  __device__ __forceinline__ void clear_bins() const {
     for (int i = tid; i < BINS; i += NT) s.count[i] = 0, s.mass[i] = 0;
     __syncthreads();
-    each([&](float l, int) {
-      const float d = distance(l);
-      if (counts(d)) {
-        const int b = bin(d);
+  }
+  __device__ __forceinline__ void fill_bins(bool masses) const {
+    vec first[1];
+    load(first, piece0 + tid);
+    fill_bins(masses, first);
+  }
+  // (A piece's bins and weights side by side, and only then what is added to them: one behind the other they would wait for each other's table entries.)
+  __device__ __forceinline__ void fill_bins(bool masses, vec (&first)[1]) const {
+    auto add = [&](float d, int b, u64 w) {
+      if (weighs(d)) {
         atomicAdd(&s.count[b], 1u);
-        if (masses) atomicAdd(&s.mass[b], weight(l));
+        if (masses) atomicAdd(&s.mass[b], w);
       }
-    });
+    };
+    pieces([&](const vec& v, int) {
+      float d[V];
+      int b[V];
+      u64 w[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        d[e] = distance((float)v[e]);
+        b[e] = bin(d[e]);
+      }
+      if (masses) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          w[e] = weight((float)v[e]);
+          if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (four at a time: eight take too many registers)
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) add(d[e], b[e], w[e]);
+    }, [&](float l, int) { add(distance(l), bin(distance(l)), weight(l)); }, first);
     __syncthreads();
-    scan_bins(s.count, s.mass, total_count, total_mass);
-  }
-  __device__ __forceinline__ void scan_bins(unsigned* count, u64* mass, unsigned* total_count, u64* total_mass) {
-    const unsigned a = count[2 * tid], b = count[2 * tid + 1], end = block_scan<unsigned>(a + b, s.wave32, total_count);
-    count[2 * tid] = end - b;
-    count[2 * tid + 1] = end;
-    const u64 c = mass[2 * tid], d = mass[2 * tid + 1], mass_end = block_scan<u64>(c + d, s.wave64, total_mass);
-    mass[2 * tid] = mass_end - d;
-    mass[2 * tid + 1] = mass_end;
-    __syncthreads();
-  }
-  // the first of `size` running sums that reaches (OVER: passes) a goal; it must be there
-  template <bool OVER, typename V>
-  __device__ __forceinline__ int first_of(const V* sums, int size, V goal) {
-    for (int i = tid; i < size; i += NT) {
-      const V at = sums[i], before = i ? sums[i - 1] : 0;
-      if (OVER ? at > goal && before <= goal : at >= goal && (i == 0 || before < goal)) s.found = i;
-    }
-    __syncthreads();
-    const int r = s.found;
-    __syncthreads();
-    return r;
   }
 
-  // The tokens that `wanted` names, sorted, with their running masses; how many, or more than CAP if they do not fit.
+  // ---- the list
+  __device__ __forceinline__ bool wanted(int b) const {
+    auto in = [b](const Bins& r) { return (int)((unsigned)(b - r.first) <= (unsigned)(r.last - r.first)); };
+    return (in(of_k) | in(of_p) | in(of_min) | in(of_u)) != 0;
+  }
+  __device__ __forceinline__ unsigned tokens_of(int b) const { return s.count[b] - (b ? s.count[b - 1] : 0); }
+  __device__ __forceinline__ float listed(int i) const { return value_of(~(unsigned)(s.list[i] >> 32)); }
+  __device__ __forceinline__ int number(int i) const { return (int)(unsigned)s.list[i]; }
+  static __device__ __forceinline__ u64 entry(float l, int i) { return (u64)~key_of(l) << 32 | (unsigned)i; }
+  // The tokens that `is` names (by logit and distance) into s.run, as they come; how many, or more than CAP if they do not fit.
   template <typename F>
-  __device__ __forceinline__ int gather(F wanted) {
+  __device__ __forceinline__ int gather(F is) const {
+    vec first[2];
+    load(first, piece0 + tid);
+    return gather(is, first);
+  }
+  template <typename F>
+  __device__ __forceinline__ int gather(F is, vec (&first)[2]) const {
     if (tid == 0) s.listed = 0;
     __syncthreads();
-    each([&](float l, int i) {
-      if (wanted(l)) {
-        const unsigned at = atomicAdd(&s.listed, 1u);
-        if (at < CAP) s.run[at] = (u64)~key_of(l) << 32 | (unsigned)i;
+    auto take = [&](float l, int i) {
+      const unsigned at = atomicAdd(&s.listed, 1u);
+      if (at < CAP) s.run[at] = entry(l, i);
+    };
+    pieces([&](const vec& v, int i) {
+      unsigned hits = 0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) hits |= (unsigned)is((float)v[e]) << e;
+      if (hits) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (hits >> e & 1) take((float)v[e], i + e);
       }
-    });
+    }, [&](float l, int i) { if (is(l)) take(l, i); }, first);
     __syncthreads();
-    const int m = (int)min(s.listed, (unsigned)CAP + 1);
-    if (m > CAP) {
-      __syncthreads();
-      return m;
+    return (int)min(s.listed, (unsigned)CAP + 1);
+  }
+  // is a token one of the bins that are gathered (or, by its value, one that min-p leaves)?
+  __device__ __forceinline__ bool of_bins(float l) const {
+    const float d = distance(l);
+    return (int)s.gathered[bin(d)] & (int)weighs(d);
+  }
+  __device__ __forceinline__ bool of_value(float l, double z_min) const { return (int)(exponent(l) >= z_min) & (int)weighs(distance(l)); }
+  // how many of `len` numbers (a multiple of 8) from `from` on are less than `mine`
+  static __device__ __forceinline__ int less(const u64* from, int len, u64 mine) {
+    int n = 0;
+    for (int j = 0; j < len; j += 8) {
+      u64 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = from[j + i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n += v[i] < mine;
     }
-    // up to 512: each token counts those ahead of it, several threads to a token; more: by exchanges
-    if (m <= 512) {
+    return n;
+  }
+  // s.run in order into s.list, then the masses of all tokens up to each.  Each token looks for its place: up to 128 among all; more, if the list is of whole bins, among those
+  // of its bin, which are brought together first (s.count holds the bins' running counts).  Where many are of one bin they are sorted by exchanges.
+  // masses: s.mass holds the bins' running masses, and the list may have gaps; else it begins with the first of all tokens and has none.
+  __device__ __forceinline__ void sort(int m, bool bins, bool masses) const {
+    auto bin_of = [&](u64 v) { return bin(distance(value_of(~(unsigned)(v >> 32)))); };
+    if (m <= 128 || (bins && m <= NT)) {
+      const bool together = m > 128;
+      u64* const from = together ? s.list : s.run;
+      for (int i = tid; i < 8 * 64; i += NT) from[m + i] = ~0ull;   // (what is read behind the last, and is not less than any)
+      if (together) {
+        for (int b = tid; b < BINS; b += NT) s.place[b] = wanted(b) ? tokens_of(b) : 0;
+        __syncthreads();
+        unsigned all;
+        running<BINS>(s.place, s.wave32, &all);
+        if (tid < m) {
+          const u64 v = s.run[tid];
+          s.list[atomicSub(&s.place[bin_of(v)], 1u) - 1u] = v;
+        }
+        // (a bin's place now is where it begins)
+      }
       int per = 1;   // threads to a token
       while (2 * per * m <= NT && per < 64) per *= 2;
       const int t = tid / per, sub = tid & (per - 1);
-      int ahead = 0;
-      const u64 mine = t < m ? s.run[t] : 0;
-      if (t < m)
-        for (int j = sub; j < m; j += per) ahead += s.run[j] < mine;
+      __syncthreads();
+      int lo = 0, many = t < m ? m : 0;
+      u64 mine = 0;
+      if (t < m) {
+        mine = from[t];
+        if (together) {
+          const int b = bin_of(mine);
+          lo = (int)s.place[b];
+          many = (int)tokens_of(b);
+        }
+      }
+      const int len = ((many + per - 1) / per + 7) / 8 * 8;   // (what lies behind a bin's tokens is not less than they are)
+      int ahead = less(from + lo + sub * len, len, mine);
       for (int d = 1; d < per; d <<= 1) ahead += __shfl_xor(ahead, d);
-      if (t < m && sub == 0) s.list[ahead] = mine;
+      __syncthreads();
+      if (t < m && sub == 0) s.list[lo + ahead] = mine;
+      __syncthreads();
     } else {
       for (int i = tid; i < CAP; i += NT) s.list[i] = i < m ? s.run[i] : ~0ull;
-      int size = 1024;
-      if (m > 1024) size = 2048;
+      int size = 256;
+      while (size < m) size *= 2;
       for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
           __syncthreads();
@@ -211,46 +433,123 @@ struct Row {
             }
           }
         }
+      __syncthreads();
+    }
+    for (int i = tid; i < (m <= NT ? NT : CAP); i += NT) {
+      u64 w = 0;
+      if (i < m) {
+        const float l = listed(i);
+        w = weight(l);
+        if (masses) {
+          const int b = bin(distance(l)), before = i ? bin_of(s.list[i - 1]) : -1;
+          if (b != before) w += (b ? s.mass[b - 1] : 0) - (before >= 0 ? s.mass[before] : 0);
+        }
+      }
+      s.run[i] = w;
     }
     __syncthreads();
-    // two neighbours to a thread
     u64 total;
-    const u64 a = 2 * tid < m ? weight(listed(2 * tid)) : 0, b = 2 * tid + 1 < m ? weight(listed(2 * tid + 1)) : 0;
-    const u64 end = block_scan<u64>(a + b, s.wave64, &total);
-    s.run[2 * tid] = end - b;
-    s.run[2 * tid + 1] = end;
-    __syncthreads();
-    return m;
+    if (m <= NT) running<NT>(s.run, s.wave64, &total);
+    else running<CAP>(s.run, s.wave64, &total);
   }
-  __device__ __forceinline__ float listed(int i) const { return value_of(~(unsigned)(s.list[i] >> 32)); }
-  __device__ __forceinline__ int number(int i) const { return (int)(unsigned)s.list[i]; }
 
+  // ---- which bins hold the places that matter, s.count and s.mass being running sums.  `have_masses`: not, where top_k tokens are to be listed from the first on.
+  __device__ __forceinline__ void plan(const Settings& t, bool have_masses, unsigned tokens, u64 total) {
+    const bool cut_k = t.top_k && (unsigned)t.top_k < tokens;
+    const int bk = cut_k ? first_of<false>(s.count, BINS, (unsigned)t.top_k) : BINS - 1;
+    const bool here = have_masses && cut_k;
+    // the kept tokens' mass lies between these (the token where top-k cuts may weigh nothing)
+    u64 lo = here ? max(bk ? s.mass[bk - 1] : 0, (u64)1) : total, hi = here ? s.mass[bk] : total;
+    int p0 = BINS, p1 = BINS, m0 = BINS, m1 = BINS, u0 = BINS, u1 = BINS;   // (no bin)
+    if (have_masses && t.cut_p) {
+      lo = max(part_up(t.top_p, lo), (u64)1);
+      hi = max(part_up(t.top_p, hi), (u64)1);
+      p0 = first_of<false>(s.mass, BINS, lo);
+      p1 = first_of<false>(s.mass, BINS, hi);
+      hi = s.mass[p1];
+    }
+    if (have_masses && t.cut_min) {   // (a token's bin and its weight are rounded apart from each other: a bin more on either side)
+      const int m = min((int)fmin(-0.5 * t.z_min / per_unit * (double)to_bin, (double)BINS), BINS - 1);
+      m0 = max(m - 1, 0);
+      m1 = min(m + 1, BINS - 1);
+      lo = min(lo, max(m > 1 ? s.mass[m - 2] : 0, (u64)1));
+      hi = min(hi, s.mass[m1]);
+    }
+    if (have_masses) {
+      u0 = first_of<true>(s.mass, BINS, part_of(t.u, lo));
+      u1 = first_of<true>(s.mass, BINS, part_of(t.u, hi));
+    }
+    static_assert(BINS == 4 * NT, "a thread's bins");
+    of_k.first = here ? bk : have_masses ? BINS : 0;
+    of_k.last = here || !have_masses ? bk : BINS;
+    of_p.first = p0, of_p.last = p1;
+    of_min.first = m0, of_min.last = m1;
+    of_u.first = u0, of_u.last = u1;
+    unsigned flags = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) flags |= wanted(tid * 4 + i) ? 1u << (8 * i) : 0u;
+    reinterpret_cast<unsigned*>(s.gathered)[tid] = flags;
+    __syncthreads();
+  }
+
+  // ---- the token, from the sorted list of m tokens and the bins
+  __device__ __forceinline__ int choose(const Settings& t, bool bins, unsigned tokens, u64 total, int m, u64* kept_mass) const {
+    u64 kept = bins ? total : s.run[m - 1];
+    if (t.top_k && (!bins || (unsigned)t.top_k < tokens)) {
+      int rank = t.top_k - 1;   // its place in the list
+      if (bins) {
+        const int b = first_of<false>(s.count, BINS, (unsigned)t.top_k);
+        rank -= (int)(b ? s.count[b - 1] : 0);
+        for (int i = tid; i < m; i += NT)
+          if (bin(distance(listed(i))) == b && (i == 0 || bin(distance(listed(i - 1))) != b)) s.found = i;
+        __syncthreads();
+        rank += s.found;
+        __syncthreads();
+      }
+      kept = s.run[min(rank, m - 1)];
+    }
+    if (t.cut_p) kept = s.run[first_of<false>(s.run, m, max(part_up(t.top_p, kept), (u64)1))];
+    if (t.cut_min) {   // (the first of all always stays)
+      if (tid == 0) s.found = -1;
+      __syncthreads();
+      for (int i = tid; i < m; i += NT)
+        if (exponent(listed(i)) >= t.z_min && (i + 1 == m || !(exponent(listed(i + 1)) >= t.z_min))) s.found = i;
+      __syncthreads();
+      u64 least = s.found >= 0 ? s.run[s.found] : 0;
+      __syncthreads();
+      if (bins && of_min.first > 0) least = max(least, s.mass[of_min.first - 1]);
+      kept = min(kept, least);
+    }
+    *kept_mass = kept;
+    return first_of<true>(s.run, m, part_of(t.u, kept));
+  }
+
+  // ---- where a bin's tokens do not fit the list: place by place, a crowded bin's tokens told apart by the digits of their keys
   enum Goal { RANK, REACH, PASS };
   struct Place { u64 mass; int number; float logit; };   // of the tokens up to the place, with its own; the token there (PASS)
-
-  // A place within bin b: its goal-th token (RANK), or the first at which the bin's masses reach or pass `goal`.
-  __device__ __forceinline__ Place within(int b, Goal kind, u64 goal) {
+  __device__ __forceinline__ Place within(int b, Goal kind, u64 goal) const {
     unsigned prefix = 0;
     int shift = 32;
     u64 base = 0;
     for (;;) {
       const int m = gather([&](float l) {
         const float d = distance(l);
-        return counts(d) && bin(d) == b && (shift == 32 || key_of(l) >> shift == prefix);
+        return weighs(d) && bin(d) == b && (shift == 32 || key_of(l) >> shift == prefix);
       });
       if (m <= CAP) {
+        sort(m, false, false);
         const int i = kind == RANK ? (int)goal - 1 : kind == REACH ? first_of<false>(s.run, m, goal) : first_of<true>(s.run, m, goal);
         return {base + s.run[i], number(i), listed(i)};
       }
       if (shift == 0) break;
-      // too many: told apart by the next digit of their keys
       const int digits = shift == 10 ? 10 : 11, next = shift - digits, mask = (1 << digits) - 1;
+      __syncthreads();
       for (int i = tid; i < BINS; i += NT) s.count2[i] = 0, s.mass2[i] = 0;
       __syncthreads();
-      each([&](float l, int) {
+      each<1>([&](float l, int) {
         const float d = distance(l);
         const unsigned key = key_of(l);
-        if (counts(d) && bin(d) == b && (shift == 32 || key >> shift == prefix)) {
+        if (weighs(d) && bin(d) == b && (shift == 32 || key >> shift == prefix)) {
           const int digit = mask - (int)(key >> next & (unsigned)mask);   // (descending)
           atomicAdd(&s.count2[digit], 1u);
           atomicAdd(&s.mass2[digit], weight(l));
@@ -259,7 +558,8 @@ struct Row {
       __syncthreads();
       unsigned tc;
       u64 tm;
-      scan_bins(s.count2, s.mass2, &tc, &tm);
+      running<BINS>(s.count2, s.wave32, &tc);
+      running<BINS>(s.mass2, s.wave64, &tm);
       const int at = kind == RANK ? first_of<false>(s.count2, BINS, (unsigned)goal)
                                   : kind == REACH ? first_of<false>(s.mass2, BINS, goal) : first_of<true>(s.mass2, BINS, goal);
       const u64 ahead = at ? s.mass2[at - 1] : 0;
@@ -277,12 +577,12 @@ struct Row {
     if (kind == PASS) {   // each thread counts a run of its own
       const int run = (n + NT - 1) / NT, lo = min(tid * run, n), hi = min(lo + run, n);
       unsigned mine = 0, total;
-      for (int i = lo; i < hi; ++i) mine += key_of(clean(logits[i])) == prefix;
-      const unsigned end = block_scan<unsigned>(mine, s.wave32, &total);
+      for (int i = lo; i < hi; ++i) mine += key_of((float)logits[i]) == prefix;
+      const unsigned end = scan<unsigned>(mine, s.wave32, &total);
       if (end >= which && end - mine < which) {
         unsigned at = end - mine;
         for (int i = lo; i < hi; ++i)
-          if (key_of(clean(logits[i])) == prefix && ++at == which) s.found = i;
+          if (key_of((float)logits[i]) == prefix && ++at == which) s.found = i;
       }
       __syncthreads();
       num = s.found;
@@ -291,7 +591,7 @@ struct Row {
     return {base + which * w, num, l};
   }
   // a place among all tokens, from the bins' running sums
-  __device__ __forceinline__ Place among(Goal kind, u64 goal) {
+  __device__ __forceinline__ Place among(Goal kind, u64 goal) const {
     const int b = kind == RANK ? first_of<false>(s.count, BINS, (unsigned)goal)
                                : kind == REACH ? first_of<false>(s.mass, BINS, goal) : first_of<true>(s.mass, BINS, goal);
     const u64 ahead = b ? s.mass[b - 1] : 0;
@@ -299,166 +599,233 @@ struct Row {
     p.mass += ahead;
     return p;
   }
+  __device__ __forceinline__ Place by_places(const Settings& t, unsigned tokens, u64 total, u64* kept_mass) const {
+    u64 kept = total;
+    Place place{0, 0, top};
+    for (int step = 0; step < 4; ++step) {
+      if ((step == 0 && !(t.top_k && (unsigned)t.top_k < tokens)) || (step == 1 && !t.cut_p) || (step == 2 && !t.cut_min)) continue;
+      if (step == 2) {
+        u64 mine = 0, sum;
+        each<1>([&](float l, int) { if (weighs(distance(l)) && exponent(l) >= t.z_min) mine += weight(l); });
+        scan<u64>(mine, s.wave64, &sum);
+        kept = min(kept, sum);
+        continue;
+      }
+      place = among(step == 0 ? RANK : step == 1 ? REACH : PASS,
+                    step == 0 ? (u64)t.top_k : step == 1 ? max(part_up(t.top_p, kept), (u64)1) : part_of(t.u, kept));
+      if (step < 3) kept = place.mass;
+    }
+    *kept_mass = kept;
+    return place;
+  }
+
+  // ---- a whole row.  ready: s.count and s.mass hold the bins of all of it, s.run its list of m tokens or, m > CAP, nothing.
+  __device__ __forceinline__ void finish(const SampleArgs& a, int r, const Settings& t, bool ready, int m) {
+    bool bins = false, masses = t.masses();
+    unsigned tokens = 0;
+    u64 total = 0, kept = 0;
+    int token = 0;
+    float logit = top;
+    bool by_value = t.by_value();
+    for (;;) {
+      if (!by_value && !ready) {
+        clear_bins();
+        fill_bins(masses);
+        running<BINS>(s.count, s.wave32, &tokens);
+        running<BINS>(s.mass, s.wave64, &total);
+        plan(t, masses, tokens, total);
+      } else if (!by_value) {
+        tokens = s.count[BINS - 1];
+        total = s.mass[BINS - 1];
+      }
+      if (!ready) m = by_value ? gather([&](float l) { return of_value(l, t.z_min); }) : gather([&](float l) { return of_bins(l); });
+      bins = !by_value && masses;
+      if (m <= CAP || bins) break;
+      by_value = ready = false;
+      masses = true;
+    }
+    if (m <= CAP) {
+      sort(m, !by_value, bins);
+      const int i = choose(t, bins, tokens, total, m, &kept);
+      token = number(i);
+      logit = listed(i);
+    } else {
+      const Place p = by_places(t, tokens, total, &kept);
+      token = p.number;
+      logit = p.logit;
+    }
+    if (tid == 0) {
+      a.tokens[r] = token;
+      if (a.probs) a.probs[r] = (float)(pow2(exponent(logit)) / ldexp((double)kept, -scale_bits));
+    }
+  }
 };
 
+__device__ __forceinline__ void leave_first(const SampleArgs& a, int r, const Top& t) {
+  const bool any = t.best > -__builtin_inff();
+  a.tokens[r] = any ? t.at : -1;
+  if (a.probs) a.probs[r] = any ? 1.f : 0.f;
+}
+
+// a workgroup to a row
 template <typename T>
 __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   __shared__ Lds s;
-  const int r = (int)blockIdx.x, tid = (int)threadIdx.x, wave = tid >> 6;
-  Row<T> row{s, static_cast<const T*>(a.logits) + (size_t)r * a.logits_stride, a.vocab, a.scale_bits};
-  row.tid = tid;
-  // settings, those that are off as such
-  float temperature = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
-  float u = a.uniform ? a.uniform[r] : 0.f;
-  int top_k = a.top_k ? a.top_k[r] : 0;
-  if (!(temperature == temperature)) temperature = 1.f;
-  if (top_k <= 0 || top_k >= a.vocab) top_k = 0;
-  const bool cut_p = top_p < 1.f, cut_min = min_p > 0.f;
-  min_p = fminf(min_p, 1.f);
-  u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);   // (a NaN: 0)
-  const bool greedy = !a.uniform || temperature <= 0.f || top_k == 1 || top_p <= 0.f;
-
-  // the maximum, the first token that has it, the lowest logit
-  float best = -__builtin_inff(), low = __builtin_inff();
-  int at = a.vocab;
-  row.each([&](float l, int i) {
-    if (l > best) best = l, at = i;
-    if (l >= -FLT_MAX) low = fminf(low, l);
-  });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const float o = __shfl_xor(best, d);
-    const int oi = __shfl_xor(at, d);
-    if (o > best || (o == best && oi < at)) best = o, at = oi;
-    low = fminf(low, __shfl_xor(low, d));
-  }
-  if ((tid & 63) == 0) s.wavef[0][wave] = best, s.wavef[1][wave] = low, s.wave32[wave] = (unsigned)at;
-  if (tid < 256) s.exp2s[tid] = exp2(tid / 256.0);
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < WAVES; ++v) {
-    const float o = s.wavef[0][v];
-    const int oi = (int)s.wave32[v];
-    if (o > best || (o == best && oi < at)) best = o, at = oi;
-    low = fminf(low, s.wavef[1][v]);
-  }
-  __syncthreads();
-  if (best == -__builtin_inff() || greedy) {
-    if (tid == 0) {
-      const bool any = best > -__builtin_inff();
-      a.tokens[r] = any ? at : -1;
-      if (a.probs) a.probs[r] = any ? 1.f : 0.f;
-    }
+  const int r = (int)blockIdx.x;
+  Row<T> row(s, a, r);
+  const Settings t(a, r);
+  const Top top = row.extremes(t);
+  if (top.best == -__builtin_inff() || t.greedy) {
+    if (threadIdx.x == 0) leave_first(a, r, top);
     return;
   }
-  row.top = best;
-  row.per_unit = 1.4426950408889634074 / (double)temperature;
-  row.half_top = 0.5f * best;
-  const double reach = 0.5 * (a.scale_bits + 1.0) / row.per_unit;   // where weights of half a unit lie
-  row.half_range = (float)fmin(reach, (double)fminf(0.5f * best - 0.5f * low, FLT_MAX));
-  row.to_bin = (float)BINS / row.half_range;
-  if (!(row.to_bin < 1e30f)) row.to_bin = 0.f;
+  row.set(top, t.temperature);
+  row.finish(a, r, t, false, 0);
+}
 
-  const double z_min = cut_min ? log2((double)min_p) : 0.0;
-  auto likely = [&](float l) { return row.exponent(l) >= z_min; };
-  unsigned tokens = 0;
-  u64 total = 0, goal_p = 0;
-  int listed = CAP + 1;                            // tokens in the list, if it holds all that can be kept
-  bool by_value = !top_k && !cut_p && cut_min;     // ... which then are those that min-p leaves
-  for (bool masses = !top_k;;) {
-    int last_bin = -1;                             // ... or those of the bins up to this
-    if (!by_value) {
-      row.histogram(masses, &tokens, &total);
-      if (top_k && (unsigned)top_k >= tokens) {    // (the rest have no weight)
-        top_k = 0;
-        by_value = !cut_p && cut_min;
-        if (!masses) {
-          masses = true;
-          continue;
-        }
-      }
-      if (top_k || cut_p) {
-        int b;
-        if (top_k) {
-          b = row.template first_of<false>(s.count, BINS, (unsigned)top_k);
-        } else {
-          goal_p = part_up(top_p, total);
-          goal_p = goal_p ? goal_p : 1;
-          b = row.template first_of<false>(s.mass, BINS, goal_p);
-        }
-        if (s.count[b] <= CAP) last_bin = b;
-      }
-    }
-    if (by_value || last_bin >= 0)
-      listed = row.gather([&](float l) {
-        const float d = row.distance(l);
-        return row.counts(d) && (by_value ? likely(l) : row.bin(d) <= last_bin);
-      });
-    if (listed <= CAP || (masses && !by_value)) break;
-    by_value = false;
-    masses = true;
+// What the workgroups of a row leave each other.  The first launch clears what the others add to.
+struct Shared {
+  u64 mass[BINS];
+  u64 list[CAP];
+  unsigned count[BINS];
+  Top top[PARTS];
+  unsigned listed, arrived;
+  unsigned pad[14];
+};
+
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_top_kernel(const SampleArgs a) {
+  __shared__ Lds s;
+  const int g = (int)blockIdx.x, parts = (int)gridDim.x, r = (int)blockIdx.y;
+  Shared& h = static_cast<Shared*>(a.workspace)[r];
+  Row<T> row(s, a, r);
+  row.share(g, parts);
+  const Top t = row.extremes(Settings(a, r));
+  if (threadIdx.x == 0) {
+    h.top[g] = t;
+    if (g == 0) h.listed = h.arrived = 0;
   }
-  if (top_k && listed <= CAP) listed = min(listed, top_k);
-  u64 kept = total;
-  int token = 0;
-  float logit = best;
-  if (listed <= CAP) {
-    // all that can be kept stands in the list, in order
-    if (cut_p) {
-      if (!goal_p) goal_p = part_up(top_p, s.run[listed - 1]);
-      goal_p = goal_p ? goal_p : 1;
-      listed = min(listed, row.template first_of<false>(s.run, listed, goal_p) + 1);
-    }
-    if (cut_min) {   // (the first of the list always stays)
-      for (int i = tid; i < listed; i += NT)
-        if (likely(row.listed(i)) && (i + 1 == listed || !likely(row.listed(i + 1)))) s.found = i;
-      __syncthreads();
-      listed = s.found + 1;
-      __syncthreads();
-    }
-    kept = s.run[listed - 1];
-    const int i = row.template first_of<true>(s.run, listed, part_of(u, kept));
-    token = row.number(i);
-    logit = row.listed(i);
-  } else {
-    for (int step = 0; step < 4; ++step) {
-      if ((step == 0 && !top_k) || (step == 1 && !cut_p) || (step == 2 && !cut_min)) continue;
-      if (step == 2) {
-        u64 mine = 0, sum;
-        row.each([&](float l, int) { if (row.counts(row.distance(l)) && likely(l)) mine += row.weight(l); });
-        block_scan<u64>(mine, s.wave64, &sum);
-        kept = sum < kept ? sum : kept;
-        continue;
-      }
-      const u64 up = part_up(top_p, kept);
-      const auto place = row.among(step == 0 ? Row<T>::RANK : step == 1 ? Row<T>::REACH : Row<T>::PASS,
-                                   step == 0 ? (u64)top_k : step == 1 ? (up ? up : 1) : part_of(u, kept));
-      if (step < 3) {
-        kept = place.mass;
-      } else {
-        token = place.number;
-        logit = place.logit;
-      }
-    }
+  for (int i = BINS * g / parts + (int)threadIdx.x; i < BINS * (g + 1) / parts; i += NT) h.mass[i] = 0, h.count[i] = 0;
+}
+
+__device__ __forceinline__ Top top_of(const Shared& h, int parts) {
+  Top t{-__builtin_inff(), __builtin_inff(), 0x7fffffff};
+  const int lane = (int)threadIdx.x & 63;
+  if (lane < parts) t = h.top[lane];
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const float best = __shfl_xor(t.best, d), low = __shfl_xor(t.low, d);
+    merge(t, best, low, __shfl_xor(t.at, d));
   }
-  if (tid == 0) {
-    a.tokens[r] = token;
-    if (a.probs) a.probs[r] = (float)(row.pow2(row.exponent(logit)) / ldexp((double)kept, -a.scale_bits));
+  return t;
+}
+
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_bins_kernel(const SampleArgs a) {
+  __shared__ Lds s;
+  const int r = (int)blockIdx.y;
+  Shared& h = static_cast<Shared*>(a.workspace)[r];
+  Row<T> row(s, a, r);
+  const Settings t(a, r);
+  row.share((int)blockIdx.x, (int)gridDim.x);
+  typename Row<T>::vec first[1];   // (on its way while the maximum is looked up)
+  row.load(first, row.piece0 + row.tid);
+  const Top top = top_of(h, (int)gridDim.x);
+  if (top.best == -__builtin_inff() || t.greedy || t.by_value()) return;
+  row.set(top, t.temperature);
+  row.clear_bins();
+  row.fill_bins(t.masses(), first);
+  for (int i = (int)threadIdx.x; i < BINS; i += NT) {
+    if (s.count[i]) atomicAdd(&h.count[i], s.count[i]);
+    if (s.mass[i]) atomicAdd(&h.mass[i], s.mass[i]);
   }
 }
 
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
+  __shared__ Lds s;
+  const int r = (int)blockIdx.y, tid = (int)threadIdx.x;
+  Shared& h = static_cast<Shared*>(a.workspace)[r];
+  Row<T> row(s, a, r);
+  const Settings t(a, r);
+  row.share((int)blockIdx.x, (int)gridDim.x);
+  typename Row<T>::vec first[2];   // (on its way while the bins are looked through)
+  row.load(first, row.piece0 + tid);
+  unsigned count[BINS / NT];
+  u64 mass[BINS / NT];
+#pragma unroll
+  for (int i = 0; i < BINS / NT; ++i) count[i] = h.count[i * NT + tid], mass[i] = h.mass[i * NT + tid];
+  const Top top = top_of(h, (int)gridDim.x);
+  if (top.best == -__builtin_inff() || t.greedy) {
+    if (blockIdx.x == 0 && tid == 0) leave_first(a, r, top);
+    return;
+  }
+  row.set(top, t.temperature);
+  const bool by_value = t.by_value();
+  if (!by_value) {
+#pragma unroll
+    for (int i = 0; i < BINS / NT; ++i) s.count[i * NT + tid] = count[i], s.mass[i * NT + tid] = mass[i];
+    __syncthreads();
+    unsigned tokens;
+    u64 total;
+    row.template running<BINS>(s.count, s.wave32, &tokens);
+    row.template running<BINS>(s.mass, s.wave64, &total);
+    row.plan(t, t.masses(), tokens, total);
+  }
+  const int m = by_value ? row.gather([&](float l) { return row.of_value(l, t.z_min); }, first) : row.gather([&](float l) { return row.of_bins(l); }, first);
+  // this part's tokens to the row's list (in any order: it is sorted), and whoever is last ends the row
+  if (tid == 0) s.found = (int)min(__hip_atomic_fetch_add(&h.listed, (unsigned)m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), 1u << 30);
+  __syncthreads();
+  const int base = s.found;
+  if (m <= CAP)
+    for (int i = tid; i < m && base + i < CAP; i += NT) __hip_atomic_store(&h.list[base + i], s.run[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) s.found = __hip_atomic_fetch_add(&h.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  __syncthreads();
+  if (!s.found) return;
+  const int all = (int)min(__hip_atomic_load(&h.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), (unsigned)CAP + 1);
+  __syncthreads();
+  if (all <= CAP)
+    for (int i = tid; i < all; i += NT) s.run[i] = __hip_atomic_load(&h.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  row.share(0, 1);
+  row.finish(a, r, t, true, all);
+}
+
+template <typename T>
+hipError_t launch_type(const SampleArgs& a, int parts, hipStream_t st) {
+  if (!a.workspace || parts == 1) {
+    hipLaunchKernelGGL((sample_kernel<T>), dim3((unsigned)a.rows), dim3(NT), 0, st, a);
+  } else {
+    const dim3 grid((unsigned)parts, (unsigned)a.rows), block(NT);
+    hipLaunchKernelGGL((sample_top_kernel<T>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((sample_bins_kernel<T>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((sample_pick_kernel<T>), grid, block, 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+// A row to a workgroup, or to as many as give every CU one.  Measured in graphs, bf16, top-k 50 and top-p 0.95, us in one launch / shared out: one row of 16000 tokens 16 / 20, of 32000 20 / 20,
+// of 64000 29 / 20, of 128000 45 / 20; 64 rows of 64000 29 / 26, of 128000 46 / 31; 128 rows of 64000 30 / 31, of 128000 51 / 41; top-p 0.9 alone 1 x 128000 72 / 26, 64 x 128000 88 / 54.
+// 256 rows of 50257 in fp32 51 / 60 (two to a row).
+int parts_of(const SampleArgs& a) {
+  const int parts = a.rows >= 256 ? 1 : 256 / a.rows < 32 ? 256 / a.rows : 32;
+  return (long)a.vocab * (parts - 1) >= 24000L * parts ? parts : 1;
+}
+
 }  // namespace
+
+size_t sample_workspace_bytes(const SampleArgs& a) { return parts_of(a) > 1 ? (size_t)a.rows * sizeof(Shared) : 0; }
 
 hipError_t launch_sample(const SampleArgs& args, int dtype, hipStream_t st) {
   SampleArgs a = args;
   int bits = 0;   // vocab <= 2^bits
   while ((1 << bits) < a.vocab) ++bits;
   a.scale_bits = 62 - bits < 51 ? 62 - bits : 51;
-  const dim3 grid((unsigned)a.rows), block(NT);
-  if (dtype == T_F16) hipLaunchKernelGGL((sample_kernel<_Float16>), grid, block, 0, st, a);
-  else if (dtype == T_BF16) hipLaunchKernelGGL((sample_kernel<__bf16>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((sample_kernel<float>), grid, block, 0, st, a);
-  return hipGetLastError();
+  const int parts = parts_of(a);
+  if (dtype == T_F16) return launch_type<_Float16>(a, parts, st);
+  return dtype == T_BF16 ? launch_type<__bf16>(a, parts, st) : launch_type<float>(a, parts, st);
 }
 
 }  // namespace relay
