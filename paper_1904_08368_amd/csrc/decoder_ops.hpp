@@ -41,7 +41,8 @@ struct RouteArgs {
   float* weights;
   void* workspace;
   unsigned* counters;   // set by the launcher, as is
-  double* logits;       // [tokens][experts]
+  double* logits;       // [splits][tokens][experts]
+  int splits;           // parts of the channels whose sums are left apart
 };
 constexpr int kRouteExperts = 1024, kRouteTopK = 64;
 size_t route_workspace_bytes(const RouteArgs& a);

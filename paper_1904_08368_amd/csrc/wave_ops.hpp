@@ -1,13 +1,31 @@
-// Sums over the 64 lanes of a wave, in a fixed order, the same bits in every lane.
+// Sums and maxima over the 64 lanes of a wave, in a fixed order, the same bits in every lane.
 #pragma once
 #include "attn_common.hpp"
 
 namespace relay {
 
 template <int CTRL>
-__device__ __forceinline__ float lane_moved(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+__device__ __forceinline__ unsigned lane_moved(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ __forceinline__ float lane_moved(float v) { return __builtin_bit_cast(float, lane_moved<CTRL>(__builtin_bit_cast(unsigned, v))); }
+template <int CTRL, typename V>   // (64 bits)
+__device__ __forceinline__ V lane_moved64(V v) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+  return __builtin_bit_cast(V, (unsigned long long)lane_moved<CTRL>((unsigned)(u >> 32)) << 32 | lane_moved<CTRL>((unsigned)u));
 }
+// the values of the lane's own row of 16 and of the other of its pair, of its own half and of the other
+template <typename V>
+struct Pair64 { V a, b; };
+template <bool HALVES, typename V>
+__device__ __forceinline__ Pair64<V> pair64(V v) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+  const unsigned lo = (unsigned)u, hi = (unsigned)(u >> 32);
+  const auto l = HALVES ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+  const auto h = HALVES ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+  const unsigned l0 = l[0], l1 = l[1], h0 = h[0], h1 = h[1];
+  return {__builtin_bit_cast(V, (unsigned long long)h0 << 32 | l0), __builtin_bit_cast(V, (unsigned long long)h1 << 32 | l1)};
+}
+
 // neighbours, pairs of neighbours, halves of eight and of sixteen mirrored; then the sixteens
 __device__ __forceinline__ float wave_sum(float v) {
   v += lane_moved<0xB1>(v);
@@ -15,6 +33,21 @@ __device__ __forceinline__ float wave_sum(float v) {
   v += lane_moved<0x141>(v);
   v += lane_moved<0x140>(v);
   return sum_quarters(v);
+}
+template <typename V, typename F>
+__device__ __forceinline__ V wave_fold64(V v, F f) {
+  v = f(v, lane_moved64<0xB1>(v));
+  v = f(v, lane_moved64<0x4E>(v));
+  v = f(v, lane_moved64<0x141>(v));
+  v = f(v, lane_moved64<0x140>(v));
+  const Pair64<V> rows = pair64<false>(v);
+  v = f(rows.a, rows.b);
+  const Pair64<V> halves = pair64<true>(v);
+  return f(halves.a, halves.b);
+}
+__device__ __forceinline__ double wave_sum64(double v) { return wave_fold64(v, [](double a, double b) { return a + b; }); }
+__device__ __forceinline__ unsigned long long wave_max64(unsigned long long v) {
+  return wave_fold64(v, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
 }
 
 }  // namespace relay
