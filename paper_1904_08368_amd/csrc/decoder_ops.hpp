@@ -66,6 +66,9 @@ struct ExpertsArgs {
   FastDiv fd_top_k;
   void* h;        // [pairs][inter]
   float* parts;   // [pairs][channels]
+  int* sorted;    // [pairs]
+  int* blocks;    // [most_blocks][3]
+  int most_blocks;
   // (a group as long as the row is the row's chunks of 128, whole, as for the dense layers)
   __host__ __device__ int group_of(int k) const { return group < k ? group : (k + 127) / 128 * 128; }
 };

@@ -5,24 +5,36 @@
 // up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
 // reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 117 and 70 (4.6 and 3.9 TB/s).
 // Codes become operands as in the dense kernels (16 + code, the sums of x taking the zero points out).
+#include <type_traits>
+
 #include "decoder_ops.hpp"
+#include "lds_dma.hpp"
 #include "w4_common.hpp"
 
 namespace relay {
 namespace {
 
+constexpr int kBlock = 64;   // pairs of one expert in a tile
+
 // The pairs that name expert e, of those from `from` on the first `most`, into this wave's rows; how many there are in all, and which is the first.
 struct Found { int all, first; };
 __device__ __forceinline__ Found pairs_of(const int32_t* chosen, int pairs, int e, int from, int most, int* rows, int lane) {
   Found f{0, pairs};
-  for (int p = 0; p < pairs; p += 64) {
-    const bool mine = p + lane < pairs && chosen[min(p + lane, pairs - 1)] == e;
-    const unsigned long long set = __ballot(mine);
-    if (!set) continue;
-    if (!f.all) f.first = p + __builtin_ctzll(set);
-    const int at = f.all + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u)) - from;
-    if (mine && at >= 0 && at < most) rows[at] = p + lane;
-    f.all += __builtin_popcountll(set);
+  for (int p0 = 0; p0 < pairs; p0 += 512) {   // (eight loads on their way: one by one each waits for its own)
+    int named[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) named[i] = chosen[min(p0 + i * 64 + lane, pairs - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = p0 + i * 64;
+      const bool mine = p + lane < pairs && named[i] == e;
+      const unsigned long long set = __ballot(mine);
+      if (!set) continue;
+      if (!f.all) f.first = p + __builtin_ctzll(set);
+      const int at = f.all + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0u)) - from;
+      if (mine && at >= 0 && at < most) rows[at] = p + lane;
+      f.all += __builtin_popcountll(set);
+    }
   }
   return f;
 }
@@ -241,6 +253,223 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
   }
 }
 
+// Pairs by their experts, for the tiles: sorted, and the blocks of up to 64 of them that one expert has (in a.blocks: expert, first place, how many; behind the last an expert of -1).  One workgroup.
+// The order of an expert's pairs is of no consequence: a row of a product does not hang on its place.
+constexpr int kPlanThreads = 1024;
+static_assert(kRouteExperts <= kPlanThreads, "an expert to a thread");
+__global__ __launch_bounds__(kPlanThreads) void experts_plan_kernel(const ExpertsArgs a) {
+  __shared__ int count[kPlanThreads], sums[2][kPlanThreads / 64];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  count[tid] = 0;
+  __syncthreads();
+  for (int p = tid; p < a.pairs; p += kPlanThreads) {
+    const int e = a.chosen[p];
+    if ((unsigned)e < (unsigned)a.experts) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  const int n = count[tid], blocks = (n + kBlock - 1) / kBlock;
+  int pairs_to = n, blocks_to = blocks;   // up to and with this expert's
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(pairs_to, d), q = __shfl_up(blocks_to, d);
+    if (lane >= d) pairs_to += o, blocks_to += q;
+  }
+  if (lane == 63) sums[0][wave] = pairs_to, sums[1][wave] = blocks_to;
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int u = 0; u < kPlanThreads / 64; ++u) {
+    if (u < wave) pairs_to += sums[0][u], blocks_to += sums[1][u];
+    all += sums[1][u];
+  }
+  count[tid] = pairs_to - n;   // where its next pair goes
+  for (int i = 0; i < blocks; ++i) {
+    int* const b = a.blocks + (blocks_to - blocks + i) * 3;
+    b[0] = tid;
+    b[1] = pairs_to - n + i * kBlock;
+    b[2] = min(kBlock, n - i * kBlock);
+  }
+  for (int i = all + tid; i < a.most_blocks; i += kPlanThreads) a.blocks[i * 3] = -1;
+  __syncthreads();
+  for (int p = tid; p < a.pairs; p += kPlanThreads) {
+    const int e = a.chosen[p];
+    if ((unsigned)e < (unsigned)a.experts) a.sorted[atomicAdd(&count[e], 1)] = p;
+  }
+}
+
+// Many rows to an expert: a matrix product of 64 pairs by 64 units of h (64 gates and the 64 beside them) or 128 channels of a pair's part of y.  The rows go through LDS, straight from memory and a
+// chunk ahead, for all four waves; a wave widens the codes of its two tiles once for all of them, and leaves out the sixteens of rows that are not there.
+// fp16 subtracts the zero points from the codes, exactly; bf16 has no such instruction, and takes them out with the sums of x.
+template <typename T, bool UP, int FL>
+__global__ __launch_bounds__(256, (std::is_same<T, _Float16>::value ? 3 : 2)) void experts_tiles_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group) {
+  typedef W4Type<T> C;
+  typedef typename C::vec vec;
+  typedef T four __attribute__((ext_vector_type(4)));
+  constexpr bool EXACT = std::is_same<T, _Float16>::value;
+  constexpr int ROWS = kBlock, RT = 4, W = 4, NT = 2, PG = 4 / FL, XP = ROWS * 16, PP = NT * PG * 3;   // 16-byte pieces of a chunk of rows; of a wave's scales and zero points
+  __shared__ __attribute__((aligned(16))) uintx4 xs_lds[2][XP];
+  __shared__ __attribute__((aligned(16))) uintx4 params_lds[W][2][PP];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
+  const int* const block = a.blocks + (int)blockIdx.y * 3;
+  const int e = block[0], have = block[2], tiles = (have + 15) / 16;
+  if (e < 0) return;
+  const int* const rows = a.sorted + block[1];
+  const int k = UP ? a.channels : a.inter, units = (UP ? a.inter : a.channels) / 16;
+  const unsigned char* const packed = static_cast<const unsigned char*>(UP ? a.gate_up : a.down);
+  const int tile0 = UP ? (int)blockIdx.x * W + wave : ((int)blockIdx.x * W + wave) * 2;
+  const long base = UP ? (long)e * 2 * units : (long)e * units;
+  // (a tile past the last: the last again, not stored)
+  const long tile[2] = {base + min(tile0, units - 1), base + (UP ? min(tile0, units - 1) + units : min(tile0 + 1, units - 1))};
+  typedef Chunk<T, NT, 1, FL> Held;
+  typename Held::Where where;
+  where.set(packed, l, a.zeros, tile, lane);
+  const Widen<T> widen;
+  const vec ones = __builtin_bit_cast(vec, (uintx4){C::kOne, C::kOne, C::kOne, C::kOne});
+  const floatx4 none = {0, 0, 0, 0};
+  const unsigned x_at = (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)&xs_lds[0][0];
+  auto x_of = [&](int p) { return UP ? static_cast<const T*>(a.x) + (long)fast_div((unsigned)p, a.fd_top_k) * a.x_stride : static_cast<const T*>(a.h) + (long)p * a.inter; };
+  // This wave copies rows 16 wave .. 16 wave + 15 of a chunk, four to an instruction; piece p of a row stands at p ^ row % 16: sixteen rows' reads of one piece fall on different
+  // banks.  (Rows that are not there repeat the last one.)
+  const T* src[4];
+  int at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = wave * 16 + 4 * i + g;
+    at[i] = (col ^ (row & 15)) * 8;
+    src[i] = x_of(rows[min(row, have - 1)]) + at[i];
+  }
+  auto copy = [&](int chunk) {
+    if (wave >= tiles) return;
+    const int buffer = chunk & 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (chunk * 128 + at[i] < k) lds_dma16_at(x_at + (unsigned)((buffer * XP + (wave * 16 + 4 * i) * 16) * 16), src[i] + chunk * 128);
+    if (chunk * 128 + 128 > k)   // pieces that lie behind k: zeros
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (chunk * 128 + at[i] >= k) xs_lds[buffer][(wave * 16 + 4 * i) * 16 + lane] = (uintx4){0, 0, 0, 0};
+  };
+  floatx4 sum[NT][RT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sum[t][r] = none;
+  Held c[2];
+  c[0].load_codes(where, l, per_group, 0, 0, lane);
+  copy(0);
+  c[1].load_codes(where, l, per_group, 0, min(1, l.chunks - 1), lane);
+  auto turn = [&](Held& now, int chunk) {
+    // Behind the rows of this chunk a wave has asked for one chunk's codes: two loads, and one of scales.
+    asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // (What was loaded for this chunk is taken before more is asked for: the compiler does not count the copies, and a wait for the codes would be one for copies just begun.)
+    uintx4* const mine = params_lds[wave][chunk & 1];
+    if (lane < PP) mine[lane] = now.params;
+    uintx4 codes[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      codes[t] = now.codes[t];
+      asm volatile("" : "+v"(codes[t]));
+    }
+    if (chunk + 1 < l.chunks) copy(chunk + 1);
+    now.load_codes(where, l, per_group, 0, min(chunk + 2, l.chunks - 1), lane);
+    const uintx4* const xl = xs_lds[chunk & 1];
+    const four* const scales = reinterpret_cast<const four*>(mine);
+    const unsigned* const zps = reinterpret_cast<const unsigned*>(mine + NT * PG * 2);
+#pragma unroll
+    for (int f = 0; f < PG; ++f) {
+      const int gr = PG == 1 ? 0 : min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
+      vec wv[NT][FL];
+      float sc[NT][4], zp[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const four s4 = scales[(t * PG + gr) * 4 + g];
+        const unsigned z4 = a.zeros ? zps[(t * PG + gr) * 4 + g] : 0x18181818u;
+        const unsigned zc = a.zeros ? reinterpret_cast<const unsigned char*>(zps + (t * PG + gr) * 4)[col] : 0x18u;   // of the unit whose codes this lane holds
+        const halfx2 minus = __builtin_bit_cast(halfx2, 0xc800c800u + zc * 0x00400040u);                              // (n = 16 .. 31 is the half 0x4800 + 64 n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[t][i] = (float)s4[i];
+          zp[t][i] = -(float)((z4 >> (8 * i)) & 255u);
+        }
+#pragma unroll
+        for (int s = 0; s < FL; ++s) {
+          wv[t][s] = widen(codes[t][f * FL + s]);
+          if constexpr (EXACT) {
+            uintx4 u = __builtin_bit_cast(uintx4, wv[t][s]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const unsigned uq = u[q];
+              u[q] = __builtin_bit_cast(unsigned, __builtin_bit_cast(halfx2, uq) + minus);
+            }
+            wv[t][s] = __builtin_bit_cast(vec, u);
+          }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (r >= tiles) break;
+        floatx4 acc[NT], xs = none;
+#pragma unroll
+        for (int s = 0; s < FL; ++s) {
+          const vec xb = __builtin_bit_cast(vec, xl[(r * 16 + col) * 16 + ((4 * (f * FL + s) + g) ^ col)]);
+          if constexpr (!EXACT) xs = C::mfma(ones, xb, xs);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[t] = C::mfma(wv[t][s], xb, s ? acc[t] : none);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[t][r][i] = fmaf(sc[t][i], EXACT ? acc[t][i] : fmaf(zp[t][i], xs[i], acc[t][i]), sum[t][r][i]);
+      }
+    }
+  };
+  for (int chunk = 0; chunk < l.chunks; chunk += 2) {
+    turn(c[0], chunk);
+    if (chunk + 1 < l.chunks) turn(c[1], chunk + 1);
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = r * 16 + col;
+    if (row >= have) continue;
+    const int p = rows[row];
+    if constexpr (UP) {
+      if (tile0 >= units) continue;
+      four h;
+      floatx4 v[2] = {sum[0][r], sum[1][r]};
+      if constexpr (!EXACT)
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          if (__builtin_expect(!is_finite(v[w]), 0))
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const float again = sum_by_weights<T>(packed, l, k, a.group_of(k), a.zeros, x_of(p), (2 * e + w) * a.inter + tile0 * 16 + 4 * g + q);
+#pragma unroll
+              for (int f = 0; f < 4; ++f) v[w][f] = q == f ? again : v[w][f];
+            }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) h[q] = (T)(a.weights[p] * activated(a.act, v[0][q]) * v[1][q]);
+      *reinterpret_cast<four*>(static_cast<T*>(a.h) + (long)p * a.inter + tile0 * 16 + 4 * g) = h;
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (tile0 + t >= units) continue;
+        floatx4 v = sum[t][r];
+        if constexpr (!EXACT)
+          if (__builtin_expect(!is_finite(v), 0))
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const float again = sum_by_weights<T>(packed, l, k, a.group_of(k), a.zeros, x_of(p), e * a.channels + (tile0 + t) * 16 + 4 * g + q);
+#pragma unroll
+              for (int f = 0; f < 4; ++f) v[f] = q == f ? again : v[f];
+            }
+        *reinterpret_cast<floatx4*>(a.parts + (long)p * a.channels + (tile0 + t) * 16 + 4 * g) = v;
+      }
+    }
+  }
+}
+
 // y of up to kJoined pairs at once: a workgroup makes 16 channels of all tokens.  Its waves take the chosen experts in turn (several share one's reduction where there are fewer experts than waves), leave
 // each pair's part in LDS, and add a token's up in the order of its choices.
 constexpr int kJoined = 64, kJoinWaves = 8;
@@ -339,6 +568,17 @@ hipError_t launch_rows(const ExpertsArgs& a, const W4Layout& l, int n, hipStream
   return hipGetLastError();
 }
 
+template <typename T, bool UP>
+hipError_t launch_tiles(const ExpertsArgs& a, const W4Layout& l, hipStream_t st) {
+  const int units = (UP ? a.inter : a.channels) / 16, tiles = UP ? 4 : 8, per_group = a.group_of(UP ? a.channels : a.inter) / 32;
+  const FastDiv fd = make_fastdiv((uint32_t)per_group);
+  const dim3 grid((unsigned)((units + tiles - 1) / tiles), (unsigned)a.most_blocks), block(256);
+  if (per_group % 4 == 0) hipLaunchKernelGGL((experts_tiles_kernel<T, UP, 4>), grid, block, 0, st, a, l, fd);
+  else if (per_group % 2 == 0) hipLaunchKernelGGL((experts_tiles_kernel<T, UP, 2>), grid, block, 0, st, a, l, fd);
+  else hipLaunchKernelGGL((experts_tiles_kernel<T, UP, 1>), grid, block, 0, st, a, l, fd);
+  return hipGetLastError();
+}
+
 template <typename T, int XL>
 hipError_t launch_join(const ExpertsArgs& a, const W4Layout& l, hipStream_t st) {
   const int per_group = a.group_of(a.inter) / 32;
@@ -356,17 +596,25 @@ hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
   const W4Layout down = w4_layout(a.experts * a.channels, a.inter, a.group_of(a.inter), a.zeros != 0);
   const long active = a.pairs < a.experts ? a.pairs : a.experts, up_waves = active * (a.inter / 16), down_waves = active * (a.channels / 32);
   const bool few = 4L * a.pairs <= a.experts, some = a.pairs <= 4L * a.experts;   // rows of an expert: one, seldom two; four on the mean
+  // Tiles where an expert has more than eight rows on the mean, and enough of them are there for the chip or the rows are many (us, rows / tiles, 2048 channels, 1408 beside them, 32 experts, fp16:
+  // 8 rows 59 / 60, 16 91 / 73, 32 159 / 106, 62 322 / 138; 4096, 1024, 8 experts, bf16 in groups of 64: 8 rows 34 / 48, 16 54 / 63, 32 96 / 100, 64 172 / 114).
+  const long mean = a.pairs / a.experts;
+  const bool tiled = mean > 32 || (mean > 8 && (long)a.experts * ((a.inter + 63) / 64) >= 512);
   hipError_t e;
-  if (few || some) {
+  if (tiled) {
+    hipLaunchKernelGGL(experts_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+    if ((e = hipGetLastError())) return e;
+  }
+  if (!tiled && (few || some)) {
     if (few) e = up_waves >= 2048 ? launch_rows<T, true, 1, 2>(a, up, 1, st) : launch_rows<T, true, 1, 4>(a, up, 1, st);
     else e = up_waves >= 4096 ? launch_rows<T, true, 2, 1>(a, up, 1, st) : up_waves >= 2048 ? launch_rows<T, true, 2, 2>(a, up, 1, st) : launch_rows<T, true, 2, 4>(a, up, 1, st);
   } else {
-    e = launch_rows<T, true, 4, 2>(a, up, 1, st);
+    e = tiled ? launch_tiles<T, true>(a, up, st) : launch_rows<T, true, 4, 2>(a, up, 1, st);
   }
   if (e != hipSuccess) return e;
   if (a.pairs <= kJoined) return few ? launch_join<T, 1>(a, down, st) : some ? launch_join<T, 2>(a, down, st) : launch_join<T, 4>(a, down, st);
-  if (some) e = down_waves >= 4096 ? launch_rows<T, false, 2, 1>(a, down, down_waves >= 8192 ? 2 : 1, st) : launch_rows<T, false, 2, 2>(a, down, 1, st);
-  else e = launch_rows<T, false, 4, 2>(a, down, 1, st);
+  if (!tiled && some) e = down_waves >= 4096 ? launch_rows<T, false, 2, 1>(a, down, down_waves >= 8192 ? 2 : 1, st) : launch_rows<T, false, 2, 2>(a, down, 1, st);
+  else e = tiled ? launch_tiles<T, false>(a, down, st) : launch_rows<T, false, 4, 2>(a, down, 1, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((experts_add_kernel<T>), dim3((unsigned)((a.channels + 1023) / 1024), (unsigned)a.tokens), dim3(256), 0, st, a);
   return hipGetLastError();
@@ -374,13 +622,14 @@ hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
 
 constexpr int kPairs = 4096;   // of a launch at most
 int tokens_at_once(const ExpertsArgs& a) { return a.top_k >= kPairs ? 1 : kPairs / a.top_k; }
+size_t blocks_of(int pairs, int experts) { return (size_t)(pairs < experts ? pairs : experts) + pairs / kBlock; }   // at most
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t experts_workspace_bytes(const ExpertsArgs& a) {
   const size_t pairs = (size_t)(a.tokens < tokens_at_once(a) ? a.tokens : tokens_at_once(a)) * a.top_k;
-  return up256(pairs * a.inter * 2) + up256(pairs * a.channels * 4);
+  return up256(pairs * a.inter * 2) + up256(pairs * a.channels * 4) + up256(pairs * 4) + up256(blocks_of((int)pairs, a.experts) * 12);
 }
 
 hipError_t launch_experts(const ExpertsArgs& args, int dtype, hipStream_t st) {
@@ -399,6 +648,9 @@ hipError_t launch_experts(const ExpertsArgs& args, int dtype, hipStream_t st) {
     a.weights = args.weights + (size_t)first * a.top_k;
     a.h = args.workspace;
     a.parts = reinterpret_cast<float*>(static_cast<char*>(args.workspace) + up256((size_t)a.pairs * a.inter * 2));
+    a.sorted = reinterpret_cast<int*>(reinterpret_cast<char*>(a.parts) + up256((size_t)a.pairs * a.channels * 4));
+    a.blocks = reinterpret_cast<int*>(reinterpret_cast<char*>(a.sorted) + up256((size_t)a.pairs * 4));
+    a.most_blocks = (int)blocks_of(a.pairs, a.experts);
     if (hipError_t e = dtype == T_F16 ? launch_type<_Float16>(a, st) : launch_type<__bf16>(a, st)) return e;
   }
   return hipSuccess;

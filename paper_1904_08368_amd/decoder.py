@@ -11,6 +11,12 @@ enqueues kernels on torch's current stream, so it can be captured into a HIP gra
     step.extend(ids, [len(p) for p in prompts])          # slots for the new tokens; what the kernels read goes to the device
     for i, layer in enumerate(layers):
         x = layer(x, i, step)
+
+A block around such a layer adds three more operators, four launches for a few tokens:
+  relay_residual_norm (the layer's output, the residual stream)  ->  relay_route  ->  relay_experts_w4  ->  relay_residual_norm,
+and a step ends with relay_sample on what the last projection leaves:
+    decoder = Decoder(blocks, first_norm, head, max_tokens)
+    tokens = sampler(decoder.logits(decoder(x, step)), uniform=u)
 """
 from __future__ import annotations
 
@@ -176,8 +182,8 @@ class AttentionLayer:
         # (rows of padding are read by the second projection and written by nothing: what the memory held before would be their input)
         self._attn = torch.zeros((max_tokens, q_heads * head_dim), dtype=qkv.dtype, device=device)
 
-    def __call__(self, x, index: int, step: Step, y=None):
-        """x [step.tokens, width] -> y; `index`: this layer's cache."""
+    def __call__(self, x, index: int, step: Step, y=None, add: bool = True):
+        """x [step.tokens, width] -> y; `index`: this layer's cache.  add: whether x is added to what the layer makes of it."""
         q_heads, kv_heads, dim = self.heads
         y = torch.empty_like(x) if y is None else y
         kc, vc = step.cache.k[index], step.cache.v[index]
@@ -188,4 +194,105 @@ class AttentionLayer:
         d = B.paged_attention_desc(q, kc, step.page_table, attn, step.max_q_len, step.max_kv_len, self.scale, True, self.window)
         ws = self.workspace.of(B.relay_paged_attention_workspace_bytes(d), x.device)
         B.relay_paged_attention(d, q, kc, vc, step.page_table, step.q_starts, step.kv_lens, attn, ws)
-        return self.out(attn.flatten(1), y, residual=x)
+        return self.out(attn.flatten(1), y, residual=x if add else None)
+
+
+class ResidualNorm:
+    """What stands between two blocks: s = residual_scale * residual + branch_scale * gate * post(x) and pre(s).  Weights and biases float32."""
+
+    def __init__(self, pre=B.NORM_RMS, post=B.NORM_NONE, pre_weight=None, pre_bias=None, post_weight=None, post_bias=None, pre_eps=1e-5, post_eps=1e-5,
+                 branch_scale=1.0, residual_scale=1.0, gate=None):
+        self.kinds, self.gate = dict(post=post, pre=pre, post_eps=post_eps, pre_eps=pre_eps, branch_scale=branch_scale, residual_scale=residual_scale), gate
+        self.params = (post_weight, post_bias, pre_weight, pre_bias)
+
+    def __call__(self, x, residual=None, sum=None, y=None):
+        """Writes s to `sum` and the normed sum to `y`, each if given; they may be x or residual."""
+        B.relay_residual_norm(B.residual_norm_desc(x, residual, self.gate, sum, y, **self.kinds), x, residual, self.gate, *self.params, sum, y)
+        return y if y is not None else sum
+
+
+class Experts:
+    """A mixture of experts with 4-bit weights behind its router.  router [experts, width] of the activations' type; up: Dense4 of 2 * inter units an expert
+    (its gates, then the units beside them), down: Dense4 back to the width; bias: added to the scores for the choice alone.  workspace: one serves all the experts of a
+    stack, and no other operator (what it holds behind a call is whatever was computed there)."""
+
+    def __init__(self, router, up: Dense4, down: Dense4, top_k: int, bias=None, score=B.SCORE_SOFTMAX, normalize=True, scale=1.0, act=B.ACT_SILU,
+                 workspace: Optional[Workspace] = None):
+        self.experts, self.inter = router.shape[0], down.k
+        if up.n != 2 * self.experts * down.k or down.n != self.experts * up.k or router.shape[1] != up.k or up.group != down.group or \
+                (up.zeros is None) != (down.zeros is None) or router.dtype != up.dtype or up.dtype != down.dtype or up.bias is not None or down.bias is not None:
+            raise ValueError("the router and the products do not go together")
+        self.router, self.up, self.down, self.top_k, self.bias = router, up, down, top_k, bias
+        self.score, self.normalize, self.scale, self.act = score, normalize, scale, act
+        # (the router's holds counters that have to stay as they are left: it is not shared)
+        self.workspace, self._cells = Workspace() if workspace is None else workspace, Workspace()
+
+    def route(self, x, chosen, weights):
+        d = B.route_desc(x, self.router, chosen, self.score, self.normalize, self.scale)
+        B.relay_route(d, x, self.router, self.bias, chosen, weights, self._cells.of(B.relay_route_workspace_bytes(d), x.device))
+
+    def __call__(self, x, y, residual=None, chosen=None, weights=None):
+        """x [tokens, width] -> y.  chosen, weights [tokens, top_k]: where the router leaves its choice, if that is wanted."""
+        if chosen is None:
+            chosen = torch.empty((x.shape[0], self.top_k), dtype=torch.int32, device=x.device)
+        if weights is None:
+            weights = torch.empty((x.shape[0], self.top_k), dtype=torch.float32, device=x.device)
+        self.route(x, chosen, weights)
+        d = B.experts_w4_desc(x, chosen, y, self.experts, self.inter, self.up.group, self.up.zeros is not None, self.act, residual)
+        d.packed_bytes = (self.up.packed.nbytes, self.down.packed.nbytes)   # (known here: not asked for again)
+        B.relay_experts_w4(d, x, chosen, weights, self.up.packed, self.down.packed, residual, y,
+                           self.workspace.of(B.relay_experts_w4_workspace_bytes(d), x.device))
+        return y
+
+
+class Block:
+    """An attention layer and a mixture of experts on a residual stream: s += attention(n), n = mid(s), s += experts(n), n = out(s), where mid and out also
+    hold what scales, gates and norms the two branches have.  `out` is what the next block starts from."""
+
+    def __init__(self, attention: AttentionLayer, mid: ResidualNorm, experts: Experts, out: ResidualNorm):
+        self.attention, self.mid, self.experts, self.out = attention, mid, experts, out
+
+    def __call__(self, s, n, branch, index: int, step: Step):
+        """s, n [step.tokens, width]: the stream and its norm, both replaced; branch: scratch of their shape."""
+        self.attention(n, index, step, branch, add=False)
+        self.mid(branch, s, s, n)
+        self.experts(n, branch)
+        self.out(branch, s, s, n)
+
+
+class Sampler:
+    """The next token of each row of logits; settings are float32 (top_k int32) tensors of a number a row, or None."""
+
+    def __init__(self):
+        self._scratch = Workspace()
+
+    def __call__(self, logits, temperature=None, top_k=None, top_p=None, min_p=None, uniform=None, tokens=None, probs=None):
+        if tokens is None:
+            tokens = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
+        d = B.sample_desc(logits)
+        B.relay_sample(d, logits, temperature, top_k, top_p, min_p, uniform, tokens, probs, self._scratch.of(B.relay_sample_workspace_bytes(d), logits.device))
+        return tokens
+
+
+class Decoder:
+    """Blocks on one residual stream, and the projection to logits."""
+
+    def __init__(self, blocks: Sequence[Block], first: ResidualNorm, head: Dense4, max_tokens: int):
+        qkv = blocks[0].attention.qkv
+        self.blocks, self.first, self.head = list(blocks), first, head
+        # (rows of padding are read by some kernels and mean nothing: they start from zeros)
+        self._s, self._n, self._branch = (torch.zeros((max_tokens, qkv.k), dtype=qkv.dtype, device=qkv.packed.device) for _ in range(3))
+        self._logits = torch.empty((max_tokens, head.n), dtype=qkv.dtype, device=qkv.packed.device)
+
+    def __call__(self, x, step: Step):
+        """x [step.tokens, width], the tokens' embeddings -> the normed stream behind the last block (this decoder's own buffer)."""
+        s, n, branch = (t[:step.tokens] for t in (self._s, self._n, self._branch))
+        self.first(x, None, s, n)
+        for i, block in enumerate(self.blocks):
+            block(s, n, branch, i, step)
+        return n
+
+    def logits(self, n, rows=None):
+        """Of all tokens, or of those that `rows` (an index tensor) names."""
+        n = n if rows is None else n.index_select(0, rows)
+        return self.head(n, self._logits[:n.shape[0]])
