@@ -596,10 +596,11 @@ hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
   const W4Layout down = w4_layout(a.experts * a.channels, a.inter, a.group_of(a.inter), a.zeros != 0);
   const long active = a.pairs < a.experts ? a.pairs : a.experts, up_waves = active * (a.inter / 16), down_waves = active * (a.channels / 32);
   const bool few = 4L * a.pairs <= a.experts, some = a.pairs <= 4L * a.experts;   // rows of an expert: one, seldom two; four on the mean
-  // Tiles where an expert has more than eight rows on the mean, and enough of them are there for the chip or the rows are many (us, rows / tiles, 2048 channels, 1408 beside them, 32 experts, fp16:
-  // 8 rows 59 / 60, 16 91 / 73, 32 159 / 106, 62 322 / 138; 4096, 1024, 8 experts, bf16 in groups of 64: 8 rows 34 / 48, 16 54 / 63, 32 96 / 100, 64 172 / 114).
+  // Tiles where an expert has six rows or more on the mean and enough tiles are there for the chip, or the rows are many.  us, rows of codes / tiles, 4, 8 and 16 rows: 2048 channels, 1408 beside
+  // them, 32 experts, fp16 56 59 90 / 49 53 62, bf16 55 60 91 / 58 63 76, groups of 32 78 82 121 / 58 69 81; 4096, 1024, 64 experts, fp16 111 129 186 / 117 122 133, bf16 110 131 187 / 122 130 155,
+  // 128 experts 215 262 381 / 217 241 275; 4096, 1024, 8 experts in groups of 64: 8 rows 34 / 48, 16 54 / 63, 32 96 / 100, 64 172 / 86.
   const long mean = a.pairs / a.experts;
-  const bool tiled = mean > 32 || (mean > 8 && (long)a.experts * ((a.inter + 63) / 64) >= 512);
+  const bool tiled = mean > 32 || (mean >= 6 && (long)a.experts * ((a.inter + 63) / 64) >= 512);
   hipError_t e;
   if (tiled) {
     hipLaunchKernelGGL(experts_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);

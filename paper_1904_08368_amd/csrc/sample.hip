@@ -16,7 +16,7 @@ namespace {
 
 constexpr int BINS = 2048, CAP = 2048;   // of a histogram; tokens that a list holds
 constexpr int NT = 512, WAVES = NT / 64; // threads of a workgroup (of 1024 each would have too few registers)
-constexpr int PARTS = 64;                // workgroups that share a row at most
+constexpr int PARTS = 32;                // workgroups that share a row at most
 typedef unsigned long long u64;
 
 template <typename T> struct Piece { typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
@@ -80,8 +80,10 @@ struct Settings {
     greedy = !a.uniform || temperature <= 0.f || top_k == 1 || top_p <= 0.f;
     z_min = cut_min ? log2((double)fminf(min_p, 1.f)) : 0.0;
   }
-  // what the second reading adds up: nothing, where the third finds all that min-p keeps by itself; otherwise bins' tokens, and their masses
+  // What the second reading adds up: nothing, where the third finds all that min-p keeps by itself, or all that top-k keeps from some `maxima` of parts of the row: as many of them as top-k asks for
+  // bound its tokens from below.  Otherwise bins' tokens, for top-k, and their masses.
   __device__ bool by_value() const { return !top_k && !cut_p && cut_min; }
+  __device__ bool by_maxima(int maxima) const { return top_k && 2 * top_k <= maxima; }   // (more of them and the bound lies low)
   __device__ bool masses() const { return !top_k || top_k > CAP / 2; }   // (of a few tokens the list tells)
 };
 
@@ -102,6 +104,7 @@ struct Row {
   float top;           // the maximum
   double per_unit;     // log2(e) / T
   float half_top, half_range, to_bin;   // distances are halved, so that none overflows
+  float own;           // the maximum of what this thread has read
   struct Bins { int first, last; };
   Bins of_k, of_p, of_min, of_u;        // what is gathered: the bins where top-k, top-p and min-p cut, and where the token is
 
@@ -223,7 +226,7 @@ struct Row {
   // ---- the maximum
   // The first token that has it where that is what is asked for; else the lowest number, which keeps the bins narrow.  -infinity among the logits hides it, unless the temperature is high and the bins
   // were wide without it.
-  __device__ __forceinline__ Top extremes(const Settings& s0) const {
+  __device__ __forceinline__ Top extremes(const Settings& s0) {
     Top t{-__builtin_inff(), __builtin_inff(), n};
     if (s0.greedy) {
       each<2>([&](float l, int i) { if (l > t.best) t.best = l, t.at = i; });
@@ -238,6 +241,7 @@ struct Row {
         t.low = fminf(t.low, l);
       });
     }
+    own = t.best;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const float best = __shfl_xor(t.best, d), low = __shfl_xor(t.low, d);
@@ -287,16 +291,16 @@ struct Row {
     for (int i = tid; i < BINS; i += NT) s.count[i] = 0, s.mass[i] = 0;
     __syncthreads();
   }
-  __device__ __forceinline__ void fill_bins(bool masses) const {
+  __device__ __forceinline__ void fill_bins(bool counts, bool masses) const {
     vec first[1];
     load(first, piece0 + tid);
-    fill_bins(masses, first);
+    fill_bins(counts, masses, first);
   }
   // (A piece's bins and weights side by side, and only then what is added to them: one behind the other they would wait for each other's table entries.)
-  __device__ __forceinline__ void fill_bins(bool masses, vec (&first)[1]) const {
+  __device__ __forceinline__ void fill_bins(bool counts, bool masses, vec (&first)[1]) const {
     auto add = [&](float d, int b, u64 w) {
       if (weighs(d)) {
-        atomicAdd(&s.count[b], 1u);
+        if (counts) atomicAdd(&s.count[b], 1u);
         if (masses) atomicAdd(&s.mass[b], w);
       }
     };
@@ -327,7 +331,6 @@ struct Row {
     auto in = [b](const Bins& r) { return (int)((unsigned)(b - r.first) <= (unsigned)(r.last - r.first)); };
     return (in(of_k) | in(of_p) | in(of_min) | in(of_u)) != 0;
   }
-  __device__ __forceinline__ unsigned tokens_of(int b) const { return s.count[b] - (b ? s.count[b - 1] : 0); }
   __device__ __forceinline__ float listed(int i) const { return value_of(~(unsigned)(s.list[i] >> 32)); }
   __device__ __forceinline__ int number(int i) const { return (int)(unsigned)s.list[i]; }
   static __device__ __forceinline__ u64 entry(float l, int i) { return (u64)~key_of(l) << 32 | (unsigned)i; }
@@ -377,17 +380,19 @@ struct Row {
     }
     return n;
   }
-  // s.run in order into s.list, then the masses of all tokens up to each.  Each token looks for its place: up to 128 among all; more, if the list is of whole bins, among those
-  // of its bin, which are brought together first (s.count holds the bins' running counts).  Where many are of one bin they are sorted by exchanges.
+  // s.run in order into s.list, then the masses of all tokens up to each.  Each token looks for its place: up to 128 among all; up to 512 among those of its bin, which are brought together
+  // first.  More are sorted by exchanges.
   // masses: s.mass holds the bins' running masses, and the list may have gaps; else it begins with the first of all tokens and has none.
-  __device__ __forceinline__ void sort(int m, bool bins, bool masses) const {
+  __device__ __forceinline__ void sort(int m, bool masses) const {
     auto bin_of = [&](u64 v) { return bin(distance(value_of(~(unsigned)(v >> 32)))); };
-    if (m <= 128 || (bins && m <= NT)) {
+    if (m <= NT) {
       const bool together = m > 128;
       u64* const from = together ? s.list : s.run;
       for (int i = tid; i < 8 * 64; i += NT) from[m + i] = ~0ull;   // (what is read behind the last, and is not less than any)
       if (together) {
-        for (int b = tid; b < BINS; b += NT) s.place[b] = wanted(b) ? tokens_of(b) : 0;
+        for (int b = tid; b < BINS; b += NT) s.place[b] = 0;
+        __syncthreads();
+        if (tid < m) atomicAdd(&s.place[bin_of(s.run[tid])], 1u);
         __syncthreads();
         unsigned all;
         running<BINS>(s.place, s.wave32, &all);
@@ -395,7 +400,7 @@ struct Row {
           const u64 v = s.run[tid];
           s.list[atomicSub(&s.place[bin_of(v)], 1u) - 1u] = v;
         }
-        // (a bin's place now is where it begins)
+        // (a bin's place now is where it begins, and that of the bin behind it where it ends)
       }
       int per = 1;   // threads to a token
       while (2 * per * m <= NT && per < 64) per *= 2;
@@ -408,7 +413,7 @@ struct Row {
         if (together) {
           const int b = bin_of(mine);
           lo = (int)s.place[b];
-          many = (int)tokens_of(b);
+          many = (b + 1 < BINS ? (int)s.place[b + 1] : m) - lo;
         }
       }
       const int len = ((many + per - 1) / per + 7) / 8 * 8;   // (what lies behind a bin's tokens is not less than they are)
@@ -455,7 +460,7 @@ struct Row {
 
   // ---- which bins hold the places that matter, s.count and s.mass being running sums.  `have_masses`: not, where top_k tokens are to be listed from the first on.
   __device__ __forceinline__ void plan(const Settings& t, bool have_masses, unsigned tokens, u64 total) {
-    const bool cut_k = t.top_k && (unsigned)t.top_k < tokens;
+    const bool cut_k = t.top_k && (unsigned)t.top_k <= tokens;
     const int bk = cut_k ? first_of<false>(s.count, BINS, (unsigned)t.top_k) : BINS - 1;
     const bool here = have_masses && cut_k;
     // the kept tokens' mass lies between these (the token where top-k cuts may weigh nothing)
@@ -490,6 +495,17 @@ struct Row {
     for (int i = 0; i < 4; ++i) flags |= wanted(tid * 4 + i) ? 1u << (8 * i) : 0u;
     reinterpret_cast<unsigned*>(s.gathered)[tid] = flags;
     __syncthreads();
+  }
+
+  // ---- the bins that hold the first top_k tokens, from the maxima of parts of the row (`have` of them, one to a thread, s.count being zero); false: not known
+  __device__ __forceinline__ bool plan_by_maxima(const Settings& t, float maximum, bool have) {
+    const float d = distance(maximum);
+    if (have && weighs(d)) atomicAdd(&s.count[bin(d)], 1u);
+    __syncthreads();
+    unsigned tokens;
+    running<BINS>(s.count, s.wave32, &tokens);
+    plan(t, false, tokens, 0);
+    return tokens >= (unsigned)t.top_k;
   }
 
   // ---- the token, from the sorted list of m tokens and the bins
@@ -537,7 +553,7 @@ struct Row {
         return weighs(d) && bin(d) == b && (shift == 32 || key_of(l) >> shift == prefix);
       });
       if (m <= CAP) {
-        sort(m, false, false);
+        sort(m, false);
         const int i = kind == RANK ? (int)goal - 1 : kind == REACH ? first_of<false>(s.run, m, goal) : first_of<true>(s.run, m, goal);
         return {base + s.run[i], number(i), listed(i)};
       }
@@ -626,11 +642,15 @@ struct Row {
     u64 total = 0, kept = 0;
     int token = 0;
     float logit = top;
-    bool by_value = t.by_value();
+    bool by_value = t.by_value(), by_maxima = !ready && t.by_maxima(NT);
     for (;;) {
-      if (!by_value && !ready) {
+      bool known = true;
+      if (by_maxima) {
         clear_bins();
-        fill_bins(masses);
+        known = plan_by_maxima(t, own, true);
+      } else if (!by_value && !ready) {
+        clear_bins();
+        fill_bins(t.top_k, masses);
         running<BINS>(s.count, s.wave32, &tokens);
         running<BINS>(s.mass, s.wave64, &total);
         plan(t, masses, tokens, total);
@@ -638,14 +658,15 @@ struct Row {
         tokens = s.count[BINS - 1];
         total = s.mass[BINS - 1];
       }
-      if (!ready) m = by_value ? gather([&](float l) { return of_value(l, t.z_min); }) : gather([&](float l) { return of_bins(l); });
-      bins = !by_value && masses;
+      if (!known) m = CAP + 1;
+      else if (!ready) m = by_value ? gather([&](float l) { return of_value(l, t.z_min); }) : gather([&](float l) { return of_bins(l); });
+      bins = !by_value && !by_maxima && masses;
       if (m <= CAP || bins) break;
-      by_value = ready = false;
-      masses = true;
+      masses = masses || !by_maxima;   // (without the maxima first by counts alone, if that may do)
+      by_value = by_maxima = ready = false;
     }
     if (m <= CAP) {
-      sort(m, !by_value, bins);
+      sort(m, bins);
       const int i = choose(t, bins, tokens, total, m, &kept);
       token = number(i);
       logit = listed(i);
@@ -689,6 +710,7 @@ struct Shared {
   u64 list[CAP];
   unsigned count[BINS];
   Top top[PARTS];
+  float maxima[PARTS * WAVES];   // of what a wave has read
   unsigned listed, arrived;
   unsigned pad[14];
 };
@@ -705,6 +727,10 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(const SampleArgs a) {
     h.top[g] = t;
     if (g == 0) h.listed = h.arrived = 0;
   }
+  float most = row.own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+  if ((threadIdx.x & 63) == 0) h.maxima[g * WAVES + (threadIdx.x >> 6)] = most;
   for (int i = BINS * g / parts + (int)threadIdx.x; i < BINS * (g + 1) / parts; i += NT) h.mass[i] = 0, h.count[i] = 0;
 }
 
@@ -731,10 +757,10 @@ __global__ __launch_bounds__(NT) void sample_bins_kernel(const SampleArgs a) {
   typename Row<T>::vec first[1];   // (on its way while the maximum is looked up)
   row.load(first, row.piece0 + row.tid);
   const Top top = top_of(h, (int)gridDim.x);
-  if (top.best == -__builtin_inff() || t.greedy || t.by_value()) return;
+  if (top.best == -__builtin_inff() || t.greedy || t.by_value() || t.by_maxima((int)gridDim.x * WAVES)) return;
   row.set(top, t.temperature);
   row.clear_bins();
-  row.fill_bins(t.masses(), first);
+  row.fill_bins(t.top_k, t.masses(), first);
   for (int i = (int)threadIdx.x; i < BINS; i += NT) {
     if (s.count[i]) atomicAdd(&h.count[i], s.count[i]);
     if (s.mass[i]) atomicAdd(&h.mass[i], s.mass[i]);
@@ -751,6 +777,9 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
   row.share((int)blockIdx.x, (int)gridDim.x);
   typename Row<T>::vec first[2];   // (on its way while the bins are looked through)
   row.load(first, row.piece0 + tid);
+  static_assert(PARTS * WAVES <= NT, "a maximum to a thread");
+  const int maxima = (int)gridDim.x * WAVES;
+  const float maximum = tid < maxima ? h.maxima[tid] : 0.f;
   unsigned count[BINS / NT];
   u64 mass[BINS / NT];
 #pragma unroll
@@ -761,8 +790,12 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
     return;
   }
   row.set(top, t.temperature);
-  const bool by_value = t.by_value();
-  if (!by_value) {
+  const bool by_value = t.by_value(), by_maxima = t.by_maxima(maxima);
+  bool known = true;
+  if (by_maxima) {
+    row.clear_bins();
+    known = row.plan_by_maxima(t, maximum, tid < maxima);
+  } else if (!by_value) {
 #pragma unroll
     for (int i = 0; i < BINS / NT; ++i) s.count[i * NT + tid] = count[i], s.mass[i * NT + tid] = mass[i];
     __syncthreads();
@@ -772,7 +805,7 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
     row.template running<BINS>(s.mass, s.wave64, &total);
     row.plan(t, t.masses(), tokens, total);
   }
-  const int m = by_value ? row.gather([&](float l) { return row.of_value(l, t.z_min); }, first) : row.gather([&](float l) { return row.of_bins(l); }, first);
+  const int m = !known ? CAP + 1 : by_value ? row.gather([&](float l) { return row.of_value(l, t.z_min); }, first) : row.gather([&](float l) { return row.of_bins(l); }, first);
   // this part's tokens to the row's list (in any order: it is sorted), and whoever is last ends the row
   if (tid == 0) s.found = (int)min(__hip_atomic_fetch_add(&h.listed, (unsigned)m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), 1u << 30);
   __syncthreads();
