@@ -50,7 +50,7 @@ enum { RELAY_SCORE_SOFTMAX = 0, RELAY_SCORE_SIGMOID = 1 };
 
 typedef struct {
   int32_t dtype;              /* of x and w: RELAY_F16 or RELAY_BF16 */
-  int32_t tokens, channels;   /* channels a multiple of 8 */
+  int32_t tokens, channels;   /* channels a multiple of 8, up to 2^24 */
   int32_t experts, top_k;     /* 1 .. 1024; 1 .. min(experts, 64) */
   int32_t score;              /* RELAY_SCORE_* */
   int32_t normalize;          /* 1: the weights of a token's experts add up to `scale` */
@@ -86,8 +86,8 @@ typedef struct {
 /* y[t] = sum_s weights[t][s] * down_e (act(gate_e x[t]) * up_e x[t])  [+ residual[t]],   e = chosen[t][s]
  * for few tokens, where the chosen experts' codes are most of what there is to read: each is read once for all the tokens that chose it.
  * weights * act * up is rounded to the tensors' type for the second product (an operand of the matrix cores); sums are fp32, in a fixed order.
- * Two launches, three for more than 64 choices: what is elementwise goes into the products' ends (paper Section 4.1), scales behind the
- * quantized operands (Section 4.2).
+ * Two launches for up to 64 choices, three or four for more (of up to 4096 at a time): what is elementwise goes into the products' ends (paper
+ * Section 4.1), scales behind the quantized operands (Section 4.2).
  * gate_up and down are packed by relay_prepack_qdense_w4 with the experts' units one behind the other:
  *   gate_up: n = experts * 2 * inter, k = channels, an expert's gates ahead of its other units;   down: n = experts * channels, k = inter
  * An entry of chosen outside 0 .. experts-1 adds nothing (a padding token has all of them -1 and gets its residual, or zeros); an
@@ -118,7 +118,7 @@ typedef struct {
  * largest, so that a result does not depend on the order of a sum; a weight below half of that is zero.
  *   logits [rows][vocab], any alignment of the type; temperature, top_p, min_p fp32, top_k int32, each [rows] or NULL (1, all, all, all); uniform
  *   fp32 [rows], or NULL: the first of each row
- *   tokens int32 [rows]; probs fp32 [rows] or NULL: w of the token over the sum of w over the kept
+ *   tokens int32 [rows]; probs fp32 [rows] or NULL: w of the token over the sum of w over the kept (1 where the first is what is asked for)
  * Workspace: NULL is valid (few rows then take longer).  Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (aliasing), _WORKSPACE, _DEVICE. */
 relay_status relay_sample_workspace_bytes(const relay_sample_desc* d, size_t* bytes);
 relay_status relay_sample(const relay_sample_desc* d, const void* logits, const float* temperature, const int32_t* top_k, const float* top_p,

@@ -72,8 +72,9 @@ relay_status relay_residual_norm(const relay_residual_norm_desc* d, const void* 
 static relay_status route_args(const relay_route_desc* d, relay::RouteArgs* out) {
   if (!d) return fail(RELAY_ERR_NULL, "descriptor is NULL");
   if (d->dtype != RELAY_F16 && d->dtype != RELAY_BF16) return fail(RELAY_ERR_DTYPE, "the router takes F16 or BF16");
-  if (d->tokens < 0 || d->channels <= 0 || d->experts <= 0 || d->experts > relay::kRouteExperts)
-    return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d channels=%d experts=%d, experts in 1 .. %d)", d->tokens, d->channels, d->experts, relay::kRouteExperts);
+  if (d->tokens < 0 || d->channels <= 0 || d->channels > relay::kRouteChannels || d->experts <= 0 || d->experts > relay::kRouteExperts)
+    return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d channels=%d experts=%d, channels in 1 .. %d, experts in 1 .. %d)", d->tokens, d->channels, d->experts, relay::kRouteChannels,
+                relay::kRouteExperts);
   if (d->top_k <= 0 || d->top_k > d->experts || d->top_k > relay::kRouteTopK)
     return fail(RELAY_ERR_SHAPE, "top_k=%d must be in 1 .. min(experts, %d)", d->top_k, relay::kRouteTopK);
   if (d->channels % 8) return fail(RELAY_ERR_ALIGN, "channels=%d must be a multiple of 8", d->channels);
@@ -119,7 +120,7 @@ static relay_status experts_args(const relay_experts_w4_desc* d, relay::ExpertsA
   if (d->tokens < 0 || d->top_k <= 0 || d->top_k > relay::kRouteTopK || d->channels <= 0 || d->inter <= 0 || d->experts <= 0 || d->experts > relay::kRouteExperts)
     return fail(RELAY_ERR_SHAPE, "bad extent (tokens=%d top_k=%d channels=%d inter=%d experts=%d)", d->tokens, d->top_k, d->channels, d->inter, d->experts);
   if (d->channels % 16 || d->inter % 16) return fail(RELAY_ERR_ALIGN, "channels=%d and inter=%d must be multiples of 16", d->channels, d->inter);
-  if (2L * d->experts * d->inter > 0x7ffffff0L || (long)d->experts * d->channels > 0x7ffffff0L || d->channels > 0x7fffff00 / 16)
+  if (2L * d->experts * d->inter > 0x40000000L || (long)d->experts * d->channels > 0x7ffffff0L || d->channels > 0x7fffff00 / 16)
     return fail(RELAY_ERR_SHAPE, "experts=%d channels=%d inter=%d too large", d->experts, d->channels, d->inter);
   if (d->group <= 0 || d->group % 32) return fail(RELAY_ERR_SHAPE, "group=%d must be a positive multiple of 32", d->group);
   if (d->has_zeros != 0 && d->has_zeros != 1) return fail(RELAY_ERR_UNSUPPORTED, "has_zeros=%d (0 or 1)", d->has_zeros);

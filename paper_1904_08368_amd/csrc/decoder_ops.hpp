@@ -44,7 +44,7 @@ struct RouteArgs {
   double* logits;       // [splits][tokens][experts]
   int splits;           // parts of the channels whose sums are left apart
 };
-constexpr int kRouteExperts = 1024, kRouteTopK = 64;
+constexpr int kRouteExperts = 1024, kRouteTopK = 64, kRouteChannels = 1 << 24;   // (channels: what 32-bit places in a row leave room for)
 size_t route_workspace_bytes(const RouteArgs& a);
 hipError_t launch_route(const RouteArgs& a, int dtype, hipStream_t st);
 

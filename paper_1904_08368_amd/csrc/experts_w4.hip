@@ -635,18 +635,18 @@ size_t experts_workspace_bytes(const ExpertsArgs& a) {
 
 hipError_t launch_experts(const ExpertsArgs& args, int dtype, hipStream_t st) {
   const int most = tokens_at_once(args);
-  for (int first = 0; first < args.tokens; first += most) {
+  for (long first = 0; first < args.tokens; first += most) {
     ExpertsArgs a = args;
-    a.tokens = args.tokens - first < most ? args.tokens - first : most;
+    a.tokens = (int)(args.tokens - first < most ? args.tokens - first : most);
     a.pairs = a.tokens * a.top_k;
     a.by_pair = a.pairs <= a.experts;
     a.fd_top_k = make_fastdiv((uint32_t)a.top_k);
-    const int64_t rows = (int64_t)first * 2;
+    const int64_t rows = first * 2;
     a.x = static_cast<const char*>(args.x) + rows * a.x_stride;
     a.y = static_cast<char*>(args.y) + rows * a.y_stride;
     if (a.res) a.res = static_cast<const char*>(args.res) + rows * a.y_stride;
-    a.chosen = args.chosen + (size_t)first * a.top_k;
-    a.weights = args.weights + (size_t)first * a.top_k;
+    a.chosen = args.chosen + first * a.top_k;
+    a.weights = args.weights + first * a.top_k;
     a.h = args.workspace;
     a.parts = reinterpret_cast<float*>(static_cast<char*>(args.workspace) + up256((size_t)a.pairs * a.inter * 2));
     a.sorted = reinterpret_cast<int*>(reinterpret_cast<char*>(a.parts) + up256((size_t)a.pairs * a.channels * 4));

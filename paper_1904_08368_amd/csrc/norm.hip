@@ -2,6 +2,8 @@
 //
 // Bytes: x and r are read once, s and y written once, and nothing else leaves the registers of the threads that share a row.  A mean is
 // formed before the squares of what lies off it (not as a difference of two sums, which loses a row whose mean is large), for which the row is at hand anyway.
+#include <type_traits>
+
 #include "decoder_ops.hpp"
 #include "wave_ops.hpp"
 
@@ -129,8 +131,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(co
 template <typename T, int TPR, int P>
 hipError_t launch(const NormArgs& a, hipStream_t st) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
-  hipLaunchKernelGGL((residual_norm_kernel<T, TPR, P>), dim3((unsigned)(((long)a.tokens + ROWS - 1) / ROWS)), dim3(TPR * ROWS), 0, st, a);
-  return hipGetLastError();
+  constexpr int kMost = 1 << 21;   // workgroups of a launch: one has fewer than 2^32 threads
+  for (long first = 0; first < a.tokens; first += (long)kMost * ROWS) {
+    NormArgs b = a;
+    b.tokens = (int)(a.tokens - first < (long)kMost * ROWS ? a.tokens - first : (long)kMost * ROWS);
+    auto on = [&](auto*& p, int64_t stride) {
+      if (p) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)(first * stride * (int64_t)sizeof(T)));
+    };
+    on(b.x, a.x_stride), on(b.res, a.res_stride), on(b.gate, a.gate_stride), on(b.sum, a.sum_stride), on(b.y, a.y_stride);
+    hipLaunchKernelGGL((residual_norm_kernel<T, TPR, P>), dim3((unsigned)((b.tokens + ROWS - 1) / ROWS)), dim3(TPR * ROWS), 0, st, b);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T>

@@ -265,12 +265,12 @@ size_t route_workspace_bytes(const RouteArgs& a) {
 }
 
 hipError_t launch_route(const RouteArgs& args, int dtype, hipStream_t st) {
-  for (int first = 0; first < args.tokens; first += kAtOnce) {
+  for (long first = 0; first < args.tokens; first += kAtOnce) {
     RouteArgs a = args;
-    a.tokens = args.tokens - first < kAtOnce ? args.tokens - first : kAtOnce;
-    a.x = static_cast<const char*>(args.x) + (size_t)first * args.x_stride * 2;
-    a.chosen = args.chosen + (size_t)first * args.top_k;
-    a.weights = args.weights + (size_t)first * args.top_k;
+    a.tokens = (int)(args.tokens - first < kAtOnce ? args.tokens - first : kAtOnce);
+    a.x = static_cast<const char*>(args.x) + first * args.x_stride * 2;
+    a.chosen = args.chosen + first * args.top_k;
+    a.weights = args.weights + first * args.top_k;
     a.counters = static_cast<unsigned*>(args.workspace);
     a.logits = reinterpret_cast<double*>(static_cast<char*>(args.workspace) + kRouteCounterBytes);
     a.splits = splits_of(a.tokens, a.experts, a.channels);

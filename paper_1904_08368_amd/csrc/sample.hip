@@ -829,7 +829,16 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
 template <typename T>
 hipError_t launch_type(const SampleArgs& a, int parts, hipStream_t st) {
   if (!a.workspace || parts == 1) {
-    hipLaunchKernelGGL((sample_kernel<T>), dim3((unsigned)a.rows), dim3(NT), 0, st, a);
+    constexpr int kMost = 1 << 22;   // rows of a launch: one has fewer than 2^32 threads
+    for (long first = 0; first < a.rows; first += kMost) {
+      SampleArgs b = a;
+      b.rows = (int)(a.rows - first < kMost ? a.rows - first : kMost);
+      b.logits = static_cast<const T*>(a.logits) + first * a.logits_stride;
+      auto on = [&](auto*& p) { if (p) p += first; };
+      on(b.temperature), on(b.top_k), on(b.top_p), on(b.min_p), on(b.uniform), on(b.tokens), on(b.probs);
+      hipLaunchKernelGGL((sample_kernel<T>), dim3((unsigned)b.rows), dim3(NT), 0, st, b);
+      if (hipError_t e = hipGetLastError()) return e;
+    }
   } else {
     const dim3 grid((unsigned)parts, (unsigned)a.rows), block(NT);
     hipLaunchKernelGGL((sample_top_kernel<T>), grid, block, 0, st, a);

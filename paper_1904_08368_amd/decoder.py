@@ -277,12 +277,13 @@ class Sampler:
 class Decoder:
     """Blocks on one residual stream, and the projection to logits."""
 
-    def __init__(self, blocks: Sequence[Block], first: ResidualNorm, head: Dense4, max_tokens: int):
+    def __init__(self, blocks: Sequence[Block], first: ResidualNorm, head: Dense4, max_tokens: int, max_rows: Optional[int] = None):
+        """max_rows: of logits at once, if they are never wanted of max_tokens."""
         qkv = blocks[0].attention.qkv
         self.blocks, self.first, self.head = list(blocks), first, head
         # (rows of padding are read by some kernels and mean nothing: they start from zeros)
         self._s, self._n, self._branch = (torch.zeros((max_tokens, qkv.k), dtype=qkv.dtype, device=qkv.packed.device) for _ in range(3))
-        self._logits = torch.empty((max_tokens, head.n), dtype=qkv.dtype, device=qkv.packed.device)
+        self._logits = torch.empty((max_tokens if max_rows is None else max_rows, head.n), dtype=qkv.dtype, device=qkv.packed.device)
 
     def __call__(self, x, step: Step):
         """x [step.tokens, width], the tokens' embeddings -> the normed stream behind the last block (this decoder's own buffer)."""
@@ -295,4 +296,6 @@ class Decoder:
     def logits(self, n, rows=None):
         """Of all tokens, or of those that `rows` (an index tensor) names."""
         n = n if rows is None else n.index_select(0, rows)
+        if n.shape[0] > self._logits.shape[0]:
+            raise ValueError(f"logits of {n.shape[0]} tokens, and room for {self._logits.shape[0]}")
         return self.head(n, self._logits[:n.shape[0]])

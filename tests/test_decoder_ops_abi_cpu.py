@@ -135,7 +135,7 @@ def _call_route(d, ws=at(9), ws_bytes=1 << 30, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=B.RELAY_F32), 3), (dict(tokens=-1), 2), (dict(channels=0), 2), (dict(channels=60), 5), (dict(experts=0), 2), (dict(experts=1025), 2),
-    (dict(top_k=0), 2), (dict(top_k=9), 2), (dict(experts=100, top_k=65), 2), (dict(score=2), 4), (dict(normalize=2), 4), (dict(scale=INF), 2), (dict(scale=NAN), 2),
+    (dict(channels=(1 << 24) + 8), 2), (dict(channels=0x7ffffff8), 2), (dict(top_k=0), 2), (dict(top_k=9), 2), (dict(experts=100, top_k=65), 2), (dict(score=2), 4), (dict(normalize=2), 4), (dict(scale=INF), 2), (dict(scale=NAN), 2),
     (dict(x_stride=-8), 2), (dict(x_stride=68), 5)])
 def test_route_refuses(kw, status):
     b = C.c_size_t()
@@ -182,7 +182,7 @@ def _call_experts(d, ws=at(9), ws_bytes=1 << 30, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=B.RELAY_F32), 3), (dict(tokens=-1), 2), (dict(top_k=0), 2), (dict(top_k=65), 2), (dict(channels=0), 2), (dict(channels=72), 5), (dict(inter=0), 2),
-    (dict(inter=40), 5), (dict(experts=0), 2), (dict(experts=1025), 2), (dict(experts=1000, inter=1 << 21), 2), (dict(experts=1000, channels=1 << 22, y_stride=1 << 22), 2),
+    (dict(inter=40), 5), (dict(experts=0), 2), (dict(experts=1025), 2), (dict(experts=1000, inter=1 << 21), 2), (dict(experts=1, inter=(1 << 29) + 16), 2), (dict(experts=1000, channels=1 << 22, y_stride=1 << 22), 2),
     (dict(group=0), 2), (dict(group=48), 2), (dict(has_zeros=2), 4), (dict(act=2), 4), (dict(flags=B.RELU), 4), (dict(flags=64), 4), (dict(x_stride=-8), 2),
     (dict(x_stride=68), 5), (dict(y_stride=63), 2)])
 def test_experts_refuse(kw, status):

@@ -192,3 +192,18 @@ def test_streams_and_replays(B):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(s["sum"], want[0]) and torch.equal(s["y"], want[1])
+
+
+def test_more_rows_than_a_launch_takes(B):
+    """2^26 rows of one element and five: y = x / sqrt(x^2 + 1), the sum in the place of x."""
+    rows = (1 << 26) + 5
+    x = ((torch.arange(rows, device=DEV, dtype=torch.int32) % 2001).float() / 500 - 2).half().view(rows, 1)
+    before, y = x.clone(), torch.zeros_like(x)
+    B.relay_residual_norm(B.residual_norm_desc(x, before, None, x, y, 0, 1, 1e-5, 1.0, 1.0, 1.0), x, before, None, None, None, None, None, x, y)
+    for part in range(0, rows, 1 << 24):
+        at = slice(part, min(part + (1 << 24), rows))
+        v = 2 * before[at].double()
+        assert torch.equal(x[at].double(), v)                        # (twice an fp16 number below 4 is one)
+        want = v / (v * v + 1).sqrt()
+        # fp32 with four roundings ahead of the one to fp16
+        assert bool(((y[at].double() - want).abs() <= want.abs() * (2.0 ** -11 + 2.0 ** -21) + 2.0 ** -25).all())

@@ -160,6 +160,53 @@ def test_masked_tokens(B, dtype):
             assert int(args[6][0]) == token
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_masked_tokens_of_long_rows(B, dtype):
+    """The same of rows that are shared out: most of them masked, fewer left than top-k asks for, one left, none."""
+    g = np.random.default_rng(17)
+    vocab = 70001
+    logits = _logits(dtype, 7, vocab, 18)
+    off = torch.from_numpy(g.random((7, vocab)) < 0.97).to(DEV)
+    off[1] = torch.from_numpy(g.random(vocab) < 1 - 30 / vocab).to(DEV)
+    for row, value in enumerate((float("-inf"), float("-inf"), torch.finfo(TYPES[dtype]).min, float("nan"))):
+        logits[row] = torch.where(off[row], torch.full_like(logits[row], value), logits[row])
+    logits[4, :] = float("-inf")
+    logits[4, vocab - 1] = -5.0                         # one token is left, the last
+    logits[5, :] = float("-inf")                        # none
+    logits[6, :] = float("nan")
+    for s in SETTINGS + [dict(top_k=128), dict(top_k=129), dict(top_k=100, temperature=8.0)]:
+        for with_workspace in (True, False):
+            _, args = _check(B, logits, uniform=0.6, with_workspace=with_workspace, **s)
+            assert args[6].tolist()[4:] == [vocab - 1, -1, -1]
+    logits[0, 100] = logits[0, 60000] = float("inf")    # they share the row
+    for u, token in ((0.2, 100), (0.8, 60000)):
+        for s in (dict(), dict(top_p=0.9), dict(min_p=0.5), dict(top_k=100)):
+            _, args = _check(B, logits[:1], uniform=u, **s)
+            assert int(args[6][0]) == token
+
+
+def test_long_rows_of_their_own_settings(B):
+    """Rows side by side that take every way through the launches, settings out of range among them."""
+    nan = float("nan")
+    logits = _logits("bf16", 12, 50257, 19)
+    for u in (0.2, 0.95):
+        _check(B, logits, [1.0, 0.0, nan, 0.7, 1.0, 9.0, 1.0, 1.0, 1.2, 1e-38, float("inf"), 1.0], [0, 50, 50, 128, 129, 2000, -3, 1, 0, 0, 60000, 256],
+               [1.0, 0.9, 0.9, nan, 0.8, 0.99, 0.9, 0.5, 1.0, 0.9, 1.0, 1.0], [0.0, 0.0, nan, 0.1, 0.0, 0.0, 0.01, 0.0, 0.05, 0.0, 0.0, 7.0], u)
+
+
+def test_more_rows_than_a_launch_takes(B):
+    """2^23 rows and three: each row's settings and outputs are its own."""
+    rows = (1 << 23) + 3
+    i = torch.arange(rows, device=DEV, dtype=torch.int32)
+    logits = torch.stack([(i % 3 == 0).half(), (i % 3 != 0).half()], 1)   # 0 and 1, the larger first in every third row
+    temperature = (i % 2).float()                                          # 0: the larger; 1: with u = 0.9 the smaller (weights 1 and 0.37)
+    tokens, probs = torch.full((rows,), -7, dtype=torch.int32, device=DEV), torch.zeros(rows, device=DEV)
+    B.relay_sample(B.sample_desc(logits), logits, temperature, None, None, None, torch.full((rows,), 0.9, device=DEV), tokens, probs)
+    larger = (i % 3 != 0).int()
+    assert torch.equal(tokens, torch.where(i % 2 == 0, larger, 1 - larger))
+    assert float((probs - torch.where(i % 2 == 0, 1.0, 1 / (1 + math.e))).abs().max()) <= 2.0 ** -23
+
+
 def test_zeros_of_both_signs_are_one_value(B):
     l = torch.zeros(1, 4000)
     l[0, ::2] *= -1.0
