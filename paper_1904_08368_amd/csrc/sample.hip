@@ -37,8 +37,8 @@ struct Lds {
   unsigned char gathered[BINS];
   union {
     struct {
-      u64 list[CAP];     // (descending value, ascending number) as one ascending number
-      u64 run[CAP];      // masses of all tokens up to a place of the list
+      alignas(16) u64 list[CAP];   // (descending value, ascending number) as one ascending number
+      alignas(16) u64 run[CAP];    // masses of all tokens up to a place of the list
     };
     struct {
       u64 mass2[BINS];   // as above, of the digits of a crowded bin's keys (while there is no list)
@@ -86,6 +86,14 @@ struct Settings {
   __device__ bool by_maxima(int maxima) const { return top_k && 2 * top_k <= maxima; }   // (more of them and the bound lies low)
   __device__ bool masses() const { return !top_k || top_k > CAP / 2; }   // (of a few tokens the list tells)
 };
+
+// the same in all lanes: kept once
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
+
+__device__ __forceinline__ double uniform(double v) {
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(double, (u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)b));
+}
 
 struct Top { float best, low; int at; };   // the maximum, the lowest number, the first token that has the maximum
 __device__ __forceinline__ void merge(Top& t, float best, float low, int at) {
@@ -262,6 +270,7 @@ struct Row {
     half_range = (float)fmin(reach, (double)fminf(0.5f * top - 0.5f * fmaxf(t.low, -FLT_MAX), FLT_MAX));
     to_bin = (float)BINS / half_range;
     if (!(to_bin < 1e30f)) to_bin = 0.f;
+    top = uniform(top), half_top = uniform(half_top), half_range = uniform(half_range), to_bin = uniform(to_bin), per_unit = uniform(per_unit);
     for (int i = tid; i < 256; i += NT) s.exp2s[i] = exp2(i / 256.0);
     __syncthreads();
   }
@@ -334,15 +343,50 @@ struct Row {
   __device__ __forceinline__ float listed(int i) const { return value_of(~(unsigned)(s.list[i] >> 32)); }
   __device__ __forceinline__ int number(int i) const { return (int)(unsigned)s.list[i]; }
   static __device__ __forceinline__ u64 entry(float l, int i) { return (u64)~key_of(l) << 32 | (unsigned)i; }
-  // The tokens that `is` names (by logit and distance) into s.run, as they come; how many, or more than CAP if they do not fit.
-  template <typename F>
-  __device__ __forceinline__ int gather(F is) const {
-    vec first[2];
-    load(first, piece0 + tid);
-    return gather(is, first);
+  // Two ranges of logits that hold all that is gathered and little else: of few tokens more is then asked.
+  struct Near {
+    float at0, reach0, at1, reach1;
+    __device__ __forceinline__ bool operator()(float l) const { return ((int)(fabsf(fmaf(-0.5f, l, at0)) <= reach0) | (int)(fabsf(fmaf(-0.5f, l, at1)) <= reach1)) != 0; }
+  };
+  // tokens at distances a .. b, which are found again with a rounding or two of their own
+  __device__ __forceinline__ void around(float a, float b, float* at, float* reach) const {
+    *at = half_top - 0.5f * (a + b);
+    *reach = 0.5f * (b - a) + 1e-6f * (fabsf(half_top) + b);
+    if (!(fabsf(*at) < FLT_MAX) || !(*reach < FLT_MAX) || top == FLT_MAX) *at = 0.f, *reach = __builtin_inff();   // (all of them)
+    *at = uniform(*at), *reach = uniform(*reach);
   }
-  template <typename F>
-  __device__ __forceinline__ int gather(F is, vec (&first)[2]) const {
+  __device__ __forceinline__ Near near_bins() const {
+    auto none = [](const Bins& r) { return r.first >= BINS; };
+    int first = BINS, last = -1;
+    if (!none(of_k)) first = min(first, of_k.first), last = max(last, of_k.last);
+    if (!none(of_p)) first = min(first, of_p.first), last = max(last, of_p.last);
+    if (!none(of_min)) first = min(first, of_min.first), last = max(last, of_min.last);
+    const float width = half_range / (float)BINS;
+    Near n;
+    around((float)of_u.first * width, (float)(of_u.last + 1) * width, &n.at0, &n.reach0);
+    n.at1 = n.at0, n.reach1 = n.reach0;
+    if (last >= 0) {
+      around((float)first * width, (float)(last + 1) * width, &n.at1, &n.reach1);
+      if (none(of_u)) n.at0 = n.at1, n.reach0 = n.reach1;
+    }
+    return n;
+  }
+  __device__ __forceinline__ Near near_value(double z_min) const {
+    Near n;
+    around(0.f, (float)fmin(-0.5 * z_min / per_unit, 2.0 * (double)half_range), &n.at0, &n.reach0);
+    n.at1 = n.at0, n.reach1 = n.reach0;
+    return n;
+  }
+  __device__ __forceinline__ int gather_bins(vec (&first)[2]) const {
+    return gather(near_bins(), [&](float l) { return of_bins(l); }, first);
+  }
+  __device__ __forceinline__ int gather_value(double z_min, vec (&first)[2]) const {
+    return gather(near_value(z_min), [&](float l) { return of_value(l, z_min); }, first);
+  }
+  // The tokens that `is` names, of those that `near` does, into s.run, as they come; how many, or more than CAP if they do not fit.
+  template <typename N, typename F>
+  __device__ __forceinline__ int gather(N near, F is, vec (&first)[2]) const {
+    constexpr bool NEAR = V > 4;   // (of four tokens to a piece, a wave waits more often for one that is near than it saves: 256 rows of 50257 in fp32 50 / 58 us; bf16, 64 x 128000 36 / 32)
     if (tid == 0) s.listed = 0;
     __syncthreads();
     auto take = [&](float l, int i) {
@@ -352,11 +396,13 @@ struct Row {
     pieces([&](const vec& v, int i) {
       unsigned hits = 0;
 #pragma unroll
-      for (int e = 0; e < V; ++e) hits |= (unsigned)is((float)v[e]) << e;
-      if (hits) {
+      for (int e = 0; e < V; ++e) hits |= (unsigned)(NEAR ? near((float)v[e]) : is((float)v[e])) << e;
+      for (; hits; hits &= hits - 1) {   // (one place of code for all of a piece's: eight took too many registers)
+        const int e = __builtin_ctz(hits);
+        float l = (float)v[0];
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (hits >> e & 1) take((float)v[e], i + e);
+        for (int j = 1; j < V; ++j) l = e == j ? (float)v[j] : l;
+        if (!NEAR || is(l)) take(l, i + e);
       }
     }, [&](float l, int i) { if (is(l)) take(l, i); }, first);
     __syncthreads();
@@ -368,15 +414,16 @@ struct Row {
     return (int)s.gathered[bin(d)] & (int)weighs(d);
   }
   __device__ __forceinline__ bool of_value(float l, double z_min) const { return (int)(exponent(l) >= z_min) & (int)weighs(distance(l)); }
-  // how many of `len` numbers (a multiple of 8) from `from` on are less than `mine`
+  // how many of `len` numbers (a multiple of 8) from `from` on, 16-byte aligned, are less than `mine`
   static __device__ __forceinline__ int less(const u64* from, int len, u64 mine) {
+    typedef u64 pair __attribute__((ext_vector_type(2)));
     int n = 0;
     for (int j = 0; j < len; j += 8) {
-      u64 v[8];
+      pair v[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = from[j + i];
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const pair*>(from + j + 2 * i);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) n += v[i] < mine;
+      for (int i = 0; i < 4; ++i) n += (v[i][0] < mine) + (v[i][1] < mine);
     }
     return n;
   }
@@ -414,6 +461,7 @@ struct Row {
           const int b = bin_of(mine);
           lo = (int)s.place[b];
           many = (b + 1 < BINS ? (int)s.place[b + 1] : m) - lo;
+          lo = lo & ~1, many += (int)s.place[b] & 1;   // (from an even place on: the one ahead of the bin's is less)
         }
       }
       const int len = ((many + per - 1) / per + 7) / 8 * 8;   // (what lies behind a bin's tokens is not less than they are)
@@ -548,10 +596,12 @@ struct Row {
     int shift = 32;
     u64 base = 0;
     for (;;) {
+      vec first[2];
+      load(first, piece0 + tid);
       const int m = gather([&](float l) {
         const float d = distance(l);
         return weighs(d) && bin(d) == b && (shift == 32 || key_of(l) >> shift == prefix);
-      });
+      }, [](float) { return true; }, first);
       if (m <= CAP) {
         sort(m, false);
         const int i = kind == RANK ? (int)goal - 1 : kind == REACH ? first_of<false>(s.run, m, goal) : first_of<true>(s.run, m, goal);
@@ -659,7 +709,11 @@ struct Row {
         total = s.mass[BINS - 1];
       }
       if (!known) m = CAP + 1;
-      else if (!ready) m = by_value ? gather([&](float l) { return of_value(l, t.z_min); }) : gather([&](float l) { return of_bins(l); });
+      else if (!ready) {
+        vec first[2];
+        load(first, piece0 + tid);
+        m = by_value ? gather_value(t.z_min, first) : gather_bins(first);
+      }
       bins = !by_value && !by_maxima && masses;
       if (m <= CAP || bins) break;
       masses = masses || !by_maxima;   // (without the maxima first by counts alone, if that may do)
@@ -805,7 +859,7 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(const SampleArgs a) {
     row.template running<BINS>(s.mass, s.wave64, &total);
     row.plan(t, t.masses(), tokens, total);
   }
-  const int m = !known ? CAP + 1 : by_value ? row.gather([&](float l) { return row.of_value(l, t.z_min); }, first) : row.gather([&](float l) { return row.of_bins(l); }, first);
+  const int m = !known ? CAP + 1 : by_value ? row.gather_value(t.z_min, first) : row.gather_bins(first);
   // this part's tokens to the row's list (in any order: it is sorted), and whoever is last ends the row
   if (tid == 0) s.found = (int)min(__hip_atomic_fetch_add(&h.listed, (unsigned)m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), 1u << 30);
   __syncthreads();
