@@ -472,7 +472,7 @@ __global__ __launch_bounds__(256, (std::is_same<T, _Float16>::value ? 3 : 2)) vo
 
 // y of up to kJoined pairs at once: a workgroup makes 16 channels of all tokens.  Its waves take the chosen experts in turn (several share one's reduction where there are fewer experts than waves), leave
 // each pair's part in LDS, and add a token's up in the order of its choices.
-constexpr int kJoined = 64, kJoinWaves = 8;
+constexpr int kJoined = 16, kJoinWaves = 8;
 template <typename T, int XL, int FL>
 __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group) {
   typedef Chunk<T, 1, XL, FL> Held;
@@ -613,7 +613,9 @@ hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
     e = tiled ? launch_tiles<T, true>(a, up, st) : launch_rows<T, true, 4, 2>(a, up, 1, st);
   }
   if (e != hipSuccess) return e;
-  if (a.pairs <= kJoined) return few ? launch_join<T, 1>(a, down, st) : some ? launch_join<T, 2>(a, down, st) : launch_join<T, 4>(a, down, st);
+  // The join where its waves take one expert each, or two and there are workgroups enough to hide the second.  us of both launches, join / rows and their sum: 2048 channels, 4 pairs 13.8 / 17.2, 8 19.1 / 19.5,
+  // 16 30.5 / 26.7, 32 44.8 / 35.6; 1024 channels, 8 pairs 20.9 / 21.0, 16 31.2 / 23.4; 4096 channels, 8 pairs 19.7 / 22.0, 16 28.2 / 30.2, 32 52.8 / 50.7; 7168 channels, 16 pairs 68 / 67, 48 137 / 132.
+  if (a.pairs <= (a.channels >= 4096 ? kJoined : kJoinWaves)) return few ? launch_join<T, 1>(a, down, st) : some ? launch_join<T, 2>(a, down, st) : launch_join<T, 4>(a, down, st);
   if (!tiled && some) e = down_waves >= 4096 ? launch_rows<T, false, 2, 1>(a, down, down_waves >= 8192 ? 2 : 1, st) : launch_rows<T, false, 2, 2>(a, down, 1, st);
   else e = tiled ? launch_tiles<T, false>(a, down, st) : launch_rows<T, false, 4, 2>(a, down, 1, st);
   if (e != hipSuccess) return e;

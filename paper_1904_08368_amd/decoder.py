@@ -12,7 +12,7 @@ enqueues kernels on torch's current stream, so it can be captured into a HIP gra
     for i, layer in enumerate(layers):
         x = layer(x, i, step)
 
-A block around such a layer adds three more operators, four launches for a few tokens:
+A block around such a layer adds three more operators, five launches for one token:
   relay_residual_norm (the layer's output, the residual stream)  ->  relay_route  ->  relay_experts_w4  ->  relay_residual_norm,
 and a step ends with relay_sample on what the last projection leaves:
     decoder = Decoder(blocks, first_norm, head, max_tokens)

@@ -102,6 +102,15 @@ def test_widths_and_groups(B, scratch, channels, inter, group):
     _check(B, scratch, layer, layer.inputs(6, 2), "gelu")
 
 
+@pytest.mark.parametrize("experts", [1, 2, 40])
+@pytest.mark.parametrize("channels", [2048, 4096])
+def test_few_pairs_of_wide_layers(B, scratch, channels, experts):
+    """Up to 8 or 16 of them the second launch adds them up itself."""
+    layer = Layer(B, "bf16", channels, 64, experts, 64, zeros=True)
+    for tokens, top_k in ((8, 1), (9, 1), (1, 9), (4, 4), (16, 1), (17, 1), (2, 9)):
+        _check(B, scratch, layer, layer.inputs(tokens, top_k))
+
+
 @pytest.mark.parametrize("experts,top_k,tokens", [(1, 1, 1), (1, 1, 50), (2, 2, 100), (4, 4, 513), (128, 8, 1), (128, 8, 16), (200, 1, 64), (1024, 64, 2), (300, 10, 30)])
 def test_mixtures(B, scratch, experts, top_k, tokens):
     layer = Layer(B, "f16", 96, 64, experts, 32)
