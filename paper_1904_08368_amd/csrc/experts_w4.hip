@@ -3,7 +3,9 @@
 // A pair is a token and one of the experts it has chosen; pairs of one expert share its codes, which are most of what there is to read.  The first
 // launch makes h of every pair; the second y, of few pairs directly (a workgroup adds up what the experts make of 16 channels), of more through a pair's parts in memory, which a third adds
 // up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
-// reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 117 and 70 (4.6 and 3.9 TB/s).
+// reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 115 and 67 (4.8 and 4.2 TB/s).  Many rows to an expert: tiles, below.
+// One token on 8 experts, 4096 channels and 1024 beside them, fp16: 19 us, 12 and 8, two chains of loads (the 50 MB take 10).  500 tokens on 32 experts, 2048 and 1408: 96 us, plan 5, tiles 58 and 35, sum 5:
+// half of a tile's 64 rows are there, so that the widening of the codes and its products, which a SIMD issues one or the other, take 3400 of 3750 clocks a chunk.
 // Codes become operands as in the dense kernels (16 + code, the sums of x taking the zero points out).
 #include <type_traits>
 
@@ -542,18 +544,28 @@ template <typename T>
 __global__ __launch_bounds__(256) void experts_add_kernel(const ExpertsArgs a) {
   const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, t = (int)blockIdx.y;
   if (c >= a.channels) return;
+  typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  const long at = (long)t * a.y_stride + c;
+  four res = {};
+  if (a.res) res = *reinterpret_cast<const four*>(static_cast<const T*>(a.res) + at);   // (on its way with the parts)
   floatx4 v = {0, 0, 0, 0};
   for (int s0 = 0; s0 < a.top_k; s0 += 8) {
     floatx4 part[8];
+    int named[8];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) part[s] = *reinterpret_cast<const floatx4*>(a.parts + (long)(t * a.top_k + min(s0 + s, a.top_k - 1)) * a.channels + c);
+    for (int s = 0; s < 8; ++s) {
+      const int p = t * a.top_k + min(s0 + s, a.top_k - 1);
+      named[s] = a.chosen[p];
+      part[s] = *reinterpret_cast<const floatx4*>(a.parts + (long)p * a.channels + c);
+    }
 #pragma unroll
     for (int s = 0; s < 8; ++s)   // (a pair that names no expert has no part: what stands in its place is not used)
-      if (s0 + s < a.top_k && (unsigned)a.chosen[t * a.top_k + s0 + s] < (unsigned)a.experts) v += part[s];
+      if (s0 + s < a.top_k && (unsigned)named[s] < (unsigned)a.experts) v += part[s];
   }
-  const long at = (long)t * a.y_stride + c;
+  four out;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) static_cast<T*>(a.y)[at + j] = (T)(a.res ? v[j] + (float)static_cast<const T*>(a.res)[at + j] : v[j]);
+  for (int j = 0; j < 4; ++j) out[j] = (T)(a.res ? v[j] + (float)res[j] : v[j]);
+  *reinterpret_cast<four*>(static_cast<T*>(a.y) + at) = out;
 }
 
 template <typename T, bool UP, int XL, int KS>

@@ -2,6 +2,8 @@
 //
 // Bytes: x and r are read once, s and y written once, and nothing else leaves the registers of the threads that share a row.  A mean is
 // formed before the squares of what lies off it (not as a difference of two sums, which loses a row whose mean is large), for which the row is at hand anyway.
+// 8192 rows of 8192 bf16: 97 us, 5.5 TB/s, as fast as a large copy.  1003 rows of 5003 fp16, three reductions, a gate and four parameters: 16.3 us, one round of workgroups, each of which waits for its
+// loads, its reductions and its parameters in turn (the bytes take 8; with 512 threads to a row 18.0, with 16-byte aligned pieces and two ends 17.1, with the parameters asked for ahead 18).
 #include <type_traits>
 
 #include "decoder_ops.hpp"
@@ -149,6 +151,7 @@ template <typename T>
 hipError_t launch_type(const NormArgs& a, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
   const int pieces = (a.channels + V - 1) / V;
+  // (A wave to a row needs no barrier.  Few rows: twice the threads, half the chain; many: workgroups of 256, of which more fit a CU.  The 1003 rows above 16.3 us with 256 and four pieces, 18.0 with 512 and two.)
   if (pieces <= 64) return launch<T, 64, 1>(a, st);
   if (pieces <= 128) return launch<T, 64, 2>(a, st);
   if (pieces <= 256) return launch<T, 256, 1>(a, st);

@@ -7,6 +7,9 @@
 // Masses are integers, multiples of 2^-S of the largest weight: sums of them have no order, and the borders between tokens are where 64 bits put them.
 // So a row is read three times: maximum; counts or masses; gathering.  One workgroup reads it where there are many rows, from the caches after the first time.  Of few rows each is shared out over
 // workgroups, a launch to each reading.
+// One row of 128000 fp16, top-k 50 and top-p: 18 us, launches of 5, 3 and 11 that wait for memory and for each other.  48 rows of 151643 bf16, top-p: 52 us, of 7, 15 and 30: weights in 64 bits and
+// additions to LDS in the second (50 % and 29 % of the clocks), in the third a last workgroup that sorts some 300 tokens of one value.  256 rows of 50257 fp32, each with its own settings: 50 us,
+// additions to LDS (some 30 clocks for a wave's, whose lanes meet on banks) and weights by eight waves a CU.
 #include <float.h>
 
 #include "decoder_ops.hpp"
