@@ -2,8 +2,8 @@
 //
 // Bytes: x and r are read once, s and y written once, and nothing else leaves the registers of the threads that share a row.  A mean is
 // formed before the squares of what lies off it (not as a difference of two sums, which loses a row whose mean is large), for which the row is at hand anyway.
-// 8192 rows of 8192 bf16: 97 us, 5.5 TB/s, as fast as a large copy.  1003 rows of 5003 fp16, three reductions, a gate and four parameters: 16.3 us, one round of workgroups, each of which waits for its
-// loads, its reductions and its parameters in turn (the bytes take 8; with 512 threads to a row 18.0, with 16-byte aligned pieces and two ends 17.1, with the parameters asked for ahead 18).
+// 8192 rows of 8192 bf16: 97 us, 5.5 TB/s, as fast as a large copy.  1003 rows of 5003 fp16, three reductions, a gate and four parameters: 15 us, one round of workgroups, each of which waits for its
+// loads, its reductions and its parameters in turn (the bytes take 8; with pieces that are 16-byte aligned and two ends 5 % more, with the parameters asked for ahead 10 %).
 #include <type_traits>
 
 #include "decoder_ops.hpp"
@@ -17,12 +17,14 @@ typedef float floatx4u __attribute__((ext_vector_type(4), aligned(4)));
 
 // TPR threads share a row, P pieces of 16 bytes each: piece i of a thread begins at channel (i TPR + thread) V.  Pieces are loaded at the alignment of the
 // element type, so rows of odd lengths take the same path; the one that ends a row short is taken element by element.
-template <typename T, int TPR, int P>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(const NormArgs a) {
-  constexpr int V = 16 / sizeof(T), ROWS = TPR < 256 ? 256 / TPR : 1, W = TPR / 64;
+// MOST 64: TPR is 64, four rows to a workgroup; more: a row to a workgroup of up to as many.
+template <typename T, int MOST, int P>
+__global__ __launch_bounds__((MOST < 256 ? 256 : MOST)) void residual_norm_kernel(const NormArgs a) {
+  constexpr int V = 16 / sizeof(T), ROWS = MOST < 256 ? 256 / MOST : 1, W = MOST / 64;
   typedef typename Piece<T>::vec vec;
-  __shared__ float part[2][W > 1 ? W : 1];
-  const int at = (int)threadIdx.x % TPR, row = (int)blockIdx.x * ROWS + (int)threadIdx.x / TPR, c = a.channels;
+  __shared__ float part[2][W];
+  const int TPR = W == 1 ? 64 : (int)blockDim.x, waves = TPR / 64, at = W == 1 ? (int)threadIdx.x % 64 : (int)threadIdx.x;
+  const int row = (int)blockIdx.x * ROWS + (W == 1 ? (int)threadIdx.x / 64 : 0), c = a.channels;
   if (ROWS > 1 && row >= a.tokens) return;   // (whole waves: nothing below waits for them)
   auto load = [&](const void* p, int64_t stride, vec (&v)[P]) {
     const T* const src = static_cast<const T*>(p) + row * stride;
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(co
       __syncthreads();
       v = 0.f;
 #pragma unroll
-      for (int u = 0; u < W; ++u) v += part[turn][u];
+      for (int u = 0; u < W; ++u) v += u < waves ? part[turn][u] : 0.f;
       turn ^= 1;   // (the other half: whoever is late still reads this one)
     }
     return v;
@@ -130,10 +132,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(co
   }
 }
 
-template <typename T, int TPR, int P>
-hipError_t launch(const NormArgs& a, hipStream_t st) {
-  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+template <typename T, int MOST, int P>
+hipError_t launch(const NormArgs& a, int pieces, hipStream_t st) {
+  constexpr int ROWS = MOST < 256 ? 256 / MOST : 1;
   constexpr int kMost = 1 << 21;   // workgroups of a launch: one has fewer than 2^32 threads
+  const int threads = MOST < 256 ? 256 : (pieces + 64 * P - 1) / (64 * P) * 64;   // (no wave without a piece)
   for (long first = 0; first < a.tokens; first += (long)kMost * ROWS) {
     NormArgs b = a;
     b.tokens = (int)(a.tokens - first < (long)kMost * ROWS ? a.tokens - first : (long)kMost * ROWS);
@@ -141,7 +144,7 @@ hipError_t launch(const NormArgs& a, hipStream_t st) {
       if (p) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)(first * stride * (int64_t)sizeof(T)));
     };
     on(b.x, a.x_stride), on(b.res, a.res_stride), on(b.gate, a.gate_stride), on(b.sum, a.sum_stride), on(b.y, a.y_stride);
-    hipLaunchKernelGGL((residual_norm_kernel<T, TPR, P>), dim3((unsigned)((b.tokens + ROWS - 1) / ROWS)), dim3(TPR * ROWS), 0, st, b);
+    hipLaunchKernelGGL((residual_norm_kernel<T, MOST, P>), dim3((unsigned)((b.tokens + ROWS - 1) / ROWS)), dim3(threads), 0, st, b);
     if (hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
@@ -151,14 +154,16 @@ template <typename T>
 hipError_t launch_type(const NormArgs& a, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
   const int pieces = (a.channels + V - 1) / V;
-  // (A wave to a row needs no barrier.  Few rows: twice the threads, half the chain; many: workgroups of 256, of which more fit a CU.  The 1003 rows above 16.3 us with 256 and four pieces, 18.0 with 512 and two.)
-  if (pieces <= 64) return launch<T, 64, 1>(a, st);
-  if (pieces <= 128) return launch<T, 64, 2>(a, st);
-  if (pieces <= 256) return launch<T, 256, 1>(a, st);
-  if (pieces <= 512) return a.tokens < 512 ? launch<T, 512, 1>(a, st) : launch<T, 256, 2>(a, st);
-  if (pieces <= 1024) return a.tokens < 512 ? launch<T, 512, 2>(a, st) : launch<T, 256, 4>(a, st);
-  if (pieces <= 2048) return launch<T, 512, 4>(a, st);
-  return launch<T, 1024, 4>(a, st);
+  // A wave to a row needs no barrier.  More pieces: as few to a thread as leave a CU four workgroups, and no more waves than have some.  us, fp16, 1000 rows (4000 with two norms, gate and biases):
+  // 2560 channels on 256 threads / the 192 that have pieces 6.9 (23.2) / 6.4 (21.9); 7168 four pieces to a thread / two 12.8 (66.9) / 11.3 (69.1), 8192 13.0 (70.5) / 12.1 (78.6); 12000 four / three
+  // 23.2 (125) / 20.8 (114).
+  if (pieces <= 64) return launch<T, 64, 1>(a, pieces, st);
+  if (pieces <= 128) return launch<T, 64, 2>(a, pieces, st);
+  if (pieces <= 256 || (pieces <= 512 && a.tokens < 512)) return launch<T, 512, 1>(a, pieces, st);
+  if (pieces <= 896 || (pieces <= 1024 && a.tokens < 512)) return launch<T, 512, 2>(a, pieces, st);
+  if (pieces > 1024 && pieces <= 1536) return launch<T, 512, 3>(a, pieces, st);
+  if (pieces <= 2048) return launch<T, 512, 4>(a, pieces, st);
+  return launch<T, 1024, 4>(a, pieces, st);
 }
 
 }  // namespace

@@ -93,6 +93,13 @@ def test_many_tokens(B, channels, tokens):
     _check(B, "bf16", _inputs("bf16", tokens, channels, gate="row"), "rms", "rms")
 
 
+@pytest.mark.parametrize("channels", [1032, 1536, 1544, 2560, 5121, 6600, 7168, 7169, 8193, 9216, 12288, 12289, 20000, 28000])
+@pytest.mark.parametrize("tokens", [2, 600])
+def test_every_number_of_waves(B, channels, tokens):
+    """Rows on 3 to 16 waves, of one to four pieces a thread."""
+    _check(B, "bf16", _inputs("bf16", tokens, channels, gate="row"), "layer", "rms")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("post", [None, "rms", "layer"])
 @pytest.mark.parametrize("pre", [None, "rms", "layer"])
