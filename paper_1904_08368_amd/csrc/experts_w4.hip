@@ -3,7 +3,7 @@
 // A pair is a token and one of the experts it has chosen; pairs of one expert share its codes, which are most of what there is to read.  The first
 // launch makes h of every pair; the second y, of few pairs directly (a workgroup adds up what the experts make of 16 channels), of more through a pair's parts in memory, which a third adds
 // up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
-// reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 115 and 67 (4.8 and 4.2 TB/s).  Many rows to an expert: tiles, below.
+// reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 115 to 123 and 67 to 70 (4.4 to 4.8 and 4.0 to 4.2 TB/s).  Many rows to an expert: tiles, below.
 // One token on 8 experts, 4096 channels and 1024 beside them, fp16: 19 us, 12 and 8, two chains of loads (the 50 MB take 10).  500 tokens on 32 experts, 2048 and 1408: 96 us, plan 5, tiles 58 and 35, sum 5:
 // half of a tile's 64 rows are there, so that the widening of the codes and its products, which a SIMD issues one or the other, take 3400 of 3750 clocks a chunk.
 // Codes become operands as in the dense kernels (16 + code, the sums of x taking the zero points out).

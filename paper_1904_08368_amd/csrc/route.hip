@@ -3,7 +3,7 @@
 // Two experts next to each other must not change places with the order of a sum, so products are added up in 64 bits (a product of two 16-bit
 // numbers is exact there).  The workgroup that is last to leave its part of the logits of a tile of tokens makes the choice for them: one launch.
 // One token, 64 experts by 4096 channels, bf16: 6.2 us, loads, one exchange between workgroups and eight choices in turn.  509 tokens, 128 experts, fp16: 19.9 us, of which the products on the matrix
-// cores of 64 bits, 43 % of the clocks, would be 8 (products by vector instructions 108 us in all); a last workgroup chooses for its 16 tokens in 4.
+// cores of 64 bits, 43 % of the clocks, would be 8 (with products by vector instructions the call took 130); a last workgroup chooses for its 16 tokens in 4.
 #include "decoder_ops.hpp"
 #include "wave_ops.hpp"
 
