@@ -5,7 +5,8 @@
 // up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
 // reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 115 to 123 and 67 to 70 (4.4 to 4.8 and 4.0 to 4.2 TB/s).  Many rows to an expert: tiles, below.
 // One token on 8 experts, 4096 channels and 1024 beside them, fp16: 19 us, 12 and 8, two chains of loads (the 50 MB take 10).  500 tokens on 32 experts, 2048 and 1408: 96 us, plan 5, tiles 58 and 35, sum 5:
-// half of a tile's 64 rows are there, so that the widening of the codes and its products, which a SIMD issues one or the other, take 3400 of 3750 clocks a chunk.
+// 47 blocks of 43 rows on the mean.  Vector and matrix work are 65 % of the clocks, the rest the start and end of a tile and the chain within a chunk (without the rows' copies 89 us, without the codes' loads 97, without
+// both 86); 1034 tiles on 768 places leave a second round short.
 // Codes become operands as in the dense kernels (16 + code, the sums of x taking the zero points out).
 #include <type_traits>
 
