@@ -44,7 +44,7 @@ typedef enum {
 typedef enum {
   RELAY_F32 = 0, RELAY_F16 = 1, RELAY_I8 = 2,
   RELAY_I16 = 3,  /* the 16/32 scheme only */
-  RELAY_BF16 = 4  /* the operators of relay_attention.h only */
+  RELAY_BF16 = 4  /* the operators of relay_attention.h and relay_decoder.h only */
 } relay_dtype;
 /* RELAY_NHWC4_PADDED: input of a first-layer conv with c <= 4 channels, stored [n][h + 2*pad_h]
  * [wp][4] with the zero border, wp - w - 2*pad_w slack columns and channels c..3 all zero

@@ -154,3 +154,14 @@ def test_parts_that_do_not_go_together(D):
                 lambda: D.Experts(router, down, up, 2)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_room_for_logits(D):
+    """max_rows of them, and a call for more is refused."""
+    full, _, _ = _model(D, "f16", layers=1, max_tokens=40)
+    few = D.Decoder(full.blocks, full.first, full.head, 40, max_rows=3)
+    n = _weights("f16", 5, 8, WIDTH, kind=torch.float16)
+    rows = torch.tensor([6, 0, 3], device=DEV)
+    assert torch.equal(few.logits(n, rows), full.logits(n)[rows]) and torch.equal(few.logits(n[:2]), full.logits(n)[:2])
+    with pytest.raises(ValueError):
+        few.logits(n)
