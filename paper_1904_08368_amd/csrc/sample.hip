@@ -13,6 +13,7 @@
 #include <float.h>
 
 #include "decoder_ops.hpp"
+#include "wave_ops.hpp"
 
 namespace relay {
 namespace {
@@ -70,11 +71,15 @@ struct Settings {
   bool cut_p, cut_min, greedy;
   double z_min;
   __device__ Settings(const SampleArgs& a, int r) {
-    temperature = a.temperature ? a.temperature[r] : 1.f;
-    top_p = a.top_p ? a.top_p[r] : 1.f;
-    min_p = a.min_p ? a.min_p[r] : 0.f;
-    u = a.uniform ? a.uniform[r] : 0.f;
-    top_k = a.top_k ? a.top_k[r] : 0;
+    // (all asked for at once; what is not there is read from some place that is, and not used)
+    const float* const some = reinterpret_cast<const float*>(a.tokens);
+    const float t = (a.temperature ? a.temperature : some)[r], p = (a.top_p ? a.top_p : some)[r], m = (a.min_p ? a.min_p : some)[r], v = (a.uniform ? a.uniform : some)[r];
+    const int k = (a.top_k ? a.top_k : a.tokens)[r];
+    temperature = a.temperature ? t : 1.f;
+    top_p = a.top_p ? p : 1.f;
+    min_p = a.min_p ? m : 0.f;
+    u = a.uniform ? v : 0.f;
+    top_k = a.top_k ? k : 0;
     if (!(temperature == temperature)) temperature = 1.f;
     if (top_k <= 0 || top_k >= a.vocab) top_k = 0;
     cut_p = top_p < 1.f;
@@ -102,6 +107,10 @@ struct Top { float best, low; int at; };   // the maximum, the lowest number, th
 __device__ __forceinline__ void merge(Top& t, float best, float low, int at) {
   if (best > t.best || (best == t.best && at < t.at)) t.best = best, t.at = at;
   t.low = fminf(t.low, low);
+}
+__device__ __forceinline__ Top of_wave(const Top& t) {   // all lanes'
+  const float best = wave_fold32(t.best, [](float x, float y) { return fmaxf(x, y); });
+  return {best, wave_fold32(t.low, [](float x, float y) { return fminf(x, y); }), wave_fold32(t.best == best ? t.at : 0x7fffffff, [](int x, int y) { return min(x, y); })};
 }
 
 template <typename T>
@@ -253,11 +262,7 @@ struct Row {
       });
     }
     own = t.best;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const float best = __shfl_xor(t.best, d), low = __shfl_xor(t.low, d);
-      merge(t, best, low, __shfl_xor(t.at, d));
-    }
+    t = of_wave(t);
     if ((tid & 63) == 0) s.wavef[0][tid >> 6] = t.best, s.wavef[1][tid >> 6] = t.low, s.wave32[tid >> 6] = (unsigned)t.at;
     __syncthreads();
 #pragma unroll
@@ -784,9 +789,7 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(const SampleArgs a) {
     h.top[g] = t;
     if (g == 0) h.listed = h.arrived = 0;
   }
-  float most = row.own;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+  const float most = wave_fold32(row.own, [](float x, float y) { return fmaxf(x, y); });
   if ((threadIdx.x & 63) == 0) h.maxima[g * WAVES + (threadIdx.x >> 6)] = most;
   for (int i = BINS * g / parts + (int)threadIdx.x; i < BINS * (g + 1) / parts; i += NT) h.mass[i] = 0, h.count[i] = 0;
 }
@@ -795,12 +798,7 @@ __device__ __forceinline__ Top top_of(const Shared& h, int parts) {
   Top t{-__builtin_inff(), __builtin_inff(), 0x7fffffff};
   const int lane = (int)threadIdx.x & 63;
   if (lane < parts) t = h.top[lane];
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const float best = __shfl_xor(t.best, d), low = __shfl_xor(t.low, d);
-    merge(t, best, low, __shfl_xor(t.at, d));
-  }
-  return t;
+  return of_wave(t);
 }
 
 template <typename T>

@@ -1,5 +1,7 @@
 // Sums and maxima over the 64 lanes of a wave, in a fixed order, the same bits in every lane.
 #pragma once
+#include <type_traits>
+
 #include "attn_common.hpp"
 
 namespace relay {
@@ -33,6 +35,22 @@ __device__ __forceinline__ float wave_sum(float v) {
   v += lane_moved<0x141>(v);
   v += lane_moved<0x140>(v);
   return sum_quarters(v);
+}
+template <typename V, typename F>   // (32 bits)
+__device__ __forceinline__ V wave_fold32(V v, F f) {
+  auto moved = [](V u, auto ctrl) { return __builtin_bit_cast(V, lane_moved<decltype(ctrl)::value>(__builtin_bit_cast(unsigned, u))); };
+  v = f(v, moved(v, std::integral_constant<int, 0xB1>()));
+  v = f(v, moved(v, std::integral_constant<int, 0x4E>()));
+  v = f(v, moved(v, std::integral_constant<int, 0x141>()));
+  v = f(v, moved(v, std::integral_constant<int, 0x140>()));
+  const unsigned b = __builtin_bit_cast(unsigned, v);
+  const auto rows = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  const unsigned r0 = rows[0], r1 = rows[1];
+  v = f(__builtin_bit_cast(V, r0), __builtin_bit_cast(V, r1));
+  const unsigned c = __builtin_bit_cast(unsigned, v);
+  const auto halves = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  const unsigned h0 = halves[0], h1 = halves[1];
+  return f(__builtin_bit_cast(V, h0), __builtin_bit_cast(V, h1));
 }
 template <typename V, typename F>
 __device__ __forceinline__ V wave_fold64(V v, F f) {
