@@ -903,12 +903,13 @@ hipError_t launch_type(const SampleArgs& a, int parts, hipStream_t st) {
   return hipGetLastError();
 }
 
-// A row to a workgroup, or to as many as give every CU one.  Measured in graphs, bf16, top-k 50 and top-p 0.95, us in one launch / shared out: one row of 16000 tokens 16 / 20, of 32000 20 / 20,
-// of 64000 29 / 20, of 128000 45 / 20; 64 rows of 64000 29 / 26, of 128000 46 / 31; 128 rows of 64000 30 / 31, of 128000 51 / 41; top-p 0.9 alone 1 x 128000 72 / 26, 64 x 128000 88 / 54.
-// 256 rows of 50257 in fp32 51 / 60 (two to a row).
+// A row to a workgroup, or to as many as give every CU one.  Measured in graphs, bf16, us in one launch / shared out, top-p 0.9 alone and top-k 50 with top-p 0.95: one row of 16000 tokens 17 / 20 and 11 / 26,
+// of 32000 23 / 21 and 13 / 17, of 64000 37 / 21 and 17 / 17, of 128000 63 / 23 and 23 / 17; 64 rows of 32000 26 / 26 and 14 / 23, of 64000 42 / 32 and 18 / 25, of 128000 81 / 51 and 26 / 30; 128 rows of 64000
+// 44 / 41 and 19 / 31, of 128000 84 / 68 and 29 / 41.  256 rows of 50257 in fp32, each with its own settings, 49 / 54 (two to a row).  What a row is asked for is known on the device alone: where there may be
+// top-k rows must be longer.
 int parts_of(const SampleArgs& a) {
   const int parts = a.rows >= 256 ? 1 : 256 / a.rows < 32 ? 256 / a.rows : 32;
-  return (long)a.vocab * (parts - 1) >= 24000L * parts ? parts : 1;
+  return (long)a.vocab * (parts - 1) >= (a.top_k ? 36000L : 24000L) * parts ? parts : 1;
 }
 
 }  // namespace
