@@ -7,8 +7,8 @@
 // Masses are integers, multiples of 2^-S of the largest weight: sums of them have no order, and the borders between tokens are where 64 bits put them.
 // So a row is read three times: maximum; counts or masses; gathering.  One workgroup reads it where there are many rows, from the caches after the first time.  Of few rows each is shared out over
 // workgroups, a launch to each reading.
-// One row of 128000 fp16, top-k 50 and top-p: 18 us, launches of 5, 3 and 11 that wait for memory and for each other.  48 rows of 151643 bf16, top-p: 52 us, of 7, 15 and 30: weights in 64 bits and
-// additions to LDS in the second (50 % and 29 % of the clocks), in the third a last workgroup that sorts some 300 tokens of one value.  256 rows of 50257 fp32, each with its own settings: 50 us,
+// One row of 128000 fp16, top-k 50 and top-p: 16.5 us, launches of 4, 2.5 and 11 that wait for memory and for each other.  48 rows of 151643 bf16, top-p: 49 us, of 7, 14 and 29: weights in 64 bits and
+// additions to LDS in the second (50 % and 28 % of the clocks), in the third a last workgroup that sorts some 300 tokens of one value.  256 rows of 50257 fp32, each with its own settings: 48 us,
 // additions to LDS (some 30 clocks for a wave's, whose lanes meet on banks) and weights by eight waves a CU.
 #include <float.h>
 
@@ -394,7 +394,7 @@ struct Row {
   // The tokens that `is` names, of those that `near` does, into s.run, as they come; how many, or more than CAP if they do not fit.
   template <typename N, typename F>
   __device__ __forceinline__ int gather(N near, F is, vec (&first)[2]) const {
-    constexpr bool NEAR = V > 4;   // (of four tokens to a piece, a wave waits more often for one that is near than it saves: 256 rows of 50257 in fp32 50 / 58 us; bf16, 64 x 128000 36 / 32)
+    constexpr bool NEAR = V > 4;   // (of four tokens to a piece, a wave waits more often for one that is near than it saves: without / with, 256 rows of 50257 in fp32 50 / 58 us; bf16, 64 x 128000 36 / 32)
     if (tid == 0) s.listed = 0;
     __syncthreads();
     auto take = [&](float l, int i) {
