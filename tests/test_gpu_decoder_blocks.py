@@ -165,3 +165,50 @@ def test_room_for_logits(D):
     assert torch.equal(few.logits(n, rows), full.logits(n)[rows]) and torch.equal(few.logits(n[:2]), full.logits(n)[:2])
     with pytest.raises(ValueError):
         few.logits(n)
+
+
+def test_calls_on_two_streams_at_once(D):
+    """Workspaces of their own, and neither sees the other: router, experts and sampler side by side, eagerly and from two graphs that are replayed together."""
+    dtype = TYPES["bf16"][0]
+    lanes = []
+    for seed in (1, 2):
+        decoder, _, _ = _model(D, "bf16", layers=1, max_tokens=64)
+        x, logits = _weights("bf16", seed, 50, WIDTH, kind=dtype), _weights("bf16", 10 + seed, 3, 60001, std=2.0, kind=dtype)
+        lanes.append(dict(experts=decoder.blocks[0].experts, sampler=D.Sampler(), x=x, y=torch.empty_like(x), logits=logits, tokens=torch.zeros(3, dtype=torch.int32, device=DEV),
+                          uniform=torch.tensor([0.2, 0.5, 0.8], device=DEV), top_p=torch.full((3,), 0.9, device=DEV), stream=torch.cuda.Stream()))
+
+    def step(lane):
+        lane["experts"](lane["x"], lane["y"])
+        lane["sampler"](lane["logits"], top_p=lane["top_p"], uniform=lane["uniform"], tokens=lane["tokens"])
+
+    want = []
+    for lane in lanes:
+        step(lane)
+        torch.cuda.synchronize()
+        want.append((lane["y"].clone(), lane["tokens"].clone()))
+
+    def check():
+        torch.cuda.synchronize()
+        for lane, (y, tokens) in zip(lanes, want):
+            assert torch.equal(lane["y"], y) and torch.equal(lane["tokens"], tokens)
+            lane["y"].zero_()
+            lane["tokens"].zero_()
+        torch.cuda.synchronize()
+
+    check()
+    for _ in range(5):
+        for lane in lanes:
+            with torch.cuda.stream(lane["stream"]):
+                for _ in range(4):
+                    step(lane)
+        check()
+    graphs = []
+    for lane in lanes:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            step(lane)
+    for _ in range(5):
+        for lane, graph in zip(lanes, graphs):
+            with torch.cuda.stream(lane["stream"]):
+                graph.replay()
+        check()
