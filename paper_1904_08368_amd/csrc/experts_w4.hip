@@ -74,11 +74,10 @@ struct Chunk {
     }
     int group;                 // this lane's of a chunk's groups
   };
-  // chunk `chunk` of the tiles `ahead` behind the first
-  __device__ __forceinline__ void load_codes(const Where& w, const W4Layout& l, const FastDiv& per_group, int ahead, int chunk, int lane) {
+  __device__ __forceinline__ void load_codes(const Where& w, const W4Layout& l, const FastDiv& per_group, int chunk, int lane) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) codes[t] = (w.codes[t] + ((size_t)ahead * l.chunks + chunk) * 64)[(unsigned)lane];
-    params = w.params[((size_t)ahead * l.groups + min((int)fast_div((unsigned)(chunk * 4), per_group) + w.group, l.groups - 1)) * w.step];
+    for (int t = 0; t < NT; ++t) codes[t] = (w.codes[t] + (size_t)chunk * 64)[(unsigned)lane];
+    params = w.params[(size_t)min((int)fast_div((unsigned)(chunk * 4), per_group) + w.group, l.groups - 1) * w.step];
   }
   __device__ __forceinline__ void load_x(const Where& w, int chunk, int k, int lane) {
     const int at = chunk * 128 + (lane & 15) * 8 < k ? chunk * 128 : 0;
@@ -86,8 +85,7 @@ struct Chunk {
     for (int i = 0; i < XL; ++i) x[i] = *reinterpret_cast<const uintx4*>(w.row[i] + at);
   }
   // sums += the chunk's part; mine: PIECES of LDS of this wave
-  template <int RT>
-  __device__ __forceinline__ void add(floatx4 (&sum)[NT][RT], uintx4* mine, const W4Layout& l, const FastDiv& per_group, bool zeros, const Widen<T>& widen, int chunk, int k, int lane) const {
+  __device__ __forceinline__ void add(floatx4 (&sum)[NT], uintx4* mine, const W4Layout& l, const FastDiv& per_group, bool zeros, const Widen<T>& widen, int chunk, int k, int lane) const {
     typedef W4Type<T> C;
     typedef typename C::vec vec;
     const int g = lane >> 4, col = lane & 15;
@@ -101,23 +99,15 @@ struct Chunk {
     const unsigned* const zps = reinterpret_cast<const unsigned*>(mine + XL * 64 + NT * PG * 2);
 #pragma unroll
     for (int f = 0; f < PG; ++f) {
-      floatx4 acc[NT][RT], xs[RT];
+      floatx4 acc[NT], xs;
 #pragma unroll
       for (int s = f * FL; s < (f + 1) * FL; ++s) {
         const bool fresh = s == f * FL;
-        vec xb[RT];
+        const int at = col & (4 * XL - 1);   // (of fewer rows than columns: those behind repeat them)
+        const vec xb = __builtin_bit_cast(vec, mine[at * 16 + ((4 * s + g) ^ (at & 15))]);
+        xs = C::mfma(ones, xb, fresh ? none : xs);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const int at = XL < 4 ? col & (4 * XL - 1) : r * 16 + col;   // (fewer rows than columns: those behind repeat them)
-          xb[r] = __builtin_bit_cast(vec, mine[at * 16 + ((4 * s + g) ^ (at & 15))]);
-          xs[r] = C::mfma(ones, xb[r], fresh ? none : xs[r]);
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const vec wv = widen(codes[t][s]);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) acc[t][r] = C::mfma(wv, xb[r], fresh ? none : acc[t][r]);
-        }
+        for (int t = 0; t < NT; ++t) acc[t] = C::mfma(widen(codes[t][s]), xb, fresh ? none : acc[t]);
       }
       // (the group of step f * FL, counted from the chunk's first)
       const int gr = PG == 1 ? 0 : min((int)fast_div((unsigned)(chunk * 4 + f * FL), per_group), l.groups - 1) - (int)fast_div((unsigned)(chunk * 4), per_group);
@@ -128,8 +118,7 @@ struct Chunk {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float z = -(float)((zp >> (8 * i)) & 255u), kf = (float)sc[i];
-#pragma unroll
-          for (int r = 0; r < RT; ++r) sum[t][r][i] = fmaf(kf, fmaf(z, xs[r][i], acc[t][r][i]), sum[t][r][i]);
+          sum[t][i] = fmaf(kf, fmaf(z, xs[i], acc[t][i]), sum[t][i]);
         }
       }
     }
@@ -140,23 +129,23 @@ __device__ __forceinline__ float activated(int act, float v) {
   return act == A_SILU ? v / (1.f + expf(-v)) : 0.5f * v * erfcf(v * -0.70710678118654752440f);   // (1 + erf(v) is erfc(-v), without the difference)
 }
 
-// sums += chunks first .. last - 1 of the tiles `ahead` behind the first, D of them on their way: c holds the first D.
-template <int D, typename T, int NT, int XL, int FL, int RT>
-__device__ __forceinline__ void walk(floatx4 (&sum)[NT][RT], Chunk<T, NT, XL, FL> (&c)[D], const typename Chunk<T, NT, XL, FL>::Where& w, const W4Layout& l, const FastDiv& per_group, bool zeros,
-                                     int ahead, int first, int last, int k, uintx4* mine, const Widen<T>& widen, int lane) {
+// sums += chunks first .. last - 1 of the tiles, D of them on their way: c holds the first D.
+template <int D, typename T, int NT, int XL, int FL>
+__device__ __forceinline__ void walk(floatx4 (&sum)[NT], Chunk<T, NT, XL, FL> (&c)[D], const typename Chunk<T, NT, XL, FL>::Where& w, const W4Layout& l, const FastDiv& per_group, bool zeros,
+                                     int first, int last, int k, uintx4* mine, const Widen<T>& widen, int lane) {
   int chunk = first;
   for (; chunk + D < last; chunk += D) {
 #pragma unroll
     for (int i = 0; i < D; ++i) {
-      c[i].template add<RT>(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
-      c[i].load_codes(w, l, per_group, ahead, min(chunk + i + D, last - 1), lane);
+      c[i].add(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
+      c[i].load_codes(w, l, per_group, min(chunk + i + D, last - 1), lane);
       c[i].load_x(w, min(chunk + i + D, last - 1), k, lane);
       __builtin_amdgcn_sched_barrier(0);   // (two chunks' sums side by side take twice the registers)
     }
   }
 #pragma unroll
   for (int i = 0; i < D; ++i) {
-    if (chunk + i < last) c[i].template add<RT>(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
+    if (chunk + i < last) c[i].add(sum, mine, l, per_group, zeros, widen, chunk + i, k, lane);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -166,7 +155,7 @@ __device__ __forceinline__ void walk(floatx4 (&sum)[NT][RT], Chunk<T, NT, XL, FL
 template <typename T, bool UP, int XL, int KS, int D, int W, int FL>
 __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsArgs a, const W4Layout l, const FastDiv per_group, const int n) {
   typedef Chunk<T, 2, XL, FL> Held;
-  constexpr int RT = XL <= 4 ? 1 : XL / 4, ROWS = XL * 4, SUMS = 2 * RT * 64, LDS = Held::PIECES > SUMS ? Held::PIECES : SUMS, PER = UP ? 1 : 2;
+  constexpr int ROWS = XL * 4, SUMS = 2 * 64, LDS = Held::PIECES > SUMS ? Held::PIECES : SUMS, PER = UP ? 1 : 2;
   __shared__ __attribute__((aligned(16))) uintx4 lds[W][LDS];
   __shared__ int rows_of[W][ROWS];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4;
@@ -190,13 +179,13 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
     const long tile[2] = {base + t, base + (UP ? t + units : min(t + 1, units - 1))};
     where.set(packed, l, a.zeros, tile, lane);
 #pragma unroll
-    for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, 0, max(min(first + j, last - 1), 0), lane);
+    for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, max(min(first + j, last - 1), 0), lane);
   };
   auto load_x = [&]() {
 #pragma unroll
     for (int j = 0; j < D; ++j) c[j].load_x(where, max(min(first + j, last - 1), 0), k, lane);
   };
-  for (int from = (int)blockIdx.z * ROWS;; from += (int)gridDim.z * ROWS) {
+  for (int from = 0;; from += ROWS) {
     at_tile(0);   // (on its way while the rows are looked up)
     const Found found = pairs_of(a.chosen, a.pairs, e, from, ROWS, rows, lane);
     if (from >= found.all || (a.by_pair && found.first != (int)blockIdx.y)) return;   // (an expert's first pair stands for it; the same for all waves)
@@ -205,16 +194,10 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
     for (int i = 0; i < XL; ++i) where.row[i] = x_of(rows[min(4 * i + g, have - 1)]) + (lane & 15) * 8;   // (rows that are not there repeat the last one)
     load_x();
     for (int i = 0; i < many; ++i) {
-      floatx4 sum[2][RT];
+      floatx4 sum[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      if (first < last) walk<D, T, 2, XL, FL>(sum, c, where, l, per_group, a.zeros, first, last, k, mine, widen, lane);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) sum[t][r] = (floatx4){0, 0, 0, 0};
-      if (first < last) walk<D, T, 2, XL, FL, RT>(sum, c, where, l, per_group, a.zeros, 0, first, last, k, mine, widen, lane);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) reinterpret_cast<floatx4*>(mine)[(t * RT + r) * 64 + lane] = sum[t][r];
+      for (int t = 0; t < 2; ++t) reinterpret_cast<floatx4*>(mine)[t * 64 + lane] = sum[t];
       if (i + 1 < many) {
         at_tile(i + 1);
         load_x();
@@ -222,8 +205,8 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
       if (KS > 1) __syncthreads();
       // four units of a pair: to a lane in turn of the KS waves
 #pragma unroll 1
-      for (int j = KS > 1 ? (wave % KS) * 64 + lane : lane; j < PER * RT * 64; j += KS * 64) {
-        const int t = j / (RT * 64), at = j / 64 % RT * 16 + (j & 15), tl = tile0 + i * PER + t;
+      for (int j = KS > 1 ? (wave % KS) * 64 + lane : lane; j < PER * 64; j += KS * 64) {
+        const int t = j / 64, at = j & 15, tl = tile0 + i * PER + t;
         if (at >= have || tl >= units) continue;
         floatx4 v[UP ? 2 : 1];
         const int p = rows[at], u0 = tl * 16 + 4 * (j >> 4 & 3);
@@ -231,7 +214,7 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
         for (int w = 0; w < (UP ? 2 : 1); ++w) {
           v[w] = (floatx4){0, 0, 0, 0};
 #pragma unroll
-          for (int u = 0; u < KS; ++u) v[w] += reinterpret_cast<const floatx4*>(lds[wave / KS * KS + u])[j + w * RT * 64];
+          for (int u = 0; u < KS; ++u) v[w] += reinterpret_cast<const floatx4*>(lds[wave / KS * KS + u])[j + w * 64];
           if (__builtin_expect(!is_finite(v[w]), 0))
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
@@ -252,7 +235,7 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
       }
       if (KS > 1) __syncthreads();
     }
-    if (from + (int)gridDim.z * ROWS >= found.all) return;
+    if (from + ROWS >= found.all) return;
   }
 }
 
@@ -358,9 +341,9 @@ __global__ __launch_bounds__(256, (std::is_same<T, _Float16>::value ? 3 : 2)) vo
 #pragma unroll
     for (int r = 0; r < RT; ++r) sum[t][r] = none;
   Held c[2];
-  c[0].load_codes(where, l, per_group, 0, 0, lane);
+  c[0].load_codes(where, l, per_group, 0, lane);
   copy(0);
-  c[1].load_codes(where, l, per_group, 0, min(1, l.chunks - 1), lane);
+  c[1].load_codes(where, l, per_group, min(1, l.chunks - 1), lane);
   auto turn = [&](Held& now, int chunk) {
     // Behind the rows of this chunk a wave has asked for one chunk's codes: two loads, and one of scales.
     asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)" ::: "memory");
@@ -376,7 +359,7 @@ __global__ __launch_bounds__(256, (std::is_same<T, _Float16>::value ? 3 : 2)) vo
       asm volatile("" : "+v"(codes[t]));
     }
     if (chunk + 1 < l.chunks) copy(chunk + 1);
-    now.load_codes(where, l, per_group, 0, min(chunk + 2, l.chunks - 1), lane);
+    now.load_codes(where, l, per_group, min(chunk + 2, l.chunks - 1), lane);
     const uintx4* const xl = xs_lds[chunk & 1];
     const four* const scales = reinterpret_cast<const four*>(mine);
     const unsigned* const zps = reinterpret_cast<const unsigned*>(mine + NT * PG * 2);
@@ -507,19 +490,19 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
     const long at[1] = {(long)e * (a.channels / 16) + tile};
     where.set(packed, l, a.zeros, at, lane);
     for (int from = 0; from < have; from += ROWS) {
-      floatx4 sum[1][1] = {{{0, 0, 0, 0}}};
+      floatx4 sum[1] = {{0, 0, 0, 0}};
 #pragma unroll
       for (int i = 0; i < XL; ++i) where.row[i] = h + (long)rows[min(from + 4 * i + g, have - 1)] * a.inter + (lane & 15) * 8;   // (rows that are not there repeat the last one)
       if (first < last) {
         Held c[D];
 #pragma unroll
-        for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, 0, min(first + j, last - 1), lane);
+        for (int j = 0; j < D; ++j) c[j].load_codes(where, l, per_group, min(first + j, last - 1), lane);
 #pragma unroll
         for (int j = 0; j < D; ++j) c[j].load_x(where, min(first + j, last - 1), a.inter, lane);
-        walk<D, T, 1, XL, FL, 1>(sum, c, where, l, per_group, a.zeros, 0, first, last, a.inter, mine, widen, lane);
+        walk<D, T, 1, XL, FL>(sum, c, where, l, per_group, a.zeros, first, last, a.inter, mine, widen, lane);
       }
       const int row = from + (lane & 15);
-      if ((lane & 15) < ROWS && row < have) parts[turn * kJoined + rows[row]][g] = sum[0][0];
+      if ((lane & 15) < ROWS && row < have) parts[turn * kJoined + rows[row]][g] = sum[0];
     }
   }
   __syncthreads();

@@ -21,15 +21,7 @@ __device__ __forceinline__ u64 key_of(double v) {
 }
 
 __device__ __forceinline__ unsigned wave_max32(unsigned v) {
-  auto most = [](unsigned a, unsigned b) { return a > b ? a : b; };
-  v = most(v, lane_moved<0xB1>(v));
-  v = most(v, lane_moved<0x4E>(v));
-  v = most(v, lane_moved<0x141>(v));
-  v = most(v, lane_moved<0x140>(v));
-  const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = most(rows[0], rows[1]);
-  const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return most(halves[0], halves[1]);
+  return wave_fold32(v, [](unsigned a, unsigned b) { return a > b ? a : b; });
 }
 
 // The choice for token t, by one wave.  Lane l holds experts l, l + 64, ..: score comes as their logits.
