@@ -85,7 +85,8 @@ typedef struct {
 
 /* y[t] = sum_s weights[t][s] * down_e (act(gate_e x[t]) * up_e x[t])  [+ residual[t]],   e = chosen[t][s]
  * for few tokens, where the chosen experts' codes are most of what there is to read: each is read once for all the tokens that chose it.
- * weights * act * up is rounded to the tensors' type for the second product (an operand of the matrix cores); sums are fp32, in a fixed order.
+ * act * up is rounded to the tensors' type for the second product (an operand of the matrix cores; past the type's range it is an infinity); sums are fp32, in a fixed order, and
+ * weights are applied to them.
  * Two launches for up to 8 or 16 choices, three or four for more (of up to 4096 at a time): what is elementwise goes into the products' ends (paper
  * Section 4.1), scales behind the quantized operands (Section 4.2).
  * gate_up and down are packed by relay_prepack_qdense_w4 with the experts' units one behind the other:

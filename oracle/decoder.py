@@ -71,7 +71,8 @@ def route(x, w, top_k, score="softmax", bias=None, normalize=True, scale=1.0):
 def experts(x, chosen, weights, gate_up, down, inter, group, act="silu", residual=None, u=2.0 ** -11, tiny=2.0 ** -24):
     """gate_up, down: (codes, scales, zeros) of all experts' units one behind the other; u, tiny: half a step and the least step of the type that h is
     rounded to.  Returns y [tokens, channels] before its rounding and a bound of its error: of the sums of 32 bits (oracle.attention.dense_w4), through the activation
-    (whose slope is 1.13 at most, its own functions off by 8 half-steps), the product and its rounding, through the second product."""
+    (whose slope is 1.13 at most, its own functions off by 8 half-steps), the product and its rounding, through the second product, and times the weight (which is added
+    up in one rounding with its part)."""
     tokens, channels = x.shape
     part = lambda w, first, n: tuple(None if a is None else a[first:first + n] for a in w)
     y, err = np.zeros((tokens, channels)), np.zeros((tokens, channels))
@@ -82,10 +83,9 @@ def experts(x, chosen, weights, gate_up, down, inter, group, act="silu", residua
         with np.errstate(over="ignore"):
             a = g / (1 + np.exp(-g)) if act == "silu" else 0.5 * g * np.vectorize(math.erfc)(-g * math.sqrt(0.5))
         da = 1.13 * dg + 8 * E32 * (np.abs(a) + dg)
-        w = weights[tok, slot][:, None]
-        h = w * a * v
-        dh = np.abs(w) * ((np.abs(a) + da) * (np.abs(v) + dv) - np.abs(a * v))
-        dh = dh + 3 * E32 * (np.abs(h) + dh)
+        h = a * v
+        dh = (np.abs(a) + da) * (np.abs(v) + dv) - np.abs(h)
+        dh = dh + E32 * (np.abs(h) + dh)
         dh = dh + u * (np.abs(h) + dh) + tiny
         wd = part(down, e * channels, channels)
         out, bound = attention.dense_w4(h, *wd, group)
@@ -94,9 +94,10 @@ def experts(x, chosen, weights, gate_up, down, inter, group, act="silu", residua
         which = np.arange(inter) // group
         mag = np.abs((codes - (8.0 if wd[2] is None else wd[2][:, which].astype(np.float64))) * wd[1][:, which])
         moved = dh @ mag.T
-        np.add.at(y, tok, out)
-        np.add.at(err, tok, 1.02 * bound + moved)
-        np.add.at(size, tok, np.abs(out) + bound + moved)
+        w = weights[tok, slot][:, None]
+        np.add.at(y, tok, w * out)
+        np.add.at(err, tok, np.abs(w) * (1.02 * bound + moved))
+        np.add.at(size, tok, np.abs(w) * (np.abs(out) + bound + moved))
     if residual is not None:
         y, size = y + residual, size + np.abs(residual)
     return y, err + (chosen.shape[1] + 2) * E32 * size

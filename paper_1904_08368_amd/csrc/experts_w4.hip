@@ -1,8 +1,9 @@
-// The experts of a mixture with 4-bit weights for a few tokens:  h = weight act(gate x) (up x),  y = sum over a token's experts of down h.
+// The experts of a mixture with 4-bit weights for a few tokens:  h = act(gate x) (up x),  y = sum over a token's experts of weight down h.
 //
 // A pair is a token and one of the experts it has chosen; pairs of one expert share its codes, which are most of what there is to read.  The first
 // launch makes h of every pair; the second y, of few pairs directly (a workgroup adds up what the experts make of 16 channels), of more through a pair's parts in memory, which a third adds
-// up.  The experts' weights go into h: the second product then needs none.  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
+// up.  h is rounded to 16 bits, an operand of the matrix cores.  A router's weight is applied to its pair's part of y, in fp32: within h a small one took fp16's bits (a weight of
+// 0.002 at an h of 1e-3: 1 % of the part).  A wave streams the codes of two tiles of 16 units through its registers and knows nothing of other waves: with the
 // reduction shared out over eight, 64 tokens on 128 experts took 343 us for the first product and 504 for the second, now 115 to 123 and 67 to 70 (4.4 to 4.8 and 4.0 to 4.2 TB/s).  Many rows to an expert: tiles, below.
 // One token on 8 experts, 4096 channels and 1024 beside them, fp16: 19 us, 12 and 8, two chains of loads (the 50 MB take 10).  500 tokens on 32 experts, 2048 and 1408: 96 us, plan 5, tiles 58 and 35, sum 5:
 // 47 blocks of 43 rows on the mean.  Vector and matrix work are 65 % of the clocks, the rest the start and end of a tile and the chain within a chunk (without the rows' copies 89 us, without the codes' loads 97, without
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
           typedef T four __attribute__((ext_vector_type(4)));
           four h;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) h[q] = (T)(a.weights[p] * activated(a.act, v[0][q]) * v[1][q]);
+          for (int q = 0; q < 4; ++q) h[q] = (T)(activated(a.act, v[0][q]) * v[1][q]);
           *reinterpret_cast<four*>(static_cast<T*>(a.h) + (long)p * a.inter + u0) = h;
         } else {
           *reinterpret_cast<floatx4*>(a.parts + (long)p * a.channels + u0) = v[0];
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(256, (std::is_same<T, _Float16>::value ? 3 : 2)) vo
               for (int f = 0; f < 4; ++f) v[w][f] = q == f ? again : v[w][f];
             }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) h[q] = (T)(a.weights[p] * activated(a.act, v[0][q]) * v[1][q]);
+      for (int q = 0; q < 4; ++q) h[q] = (T)(activated(a.act, v[0][q]) * v[1][q]);
       *reinterpret_cast<four*>(static_cast<T*>(a.h) + (long)p * a.inter + tile0 * 16 + 4 * g) = h;
     } else {
 #pragma unroll
@@ -466,10 +467,12 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
   __shared__ __attribute__((aligned(16))) uintx4 lds[W][Held::PIECES];
   __shared__ __attribute__((aligned(16))) floatx4 parts[W * kJoined][4];   // [share of the reduction][pair]
   __shared__ int rows_of[W][kJoined];
+  __shared__ float weight_of[kJoined];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, tile = (int)blockIdx.x;
   const unsigned char* const packed = static_cast<const unsigned char*>(a.down);
   const T* const h = static_cast<const T*>(a.h);
   const int named = lane < a.pairs ? a.chosen[lane] : -1;
+  if ((int)threadIdx.x < a.pairs) weight_of[threadIdx.x] = a.weights[threadIdx.x];
   const unsigned long long valid = __ballot((unsigned)named < (unsigned)a.experts);
   int many = 0;
   for (unsigned long long left = valid; left; ++many) left &= ~__ballot(named == __builtin_amdgcn_readlane(named, __builtin_ctzll(left)));
@@ -515,7 +518,7 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
       for (int u = 0; u < shares; ++u) part += reinterpret_cast<const float*>(parts[u * kJoined + p])[j];
       if (__builtin_expect(!is_finite(part), 0))
         part = sum_by_weights<T>(packed, l, a.inter, a.group_of(a.inter), a.zeros, h + (long)p * a.inter, a.chosen[p] * a.channels + tile * 16 + j);
-      v += part;
+      v = fmaf(weight_of[p], part, v);
     }
     const long at = (long)t * a.y_stride + tile * 16 + j;
     if (a.res) v += (float)static_cast<const T*>(a.res)[at];
@@ -536,15 +539,19 @@ __global__ __launch_bounds__(256) void experts_add_kernel(const ExpertsArgs a) {
   for (int s0 = 0; s0 < a.top_k; s0 += 8) {
     floatx4 part[8];
     int named[8];
+    float weight[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       const int p = t * a.top_k + min(s0 + s, a.top_k - 1);
       named[s] = a.chosen[p];
+      weight[s] = a.weights[p];
       part[s] = *reinterpret_cast<const floatx4*>(a.parts + (long)p * a.channels + c);
     }
 #pragma unroll
     for (int s = 0; s < 8; ++s)   // (a pair that names no expert has no part: what stands in its place is not used)
-      if (s0 + s < a.top_k && (unsigned)named[s] < (unsigned)a.experts) v += part[s];
+      if (s0 + s < a.top_k && (unsigned)named[s] < (unsigned)a.experts)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(weight[s], part[s][j], v[j]);
   }
   four out;
 #pragma unroll
