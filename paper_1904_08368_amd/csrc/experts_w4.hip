@@ -13,6 +13,7 @@
 
 #include "decoder_ops.hpp"
 #include "lds_dma.hpp"
+#include "row_piece.hpp"
 #include "w4_common.hpp"
 
 namespace relay {
@@ -57,7 +58,7 @@ struct Chunk {
     const uintx4* codes[NT];   // of the tiles' first chunk (the same for all lanes)
     const uintx4* params;      // this lane's piece of the scales (of the zero points) of the tiles' first group
     int step, half;            // pieces from group to group; of scales
-    const T* row[XL];          // this lane's rows, at its piece of a chunk
+    const T* row[XL];          // this lane's rows
     __device__ __forceinline__ void set(const unsigned char* packed, const W4Layout& l, bool zeros, const long (&tile)[NT], int lane) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) codes[t] = reinterpret_cast<const uintx4*>(packed) + (size_t)tile[t] * l.chunks * 64;
@@ -81,7 +82,7 @@ struct Chunk {
     params = w.params[(size_t)min((int)fast_div((unsigned)(chunk * 4), per_group) + w.group, l.groups - 1) * w.step];
   }
   __device__ __forceinline__ void load_x(const Where& w, int chunk, int k, int lane) {
-    const int at = chunk * 128 + (lane & 15) * 8 < k ? chunk * 128 : 0;
+    const int at = row_piece(chunk, lane & 15, k);   // (what lies past k is taken as zeros)
 #pragma unroll
     for (int i = 0; i < XL; ++i) x[i] = *reinterpret_cast<const uintx4*>(w.row[i] + at);
   }
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(W * 64, 2) void experts_rows_kernel(const ExpertsAr
     if (from >= found.all || (a.by_pair && found.first != (int)blockIdx.y)) return;   // (an expert's first pair stands for it; the same for all waves)
     const int have = min(ROWS, found.all - from);
 #pragma unroll
-    for (int i = 0; i < XL; ++i) where.row[i] = x_of(rows[min(4 * i + g, have - 1)]) + (lane & 15) * 8;   // (rows that are not there repeat the last one)
+    for (int i = 0; i < XL; ++i) where.row[i] = x_of(rows[min(4 * i + g, have - 1)]);   // (rows that are not there repeat the last one)
     load_x();
     for (int i = 0; i < many; ++i) {
       floatx4 sum[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -495,7 +496,7 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
     for (int from = 0; from < have; from += ROWS) {
       floatx4 sum[1] = {{0, 0, 0, 0}};
 #pragma unroll
-      for (int i = 0; i < XL; ++i) where.row[i] = h + (long)rows[min(from + 4 * i + g, have - 1)] * a.inter + (lane & 15) * 8;   // (rows that are not there repeat the last one)
+      for (int i = 0; i < XL; ++i) where.row[i] = h + (long)rows[min(from + 4 * i + g, have - 1)] * a.inter;   // (rows that are not there repeat the last one)
       if (first < last) {
         Held c[D];
 #pragma unroll
