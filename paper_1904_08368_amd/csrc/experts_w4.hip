@@ -473,7 +473,7 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
   const unsigned char* const packed = static_cast<const unsigned char*>(a.down);
   const T* const h = static_cast<const T*>(a.h);
   const int named = lane < a.pairs ? a.chosen[lane] : -1;
-  if ((int)threadIdx.x < a.pairs) weight_of[threadIdx.x] = a.weights[threadIdx.x];
+  const float weight = lane < a.pairs ? a.weights[lane] : 0.f;
   const unsigned long long valid = __ballot((unsigned)named < (unsigned)a.experts);
   int many = 0;
   for (unsigned long long left = valid; left; ++many) left &= ~__ballot(named == __builtin_amdgcn_readlane(named, __builtin_ctzll(left)));
@@ -509,17 +509,19 @@ __global__ __launch_bounds__(kJoinWaves * 64, 2) void experts_join_kernel(const 
       if ((lane & 15) < ROWS && row < have) parts[turn * kJoined + rows[row]][g] = sum[0];
     }
   }
+  if (wave == 0 && lane < kJoined) weight_of[lane] = weight;
   __syncthreads();
   for (int i = (int)threadIdx.x; i < a.tokens * 16; i += W * 64) {
     const int t = i >> 4, j = i & 15;
     float v = 0.f;
     for (int p = t * a.top_k; p < (t + 1) * a.top_k; ++p) {
       if (!(valid >> p & 1)) continue;
-      float part = 0.f;
+      float part = 0.f, w = weight_of[p];
       for (int u = 0; u < shares; ++u) part += reinterpret_cast<const float*>(parts[u * kJoined + p])[j];
+      asm volatile("" : "+v"(w));   // (asked for with the part: behind the branch it would be a read of its own)
       if (__builtin_expect(!is_finite(part), 0))
         part = sum_by_weights<T>(packed, l, a.inter, a.group_of(a.inter), a.zeros, h + (long)p * a.inter, a.chosen[p] * a.channels + tile * 16 + j);
-      v = fmaf(weight_of[p], part, v);
+      v = fmaf(w, part, v);
     }
     const long at = (long)t * a.y_stride + tile * 16 + j;
     if (a.res) v += (float)static_cast<const T*>(a.res)[at];
