@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256) void route_few_kernel(const RouteArgs a) {
       if (r < a.tokens) {
         const vec xv = *reinterpret_cast<const vec*>(x + (size_t)r * a.x_stride + c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[r] += (double)((float)wv[i] * (float)xv[i]);
+        for (int i = 0; i < 8; ++i) sum[r] = fma((double)(float)wv[i], (double)(float)xv[i], sum[r]);   // (in 32 bits a product of two bf16 numbers may leave the range)
       }
   }
 #pragma unroll
