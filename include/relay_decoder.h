@@ -110,7 +110,7 @@ typedef struct {
 /* One token of each row, in one primitive function from the logits (paper Section 4.1).  With w_i = exp((l_i - max l) / temperature), tokens in descending order of their logits, equal ones in the order of their numbers:
  *   top_k:  the first top_k of them                                       (0 or less: all)
  *   top_p:  of these the shortest run from the first on whose w add up to at least top_p times the sum over them   (1 or more: all)
- *   min_p:  of these the ones with w >= min_p                              (0 or less: all)
+ *   min_p:  of these the ones with w >= min_p                              (0 or less: all; above 1: none but the first)
  * the first is always kept, and the token is the first kept one at which the running sum of w exceeds uniform times the sum over the kept.
  * temperature 0 (or less): the first.  uniform: in 0 <= u < 1 (less counts as 0, more as the number before 1).  A setting that is NaN is off, a NaN temperature is 1, a NaN uniform 0.
  * A logit that is NaN counts as -infinity; tokens of -infinity are never named.  A row without any other gets token -1 and probability 0; a

@@ -123,7 +123,7 @@ def sample(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, uniform=0.0):
         mass = np.cumsum(w[:n])
         n = int(np.searchsorted(mass, top_p * mass[-1], side="left")) + 1 if top_p > 0 else 1
     if min_p > 0:
-        n = max(1, min(n, int((w >= min(min_p, 1.0)).sum())))
+        n = max(1, min(n, int((w >= min_p).sum())))
     cum = np.cumsum(w[:n])
     u = 0.0 if math.isnan(uniform) else min(max(uniform, 0.0), 1 - 2.0 ** -24)
     at = int(np.searchsorted(cum, u * cum[-1], side="right"))

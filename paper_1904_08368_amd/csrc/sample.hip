@@ -85,8 +85,8 @@ struct Settings {
     cut_p = top_p < 1.f;
     cut_min = min_p > 0.f;
     u = fminf(fmaxf(u, 0.f), 0x1.fffffep-1f);   // (a NaN: 0)
-    greedy = !a.uniform || temperature <= 0.f || top_k == 1 || top_p <= 0.f;
-    z_min = cut_min ? log2((double)fminf(min_p, 1.f)) : 0.0;
+    greedy = !a.uniform || temperature <= 0.f || top_k == 1 || top_p <= 0.f || min_p > 1.f;   // (no w is above 1)
+    z_min = cut_min ? log2((double)min_p) : 0.0;
   }
   // What the second reading adds up: nothing, where the third finds all that min-p keeps by itself, or all that top-k keeps from some `maxima` of parts of the row: as many of them as top-k asks for
   // bound its tokens from below.  Otherwise bins' tokens, for top-k, and their masses.
