@@ -119,7 +119,7 @@ typedef struct {
  * largest, so that a result does not depend on the order of a sum; a weight below half of that is zero.
  *   logits [rows][vocab], any alignment of the type; temperature, top_p, min_p fp32, top_k int32, each [rows] or NULL (1, all, all, all); uniform
  *   fp32 [rows], or NULL: the first of each row
- *   tokens int32 [rows]; probs fp32 [rows] or NULL: w of the token over the sum of w over the kept (1 where the first is what is asked for)
+ *   tokens int32 [rows]; probs fp32 [rows] or NULL: w of the token over the sum of w over the kept (1 where the first is what is asked for); neither may overlap a setting
  * Workspace: NULL is valid (few rows then take longer).  Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (aliasing), _WORKSPACE, _DEVICE. */
 relay_status relay_sample_workspace_bytes(const relay_sample_desc* d, size_t* bytes);
 relay_status relay_sample(const relay_sample_desc* d, const void* logits, const float* temperature, const int32_t* top_k, const float* top_p,

@@ -17,6 +17,12 @@ size_t esize(int dtype) { return dtype == RELAY_F32 ? 4 : dtype == RELAY_F16 || 
 // a stride that keeps rows of `what` apart
 bool apart(int64_t stride, int rows, int64_t what) { return rows <= 1 ? stride >= 0 : stride >= what; }
 
+// whether `n` bytes from p on and `m` from q on have any in common
+bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && n && m && (a < b ? b - a < n : a - b < m);
+}
+
 relay_status check_workspace(const void* workspace, size_t bytes, size_t need) {
   if (!workspace || bytes < need) return fail(RELAY_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? bytes : 0, need);
   if (!aligned(workspace, 256)) return fail(RELAY_ERR_ALIGN, "workspace must be 256-byte aligned");
@@ -193,6 +199,11 @@ relay_status relay_sample(const relay_sample_desc* d, const void* logits, const 
     return fail(RELAY_ERR_ALIGN, "tensors must be aligned to their type");
   if (static_cast<const void*>(tokens) == probs || static_cast<const void*>(tokens) == logits || probs == logits)
     return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
+  // (all workgroups of a row read its settings, one writes its outputs)
+  const size_t numbers = (size_t)a.rows * 4;
+  for (const void* in : {static_cast<const void*>(temperature), static_cast<const void*>(top_k), static_cast<const void*>(top_p), static_cast<const void*>(min_p),
+                         static_cast<const void*>(uniform)})
+    if (overlap(tokens, numbers, in, numbers) || overlap(probs, numbers, in, numbers)) return fail(RELAY_ERR_UNSUPPORTED, "an output must not overlap a setting");
   if (workspace) {
     const size_t need = relay::sample_workspace_bytes(a);
     if (relay_status st = check_workspace(workspace, workspace_bytes, need)) return st;
