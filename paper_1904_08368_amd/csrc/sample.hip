@@ -64,6 +64,7 @@ __device__ __forceinline__ u64 part_up(float f, u64 x) {
   return __umul64hi(x, m) + (x * m != 0);
 }
 
+__device__ const float kNothing = 0.f;
 // A row's settings; those that are off as such.
 struct Settings {
   float temperature, top_p, min_p, u;
@@ -71,14 +72,15 @@ struct Settings {
   bool cut_p, cut_min, greedy;
   double z_min;
   __device__ Settings(const SampleArgs& a, int r) {
-    // (all asked for at once; what is not there is read from some place that is, and not used)
-    const float* const some = reinterpret_cast<const float*>(a.tokens);
-    const float t = (a.temperature ? a.temperature : some)[r], p = (a.top_p ? a.top_p : some)[r], m = (a.min_p ? a.min_p : some)[r], v = (a.uniform ? a.uniform : some)[r];
-    const int k = (a.top_k ? a.top_k : a.tokens)[r];
+    // (all asked for at once; what is not there is read from the uniform numbers, and not used.  Without these the first is what is asked for, whatever the rest.)
+    const float* const some = a.uniform ? a.uniform : &kNothing;
+    const int at = a.uniform ? r : 0;
+    const float t = (a.temperature ? a.temperature : some)[at], p = (a.top_p ? a.top_p : some)[at], m = (a.min_p ? a.min_p : some)[at], v = some[at];
+    const int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t*>(some))[at];
     temperature = a.temperature ? t : 1.f;
     top_p = a.top_p ? p : 1.f;
     min_p = a.min_p ? m : 0.f;
-    u = a.uniform ? v : 0.f;
+    u = v;
     top_k = a.top_k ? k : 0;
     if (!(temperature == temperature)) temperature = 1.f;
     if (top_k <= 0 || top_k >= a.vocab) top_k = 0;
