@@ -6,7 +6,7 @@
  * caller owns, preallocated outputs and scratch, work enqueued on `hip_stream`, argument checks on the host before any HIP call, a status and a
  * message on failure (paper Section 3.3, "Backends").  Strides are in elements, the innermost extent is contiguous.  What a program chooses on
  * the device (experts, settings of a row) is checked there: what names nothing is skipped.  A call without tokens or rows is valid and launches nothing.
- * Workspaces: 256-byte aligned, at least as many bytes as the call's _workspace_bytes says, zero before their first use, left ready for the next call
+ * Workspaces: 256-byte aligned, at least as many bytes as the call's _workspace_bytes says, apart from all operands, zero before their first use, left ready for the next call
  * of the same operator that asks for no more.  Operators, and calls that may run at the same time, need workspaces of their own.
  *
  * One block, beside its attention layer: relay_residual_norm -> relay_route -> relay_experts_w4 -> relay_residual_norm.
@@ -64,7 +64,7 @@ typedef struct {
  * the order of a sum; weights are rounded once, to fp32.  A sum of zero leaves weights of zero.
  *   x [tokens][channels], 16-byte aligned with x_stride a multiple of 8; w [experts][channels], 16-byte aligned; bias fp32 [experts] or NULL
  *   chosen int32, weights fp32 [tokens][top_k]
- * Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED, _WORKSPACE (the workspace is required), _DEVICE. */
+ * Errors: _NULL, _DTYPE, _SHAPE, _ALIGN, _UNSUPPORTED (score, normalize, aliasing), _WORKSPACE (the workspace is required), _DEVICE. */
 relay_status relay_route_workspace_bytes(const relay_route_desc* d, size_t* bytes);
 relay_status relay_route(const relay_route_desc* d, const void* x, const void* w, const float* bias, int32_t* chosen, float* weights,
                          void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -1,6 +1,7 @@
 // C-ABI layer of a decoder's operators beside its attention layer (relay_decoder.h): argument checks on the host, then dispatch.
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "../../include/relay_decoder.h"
 #include "api_common.hpp"
@@ -17,15 +18,27 @@ size_t esize(int dtype) { return dtype == RELAY_F32 ? 4 : dtype == RELAY_F16 || 
 // a stride that keeps rows of `what` apart
 bool apart(int64_t stride, int rows, int64_t what) { return rows <= 1 ? stride >= 0 : stride >= what; }
 
-// whether `n` bytes from p on and `m` from q on have any in common
-bool overlap(const void* p, size_t n, const void* q, size_t m) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && n && m && (a < b ? b - a < n : a - b < m);
+// `rows` pieces of `bytes` bytes, `stride` bytes from one to the next
+struct Operand {
+  const void* at;
+  size_t bytes;
+  int64_t rows = 1, stride = 0;
+};
+// whether any of an operand lies within `size` bytes from `from` on
+bool overlap(const Operand& o, const void* from, size_t size) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(o.at), q = reinterpret_cast<uintptr_t>(from);
+  if (!o.at || !from || !o.bytes || !size || o.rows <= 0 || p >= q + size) return false;
+  if (p + o.bytes > q) return true;
+  if (o.stride <= 0) return false;
+  const uintptr_t i = (q - p - o.bytes) / (uintptr_t)o.stride + 1;   // the first piece that ends behind q
+  return i < (uintptr_t)o.rows && p + i * (uintptr_t)o.stride < q + size;
 }
 
-relay_status check_workspace(const void* workspace, size_t bytes, size_t need) {
+relay_status check_workspace(const void* workspace, size_t bytes, size_t need, std::initializer_list<Operand> operands) {
   if (!workspace || bytes < need) return fail(RELAY_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? bytes : 0, need);
   if (!aligned(workspace, 256)) return fail(RELAY_ERR_ALIGN, "workspace must be 256-byte aligned");
+  for (const Operand& o : operands)
+    if (overlap(o, workspace, need)) return fail(RELAY_ERR_UNSUPPORTED, "the workspace must not overlap an operand");
   return RELAY_OK;
 }
 
@@ -115,7 +128,10 @@ relay_status relay_route(const relay_route_desc* d, const void* x, const void* w
   if (!aligned(bias, 4) || !aligned(chosen, 4) || !aligned(weights, 4)) return fail(RELAY_ERR_ALIGN, "bias, chosen and weights must be aligned to their type");
   if (static_cast<const void*>(chosen) == weights || chosen == x || weights == x || chosen == w || weights == w || (bias && (weights == bias || static_cast<const void*>(chosen) == bias)))
     return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
-  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_bytes(a))) return st;
+  const size_t row = (size_t)a.channels * 2, choices = (size_t)a.tokens * a.top_k * 4;
+  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_bytes(a),
+                                        {{x, row, a.tokens, a.x_stride * 2}, {w, (size_t)a.experts * row}, {bias, (size_t)a.experts * 4}, {chosen, choices}, {weights, choices}}))
+    return st;
   a.x = x; a.w = w; a.bias = bias; a.chosen = chosen; a.weights = weights; a.workspace = workspace;
   return device_status(relay::launch_route(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "router launch");
 }
@@ -161,7 +177,11 @@ relay_status relay_experts_w4(const relay_experts_w4_desc* d, const void* x, con
   if (!aligned(y, 2) || !aligned(residual, 2) || !aligned(chosen, 4) || !aligned(weights, 4))
     return fail(RELAY_ERR_ALIGN, "y, residual, chosen and weights must be aligned to their type");
   if (y == x || y == gate_up || y == down || y == chosen || y == weights || y == workspace) return fail(RELAY_ERR_UNSUPPORTED, "output must not alias an input");
-  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::experts_workspace_bytes(a))) return st;
+  const size_t row = (size_t)a.channels * 2, choices = (size_t)a.tokens * a.top_k * 4;
+  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::experts_workspace_bytes(a),
+                                        {{x, row, a.tokens, a.x_stride * 2}, {chosen, choices}, {weights, choices}, {gate_up, relay::experts_packed_bytes(a, true)},
+                                         {down, relay::experts_packed_bytes(a, false)}, {residual, row, a.tokens, a.y_stride * 2}, {y, row, a.tokens, a.y_stride * 2}}))
+    return st;
   a.x = x; a.chosen = chosen; a.weights = weights; a.gate_up = gate_up; a.down = down; a.res = residual; a.y = y; a.workspace = workspace;
   return device_status(relay::launch_experts(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "experts launch");
 }
@@ -203,10 +223,14 @@ relay_status relay_sample(const relay_sample_desc* d, const void* logits, const 
   const size_t numbers = (size_t)a.rows * 4;
   for (const void* in : {static_cast<const void*>(temperature), static_cast<const void*>(top_k), static_cast<const void*>(top_p), static_cast<const void*>(min_p),
                          static_cast<const void*>(uniform)})
-    if (overlap(tokens, numbers, in, numbers) || overlap(probs, numbers, in, numbers)) return fail(RELAY_ERR_UNSUPPORTED, "an output must not overlap a setting");
+    if (overlap({tokens, numbers}, in, numbers) || overlap({probs, numbers}, in, numbers)) return fail(RELAY_ERR_UNSUPPORTED, "an output must not overlap a setting");
   if (workspace) {
     const size_t need = relay::sample_workspace_bytes(a);
-    if (relay_status st = check_workspace(workspace, workspace_bytes, need)) return st;
+    const size_t es = esize(d->dtype);
+    if (relay_status st = check_workspace(workspace, workspace_bytes, need,
+                                          {{logits, a.vocab * es, a.rows, a.logits_stride * (int64_t)es}, {temperature, numbers}, {top_k, numbers}, {top_p, numbers}, {min_p, numbers},
+                                           {uniform, numbers}, {tokens, numbers}, {probs, numbers}}))
+      return st;
     a.workspace = need ? workspace : nullptr;
   }
   a.logits = logits; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.uniform = uniform;

@@ -72,6 +72,10 @@ struct ExpertsArgs {
   // (a group as long as the row is the row's chunks of 128, whole, as for the dense layers)
   __host__ __device__ int group_of(int k) const { return group < k ? group : (k + 127) / 128 * 128; }
 };
+// of the packed weights that a call reads
+inline size_t experts_packed_bytes(const ExpertsArgs& a, bool up) {
+  return up ? w4_layout(a.experts * 2 * a.inter, a.channels, a.group_of(a.channels), a.zeros != 0).bytes : w4_layout(a.experts * a.channels, a.inter, a.group_of(a.inter), a.zeros != 0).bytes;
+}
 size_t experts_workspace_bytes(const ExpertsArgs& a);
 hipError_t launch_experts(const ExpertsArgs& a, int dtype, hipStream_t st);
 
