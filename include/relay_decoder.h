@@ -7,7 +7,7 @@
  * message on failure (paper Section 3.3, "Backends").  Strides are in elements, the innermost extent is contiguous.  What a program chooses on
  * the device (experts, settings of a row) is checked there: what names nothing is skipped.  A call without tokens or rows is valid and launches nothing.
  * Workspaces: 256-byte aligned, at least as many bytes as the call's _workspace_bytes says, apart from all operands, zero before their first use, left ready for the next call
- * of the same operator that asks for no more.  Operators, and calls that may run at the same time, need workspaces of their own.
+ * of the same operator that asks for no more.  What _workspace_bytes says also suffices for fewer tokens or rows of the same descriptor.  Operators, and calls that may run at the same time, need workspaces of their own.
  *
  * One block, beside its attention layer: relay_residual_norm -> relay_route -> relay_experts_w4 -> relay_residual_norm.
  */

@@ -129,7 +129,7 @@ relay_status relay_route(const relay_route_desc* d, const void* x, const void* w
   if (static_cast<const void*>(chosen) == weights || chosen == x || weights == x || chosen == w || weights == w || (bias && (weights == bias || static_cast<const void*>(chosen) == bias)))
     return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
   const size_t row = (size_t)a.channels * 2, choices = (size_t)a.tokens * a.top_k * 4;
-  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_bytes(a),
+  if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_need(a),
                                         {{x, row, a.tokens, a.x_stride * 2}, {w, (size_t)a.experts * row}, {bias, (size_t)a.experts * 4}, {chosen, choices}, {weights, choices}}))
     return st;
   a.x = x; a.w = w; a.bias = bias; a.chosen = chosen; a.weights = weights; a.workspace = workspace;
@@ -225,7 +225,7 @@ relay_status relay_sample(const relay_sample_desc* d, const void* logits, const 
                          static_cast<const void*>(uniform)})
     if (overlap({tokens, numbers}, in, numbers) || overlap({probs, numbers}, in, numbers)) return fail(RELAY_ERR_UNSUPPORTED, "an output must not overlap a setting");
   if (workspace) {
-    const size_t need = relay::sample_workspace_bytes(a);
+    const size_t need = relay::sample_workspace_need(a);
     const size_t es = esize(d->dtype);
     if (relay_status st = check_workspace(workspace, workspace_bytes, need,
                                           {{logits, a.vocab * es, a.rows, a.logits_stride * (int64_t)es}, {temperature, numbers}, {top_k, numbers}, {top_p, numbers}, {min_p, numbers},

@@ -45,7 +45,8 @@ struct RouteArgs {
   int splits;           // parts of the channels whose sums are left apart
 };
 constexpr int kRouteExperts = 1024, kRouteTopK = 64, kRouteChannels = 1 << 24;   // (channels: what 32-bit places in a row leave room for)
-size_t route_workspace_bytes(const RouteArgs& a);
+size_t route_workspace_need(const RouteArgs& a);    // of this call
+size_t route_workspace_bytes(const RouteArgs& a);   // of it and of any with fewer tokens
 hipError_t launch_route(const RouteArgs& a, int dtype, hipStream_t st);
 
 enum : int { A_SILU = 0, A_GELU = 1 };  // RELAY_ACT_*
@@ -94,7 +95,8 @@ struct SampleArgs {
   int scale_bits;   // set by the launcher
 };
 constexpr int kVocab = 1 << 20;
-size_t sample_workspace_bytes(const SampleArgs& a);
+size_t sample_workspace_need(const SampleArgs& a);    // of this call
+size_t sample_workspace_bytes(const SampleArgs& a);   // of it and of any with fewer rows
 hipError_t launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
 
 }  // namespace relay

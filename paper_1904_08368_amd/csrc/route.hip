@@ -251,11 +251,22 @@ int splits_of(int tokens, int experts, int channels) {
   return s < 1 ? 1 : s > 4 ? 4 : s;   // (four: what the last workgroup fetches of a logit at once)
 }
 
+size_t route_bytes(const RouteArgs& a, int parts) { return kRouteCounterBytes + ((size_t)parts * a.experts * 8 + 255) / 256 * 256; }
+
 }  // namespace
 
+size_t route_workspace_need(const RouteArgs& a) {
+  const int tokens = a.tokens < kAtOnce ? a.tokens : kAtOnce;
+  return route_bytes(a, tokens * splits_of(tokens, a.experts, a.channels));
+}
 size_t route_workspace_bytes(const RouteArgs& a) {
   const int tokens = a.tokens < kAtOnce ? a.tokens : kAtOnce;
-  return kRouteCounterBytes + ((size_t)tokens * a.experts * 8 * splits_of(tokens, a.experts, a.channels) + 255) / 256 * 256;
+  int most = tokens;   // parts of an expert's logits: tokens times splits
+  for (int s = 2; s <= 4; ++s) {
+    const int up_to = 16 * (256 / s / ((a.experts + 15) / 16)), t = tokens < up_to ? tokens : up_to;   // the most tokens that may have as many splits
+    if (t > 0 && splits_of(t, a.experts, a.channels) >= s && t * s > most) most = t * s;
+  }
+  return route_bytes(a, most);
 }
 
 hipError_t launch_route(const RouteArgs& args, int dtype, hipStream_t st) {

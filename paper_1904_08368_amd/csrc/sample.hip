@@ -916,7 +916,13 @@ int parts_of(const SampleArgs& a) {
 
 }  // namespace
 
-size_t sample_workspace_bytes(const SampleArgs& a) { return parts_of(a) > 1 ? (size_t)a.rows * sizeof(Shared) : 0; }
+size_t sample_workspace_need(const SampleArgs& a) { return parts_of(a) > 1 ? (size_t)a.rows * sizeof(Shared) : 0; }
+size_t sample_workspace_bytes(const SampleArgs& a) {
+  SampleArgs b = a;
+  for (b.rows = a.rows < 128 ? a.rows : 128; b.rows > 0; b.rows = 256 / (256 / b.rows + 1))   // (the most rows that have a share more each; more than 128 have one)
+    if (parts_of(b) > 1) return sample_workspace_need(b);
+  return 0;
+}
 
 hipError_t launch_sample(const SampleArgs& args, int dtype, hipStream_t st) {
   SampleArgs a = args;
