@@ -362,7 +362,7 @@ struct Row {
   __device__ __forceinline__ void around(float a, float b, float* at, float* reach) const {
     *at = half_top - 0.5f * (a + b);
     *reach = 0.5f * (b - a) + 1e-6f * (fabsf(half_top) + b);
-    if (!(fabsf(*at) < FLT_MAX) || !(*reach < FLT_MAX) || top == FLT_MAX) *at = 0.f, *reach = __builtin_inff();   // (all of them)
+    if (!(fabsf(*at) < FLT_MAX) || !(*reach < FLT_MAX) || top == FLT_MAX || to_bin == 0.f) *at = 0.f, *reach = __builtin_inff();   // (all of them: also where bins have no width, and the first holds all)
     *at = uniform(*at), *reach = uniform(*reach);
   }
   __device__ __forceinline__ Near near_bins() const {
