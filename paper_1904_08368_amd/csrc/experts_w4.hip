@@ -630,7 +630,8 @@ hipError_t launch_type(const ExpertsArgs& a, hipStream_t st) {
 }
 
 constexpr int kPairs = 4096;   // of a launch at most
-int tokens_at_once(const ExpertsArgs& a) { return a.top_k >= kPairs ? 1 : kPairs / a.top_k; }
+static_assert(kRouteTopK <= kPairs, "a token's pairs");
+int tokens_at_once(const ExpertsArgs& a) { return kPairs / a.top_k; }
 size_t blocks_of(int pairs, int experts) { return (size_t)(pairs < experts ? pairs : experts) + pairs / kBlock; }   // at most
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 

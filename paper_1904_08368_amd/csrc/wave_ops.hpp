@@ -64,8 +64,5 @@ __device__ __forceinline__ V wave_fold64(V v, F f) {
   return f(halves.a, halves.b);
 }
 __device__ __forceinline__ double wave_sum64(double v) { return wave_fold64(v, [](double a, double b) { return a + b; }); }
-__device__ __forceinline__ unsigned long long wave_max64(unsigned long long v) {
-  return wave_fold64(v, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
-}
 
 }  // namespace relay
