@@ -84,7 +84,8 @@ typedef struct {
 } relay_experts_w4_desc;
 
 /* y[t] = sum_s weights[t][s] * down_e (act(gate_e x[t]) * up_e x[t])  [+ residual[t]],   e = chosen[t][s]
- * for few tokens, where the chosen experts' codes are most of what there is to read: each is read once for all the tokens that chose it.
+ * for few tokens, where the chosen experts' codes are most of what there is to read: each is read once for 4, 8 or 16 of the tokens that chose it (as many as that are on the
+ * mean, from the numbers of tokens and experts), or for 64 where experts have many.
  * act * up is rounded to the tensors' type for the second product (an operand of the matrix cores; past the type's range it is an infinity); sums are fp32, in a fixed order, and
  * weights are applied to them.
  * Two launches for up to 8 or 16 choices, three or four for more (of up to 4096 at a time): what is elementwise goes into the products' ends (paper
