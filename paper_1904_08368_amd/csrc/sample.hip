@@ -608,10 +608,11 @@ struct Row {
     for (;;) {
       vec first[2];
       load(first, piece0 + tid);
-      const int m = gather([&](float l) {
+      auto here = [&](float l) {
         const float d = distance(l);
         return weighs(d) && bin(d) == b && (shift == 32 || key_of(l) >> shift == prefix);
-      }, [](float) { return true; }, first);
+      };
+      const int m = gather(here, here, first);
       if (m <= CAP) {
         sort(m, false);
         const int i = kind == RANK ? (int)goal - 1 : kind == REACH ? first_of<false>(s.run, m, goal) : first_of<true>(s.run, m, goal);
