@@ -605,6 +605,7 @@ struct Row {
     unsigned prefix = 0;
     int shift = 32;
     u64 base = 0;
+    __syncthreads();   // (the next gathering clears s.listed, which a late wave may still be reading behind the one before)
     for (;;) {
       vec first[2];
       load(first, piece0 + tid);
