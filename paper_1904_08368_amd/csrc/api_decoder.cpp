@@ -22,16 +22,17 @@ bool apart(int64_t stride, int rows, int64_t what) { return rows <= 1 ? stride >
 struct Operand {
   const void* at;
   size_t bytes;
-  int64_t rows = 1, stride = 0;
+  int64_t rows = 1;
+  uint64_t stride = 0;
 };
 // whether any of an operand lies within `size` bytes from `from` on
 bool overlap(const Operand& o, const void* from, size_t size) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(o.at), q = reinterpret_cast<uintptr_t>(from);
   if (!o.at || !from || !o.bytes || !size || o.rows <= 0 || p >= q + size) return false;
   if (p + o.bytes > q) return true;
-  if (o.stride <= 0) return false;
-  const uintptr_t i = (q - p - o.bytes) / (uintptr_t)o.stride + 1;   // the first piece that ends behind q
-  return i < (uintptr_t)o.rows && p + i * (uintptr_t)o.stride < q + size;
+  if (o.stride == 0) return false;
+  const uintptr_t i = (q - p - o.bytes) / o.stride + 1;   // the first piece that ends behind q
+  return i < (uintptr_t)o.rows && p + i * o.stride < q + size;
 }
 
 relay_status check_workspace(const void* workspace, size_t bytes, size_t need, std::initializer_list<Operand> operands) {
@@ -130,7 +131,7 @@ relay_status relay_route(const relay_route_desc* d, const void* x, const void* w
     return fail(RELAY_ERR_UNSUPPORTED, "an output must not alias another operand");
   const size_t row = (size_t)a.channels * 2, choices = (size_t)a.tokens * a.top_k * 4;
   if (relay_status st = check_workspace(workspace, workspace_bytes, relay::route_workspace_need(a),
-                                        {{x, row, a.tokens, a.x_stride * 2}, {w, (size_t)a.experts * row}, {bias, (size_t)a.experts * 4}, {chosen, choices}, {weights, choices}}))
+                                        {{x, row, a.tokens, (uint64_t)a.x_stride * 2}, {w, (size_t)a.experts * row}, {bias, (size_t)a.experts * 4}, {chosen, choices}, {weights, choices}}))
     return st;
   a.x = x; a.w = w; a.bias = bias; a.chosen = chosen; a.weights = weights; a.workspace = workspace;
   return device_status(relay::launch_route(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "router launch");
@@ -179,8 +180,8 @@ relay_status relay_experts_w4(const relay_experts_w4_desc* d, const void* x, con
   if (y == x || y == gate_up || y == down || y == chosen || y == weights || y == workspace) return fail(RELAY_ERR_UNSUPPORTED, "output must not alias an input");
   const size_t row = (size_t)a.channels * 2, choices = (size_t)a.tokens * a.top_k * 4;
   if (relay_status st = check_workspace(workspace, workspace_bytes, relay::experts_workspace_bytes(a),
-                                        {{x, row, a.tokens, a.x_stride * 2}, {chosen, choices}, {weights, choices}, {gate_up, relay::experts_packed_bytes(a, true)},
-                                         {down, relay::experts_packed_bytes(a, false)}, {residual, row, a.tokens, a.y_stride * 2}, {y, row, a.tokens, a.y_stride * 2}}))
+                                        {{x, row, a.tokens, (uint64_t)a.x_stride * 2}, {chosen, choices}, {weights, choices}, {gate_up, relay::experts_packed_bytes(a, true)},
+                                         {down, relay::experts_packed_bytes(a, false)}, {residual, row, a.tokens, (uint64_t)a.y_stride * 2}, {y, row, a.tokens, (uint64_t)a.y_stride * 2}}))
     return st;
   a.x = x; a.chosen = chosen; a.weights = weights; a.gate_up = gate_up; a.down = down; a.res = residual; a.y = y; a.workspace = workspace;
   return device_status(relay::launch_experts(a, d->dtype, static_cast<hipStream_t>(hip_stream)), "experts launch");
@@ -228,7 +229,7 @@ relay_status relay_sample(const relay_sample_desc* d, const void* logits, const 
     const size_t need = relay::sample_workspace_need(a);
     const size_t es = esize(d->dtype);
     if (relay_status st = check_workspace(workspace, workspace_bytes, need,
-                                          {{logits, a.vocab * es, a.rows, a.logits_stride * (int64_t)es}, {temperature, numbers}, {top_k, numbers}, {top_p, numbers}, {min_p, numbers},
+                                          {{logits, a.vocab * es, a.rows, (uint64_t)a.logits_stride * es}, {temperature, numbers}, {top_k, numbers}, {top_p, numbers}, {min_p, numbers},
                                            {uniform, numbers}, {tokens, numbers}, {probs, numbers}}))
       return st;
     a.workspace = need ? workspace : nullptr;

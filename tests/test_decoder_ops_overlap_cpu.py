@@ -65,3 +65,14 @@ def test_a_workspace_between_the_rows_of_an_operand():
 def _set(d, field, value):
     setattr(d._obj, field, value)
     return d
+
+
+def test_strides_at_the_end_of_their_type():
+    """A call of one row may have any stride: it is not multiplied out as a signed number."""
+    far = 2 ** 63 - 8
+    for operator, (call, desc, _) in OPERANDS.items():
+        d = _set(_set(desc(), "rows" if operator == "sample" else "tokens", 1), "logits_stride" if operator == "sample" else "x_stride", far)
+        given = dict(ws=at(40), ws_bytes=_need(operator, d))
+        if operator == "experts_w4":
+            given["residual"] = at(5)
+        assert call(d, **given) not in (2, 4, 6)

@@ -18,7 +18,7 @@ def test_tiny_differences(B, dtype, rows, vocab, power):
         for u in (0.0, 0.3, 0.99):
             _check(B, logits, uniform=u, **more)
             _check(B, -logits, uniform=u, **more)
-        # min-p of 1 keeps the largest alone: exp of anything below zero is less than 1, which 64 bits of the weight itself (and so the checker) do not tell; the kernels compare exponents.
+        # min-p of 1 keeps the largest alone: exp of anything below zero is less than 1, which 64 bits of the weight itself (and so the oracle) do not tell; the kernels compare exponents.
         _, args = _check(B, logits, uniform=0.5, top_k=1)
         tokens, probs = args[6].clone(), args[7].clone()
         B.relay_sample(B.sample_desc(logits), logits, None, None, None, torch.ones(rows, device=DEV), torch.full((rows,), 0.0, device=DEV), tokens, probs, args[8])
